@@ -19,6 +19,10 @@
  *   pvlm_topk_select    Eq. (topk_selection): keep the top 1 - alpha fraction;
  *                       pvlm_uvprune_topk_mass with the MASS score in one call
  *   pvlm_gather_kv      the draft's compact cache [V*, X] (Sec. 4.2, Stage I)
+ *   pvlm_rope_append_q8, pvlm_quantize_kv, pvlm_verify_attn_q8,
+ *   pvlm_gather_kv_q8   append, verify and gather over a cache of 8-bit rows,
+ *                       padded or paged, and the rows of a 16- or 32-bit cache
+ *                       into one
  *   pvlm_spec_accept    speculative-sampling accept/reject (Sec. 2.2) with the
  *                       bonus token of Suppl. B
  *   pvlm_set_stream_cu_budget  compute-unit budgets, so the draft's and the
@@ -94,7 +98,9 @@ typedef enum {
   PVLM_ERR_HIP = 5           /* a HIP call failed; see pvlm_last_hip_error()   */
 } pvlm_status;
 
-typedef enum { PVLM_F32 = 0, PVLM_BF16 = 1 } pvlm_dtype;
+/* PVLM_E4M3: 8-bit cache rows (see pvlm_rope_append_q8), taken only where a call
+ * says so. */
+typedef enum { PVLM_F32 = 0, PVLM_BF16 = 1, PVLM_E4M3 = 2 } pvlm_dtype;
 
 /* Criterion fed to UV-Prune's variation operator. */
 typedef enum {
@@ -442,6 +448,139 @@ pvlm_status pvlm_gather_kv_paged(pvlm_dtype dt, int n_layers, int B, int Hkv, in
                                  int32_t k_cap, const int32_t* tail_begin,
                                  const int32_t* tail_len, int64_t dst_cap, void* k_dst,
                                  void* v_dst, int32_t* status, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * 8-bit caches.  The verify step is bound by the bytes of a long video cache;
+ * these calls keep its rows in 8 bits, half of bf16.
+ *
+ * A row x of D values (one position, one KV head, K or V) is D e4m3 codes (OCP
+ * 8-bit floats: 4 exponent and 3 mantissa bits, largest 448, 0x7f and 0xff NaN)
+ * and one exponent byte e, and stands for code_i * 2^(e - 127):
+ *   e      = the smallest integer in [1, 254] with max |x_i| <= 448 * 2^(e - 127)
+ *            over the row's finite x_i (1 for a row of zeros),
+ *   code_i = x_i * 2^(127 - e) rounded to nearest, ties to even; an infinity or
+ *            NaN becomes NaN.
+ * The scaling is exact, so a code is off by at most half a step, 2^-4 of its
+ * value (2^-10 * 2^(e - 127) for values below 2^-6 * 2^(e - 127)).
+ *   padded  codes [B][Hkv][n_cap][D], exponents [B][Hkv][n_cap]; n_cap is a
+ *           multiple of 32 (PVLM_ERR_SHAPE).
+ *   paged   codes [n_pages][Hkv][page_size][D], exponents [n_pages][Hkv]
+ *           [page_size], page_size and page_table as for
+ *           pvlm_verify_attn_paged; logical capacity n_cap = max_pages *
+ *           page_size.
+ * Of a cache written by other means, exponent bytes 0 and 255 have no value
+ * here (a result that one enters is unspecified).  D is 64 or 128
+ * (PVLM_ERR_UNSUPPORTED).  Pointers of codes are 16-byte aligned, of exponents
+ * 4-byte, of q_in, k_in, v_in and q_out 8-byte, of q, sources, bf16 or fp32
+ * destinations and workspaces 16-byte (PVLM_ERR_UNSUPPORTED, PVLM_ERR_WORKSPACE
+ * for the last).  None of these launches waits for another workgroup, captured
+ * or not.
+ *
+ * pvlm_rope_append_q8(_paged) -- pvlm_rope_append into an 8-bit cache: rotated
+ * queries to q_out (bf16, as pvlm_rope_append gives them), the rotated keys
+ * rounded to bf16 and then quantised, the values quantised.  The rows written
+ * are therefore those that pvlm_quantize_kv makes of the cache that
+ * pvlm_rope_append writes.  T may be a whole prompt (ctx_len 0).  dt PVLM_BF16 only
+ * (PVLM_ERR_UNSUPPORTED).  Arguments, flags and errors are otherwise those of
+ * pvlm_rope_append(_paged); PVLM_ERR_SHAPE for B * T > 2^24 - 1.
+ * ---------------------------------------------------------------------- */
+pvlm_status pvlm_rope_append_q8(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
+                                double base, const int32_t* sections, const int32_t* pos,
+                                const void* q_in, const void* k_in, const void* v_in,
+                                const int32_t* ctx_len, void* q_out, uint8_t* k_codes,
+                                uint8_t* k_exps, uint8_t* v_codes, uint8_t* v_exps,
+                                int32_t* status, hipStream_t stream);
+pvlm_status pvlm_rope_append_q8_paged(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D,
+                                      int page_size, int max_pages, int64_t n_pages, double base,
+                                      const int32_t* sections, const int32_t* pos, const void* q_in,
+                                      const void* k_in, const void* v_in, const int32_t* page_table,
+                                      const int32_t* ctx_len, void* q_out, uint8_t* k_codes,
+                                      uint8_t* k_exps, uint8_t* v_codes, uint8_t* v_exps,
+                                      int32_t* status, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * pvlm_quantize_kv(_paged) -- rows 0 .. len[b] - 1 of a cache that a prefill left
+ * (post-rotation K, and V), of every layer, into an 8-bit cache (row format
+ * above); rows past len[b] are left as they were.
+ *   dt            PVLM_BF16 or PVLM_F32.
+ *   k_src, v_src  [n_layers][B][Hkv][src_cap][D]; len [B] int32 device.
+ *   codes, exps   the caches above, n_layers of them in a row; one page table
+ *                 serves every layer.
+ * A len[b] outside [0, min(src_cap, n_cap)] is clamped into it and flagged
+ * PVLM_DEV_RANGE; a row whose page entry lies outside the pool is skipped and
+ * flagged.  n_layers * B <= 65535, Hkv <= 65535, src_cap <= 2^30.
+ * ---------------------------------------------------------------------- */
+pvlm_status pvlm_quantize_kv(pvlm_dtype dt, int n_layers, int B, int Hkv, int D, int64_t src_cap,
+                             const void* k_src, const void* v_src, const int32_t* len,
+                             int64_t n_cap, uint8_t* k_codes, uint8_t* k_exps, uint8_t* v_codes,
+                             uint8_t* v_exps, int32_t* status, hipStream_t stream);
+pvlm_status pvlm_quantize_kv_paged(pvlm_dtype dt, int n_layers, int B, int Hkv, int D,
+                                   int page_size, int max_pages, int64_t n_pages, int64_t src_cap,
+                                   const void* k_src, const void* v_src, const int32_t* len,
+                                   const int32_t* page_table, uint8_t* k_codes, uint8_t* k_exps,
+                                   uint8_t* v_codes, uint8_t* v_exps, int32_t* status,
+                                   hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * pvlm_verify_attn_q8(_paged) -- pvlm_verify_attn(_paged) over an 8-bit cache:
+ * the same definition with k_i and v_i the values that the rows stand for; T = 1
+ * with mass = NULL is a decode step.  q and out are bf16 (dt PVLM_BF16;
+ * PVLM_ERR_UNSUPPORTED otherwise) and q is not rounded further; scores, softmax
+ * statistics and sums are fp32, P is rounded to bf16 before P . V.
+ * A value of NaN reaches the rows that see it and no other; cache rows at and
+ * past ctx_len[b] + T are not used, whatever they hold.
+ *   ws    >= pvlm_verify_attn_q8_workspace_size() bytes (under every compute-unit
+ *         budget).
+ * Other arguments, flags and errors are those of pvlm_verify_attn(_paged);
+ * PVLM_ERR_SHAPE for B * Hq * T > 2^22.
+ * ---------------------------------------------------------------------- */
+size_t pvlm_verify_attn_q8_workspace_size(int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
+                                          int64_t max_ctx);
+pvlm_status pvlm_verify_attn_q8(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
+                                int64_t max_ctx, float scale, const void* q,
+                                const uint8_t* k_codes, const uint8_t* k_exps,
+                                const uint8_t* v_codes, const uint8_t* v_exps,
+                                const int32_t* ctx_len, void* out, float* mass, float* lse,
+                                void* ws, size_t ws_bytes, int32_t* status, hipStream_t stream);
+pvlm_status pvlm_verify_attn_q8_paged(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D,
+                                      int page_size, int max_pages, int64_t n_pages,
+                                      int64_t max_ctx, float scale, const void* q,
+                                      const uint8_t* k_codes, const uint8_t* k_exps,
+                                      const uint8_t* v_codes, const uint8_t* v_exps,
+                                      const int32_t* page_table, const int32_t* ctx_len, void* out,
+                                      float* mass, float* lse, void* ws, size_t ws_bytes,
+                                      int32_t* status, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * pvlm_gather_kv_q8(_paged) -- pvlm_gather_kv(_paged) from an 8-bit cache.  The
+ * draft's compact cache is
+ *   dst_dt PVLM_E4M3            an 8-bit cache again (codes and exponents copied;
+ *                               dst_cap a multiple of 32), or
+ *   dst_dt PVLM_BF16, PVLM_F32  the values that the rows stand for (exact, but
+ *                               that a bf16 value under 2^-126 is rounded);
+ *                               k_dst_exps and v_dst_exps are then not used.
+ *   fill                        0: destination rows past k[b] + tail_len[b], and
+ *                               skipped ones, are left as they were; else they
+ *                               are written 0 (for a destination that is new).
+ * Source rows, order, clamps, flags and limits are those of
+ * pvlm_gather_kv(_paged).
+ * ---------------------------------------------------------------------- */
+pvlm_status pvlm_gather_kv_q8(pvlm_dtype dst_dt, int n_layers, int B, int Hkv, int D, int64_t n_cap,
+                              const uint8_t* k_codes, const uint8_t* k_exps,
+                              const uint8_t* v_codes, const uint8_t* v_exps, const int32_t* idx,
+                              const int32_t* k, int32_t k_cap, const int32_t* tail_begin,
+                              const int32_t* tail_len, int64_t dst_cap, int fill,
+                              void* k_dst, uint8_t* k_dst_exps, void* v_dst,
+                              uint8_t* v_dst_exps, int32_t* status, hipStream_t stream);
+pvlm_status pvlm_gather_kv_q8_paged(pvlm_dtype dst_dt, int n_layers, int B, int Hkv, int D,
+                                    int page_size, int max_pages, int64_t n_pages,
+                                    const uint8_t* k_codes, const uint8_t* k_exps,
+                                    const uint8_t* v_codes, const uint8_t* v_exps,
+                                    const int32_t* page_table, const int32_t* idx,
+                                    const int32_t* k, int32_t k_cap, const int32_t* tail_begin,
+                                    const int32_t* tail_len, int64_t dst_cap, int fill,
+                                    void* k_dst, uint8_t* k_dst_exps, void* v_dst,
+                                    uint8_t* v_dst_exps, int32_t* status, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
  * pvlm_spec_accept -- speculative-sampling accept/reject (Sec. 2.2) with the

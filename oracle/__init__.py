@@ -34,6 +34,8 @@ explicit loops over the indices the paper sums over, following the paper:
 * ``paged``            -- verify attention, rope append and the compact-cache
                           gather over a paged cache, every row read or
                           written through the page table.
+* ``quant``            -- rows of an 8-bit KV cache: e4m3 codes and a power of two
+                          per row.
 
 Parity status: every function here is pinned by the ``-m "not gpu"`` tests in
 ``tests/test_oracle_*.py`` against brute force, closed forms, library routines
@@ -44,7 +46,7 @@ from .uvprune import (cos_similarity, criterion_cossim, prefill_epilogue, uvprun
                       uvprune_score_mass)
 from .select import topk_keys, topk_select, gather_kv
 from .accept import spec_accept, softmax_t, NEAR_TIE_REL
-from . import paged, pipeline, rope, window
+from . import paged, pipeline, quant, rope, window
 
 __all__ = [
     "verify_attn", "verify_attn_rows", "cos_similarity", "criterion_cossim", "prefill_epilogue",

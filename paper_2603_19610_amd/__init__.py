@@ -20,7 +20,7 @@ import torch
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libpvlm.so")
 
-PVLM_F32, PVLM_BF16 = 0, 1
+PVLM_F32, PVLM_BF16, PVLM_E4M3 = 0, 1, 2
 PVLM_CRIT_MASS, PVLM_CRIT_COSSIM = 0, 1
 PVLM_DEV_RANGE, PVLM_DEV_TIMEOUT, PVLM_DEV_PLACEMENT = 1, 2, 4
 
@@ -33,6 +33,9 @@ EXPORTS = (
     "pvlm_prefill_epilogue_cossim",
     "pvlm_topk_workspace_size", "pvlm_topk_select", "pvlm_uvprune_topk_mass",
     "pvlm_gather_kv", "pvlm_gather_kv_paged",
+    "pvlm_rope_append_q8", "pvlm_rope_append_q8_paged", "pvlm_quantize_kv", "pvlm_quantize_kv_paged",
+    "pvlm_verify_attn_q8_workspace_size", "pvlm_verify_attn_q8", "pvlm_verify_attn_q8_paged",
+    "pvlm_gather_kv_q8", "pvlm_gather_kv_q8_paged",
     "pvlm_spec_accept_workspace_size", "pvlm_spec_accept",
     "pvlm_rope_append", "pvlm_rope_append_paged",
     "pvlm_speedup", "pvlm_window_size",
@@ -131,6 +134,19 @@ _SIGS = {
                               _P, _P, _P]),
     "pvlm_rope_append_paged": (_I, [_I, _I, _I, _I, _I, _I, _I, _I, _I64, _D, _P, _P, _P, _P, _P,
                                     _P, _P, _P, _P, _P, _P, _P]),
+    "pvlm_rope_append_q8": (_I, [_I, _I, _I, _I, _I, _I, _I64, _D] + [_P] * 13),
+    "pvlm_rope_append_q8_paged": (_I, [_I, _I, _I, _I, _I, _I, _I, _I, _I64, _D] + [_P] * 14),
+    "pvlm_quantize_kv": (_I, [_I, _I, _I, _I, _I, _I64, _P, _P, _P, _I64] + [_P] * 6),
+    "pvlm_quantize_kv_paged": (_I, [_I, _I, _I, _I, _I, _I, _I, _I64, _I64] + [_P] * 10),
+    "pvlm_verify_attn_q8_workspace_size": (_SZ, [_I, _I, _I, _I, _I, _I64, _I64]),
+    "pvlm_verify_attn_q8": (_I, [_I, _I, _I, _I, _I, _I, _I64, _I64, _F] + [_P] * 10
+                            + [_SZ, _P, _P]),
+    "pvlm_verify_attn_q8_paged": (_I, [_I, _I, _I, _I, _I, _I, _I, _I, _I64, _I64, _F] + [_P] * 11
+                                  + [_SZ, _P, _P]),
+    "pvlm_gather_kv_q8": (_I, [_I, _I, _I, _I, _I, _I64, _P, _P, _P, _P, _P, _P, _I, _P, _P, _I64, _I]
+                          + [_P] * 6),
+    "pvlm_gather_kv_q8_paged": (_I, [_I, _I, _I, _I, _I, _I, _I, _I64, _P, _P, _P, _P, _P, _P, _P,
+                                     _I, _P, _P, _I64, _I] + [_P] * 6),
     "pvlm_pd_create": (_I, [_I, _D, _I, _c.POINTER(_P)]),
     "pvlm_pd_destroy": (None, [_P]),
     "pvlm_pd_start": (_I, [_P, _P]),
@@ -705,9 +721,12 @@ __all__ = [
     "release_workspaces", "set_stream_cu_budget", "stream_cu_budget",
     "verify_attn", "verify_attn_paged", "verify_attn_noalloc",
     "gather_kv_paged", "rope_append", "rope_append_paged",
+    "rope_append_q8", "rope_append_q8_paged", "quantize_kv", "quantize_kv_paged",
+    "verify_attn_q8", "verify_attn_q8_paged", "verify_attn_q8_workspace_size",
+    "gather_kv_q8", "gather_kv_q8_paged",
     "verify_attn_workspace_size", "uvprune_score_mass", "uvprune_score_cossim",
     "uvprune_criterion_cossim", "prefill_epilogue_cossim", "topk_select", "uvprune_topk_mass", "gather_kv", "spec_accept",
-    "PVLM_F32", "PVLM_BF16", "PVLM_CRIT_MASS", "PVLM_CRIT_COSSIM", "PVLM_DEV_RANGE",
+    "PVLM_F32", "PVLM_BF16", "PVLM_E4M3", "PVLM_CRIT_MASS", "PVLM_CRIT_COSSIM", "PVLM_DEV_RANGE",
     "PVLM_DEV_TIMEOUT", "PVLM_DEV_PLACEMENT",
 ]
 
@@ -869,3 +888,264 @@ def rope_append_paged(q, k_new, v_new, pos, ctx_len, k_pool, v_pool, page_table,
                                       _stream())
     _check(st, "pvlm_rope_append_paged")
     return q_out
+
+
+# ------------------------------------------------------------ 8-bit caches --
+# Codes are torch.float8_e4m3fn (or the same bytes as torch.uint8), exponents
+# torch.uint8: a row stands for code * 2^(exponent - 127).
+def _need_q8(k_codes, k_exps, v_codes, v_exps, dev, paged, stacked=None):
+    """Check a cache's four tensors; returns the codes' shape.  ``dev`` has to be
+    the current device (its stream is the one that a call is enqueued on)."""
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {dev}, but the current device is cuda:{torch.cuda.current_device()}")
+    for t, name in ((k_codes, "k_codes"), (v_codes, "v_codes")):
+        _need(t, name, None, dev)
+        if t.dtype is not torch.float8_e4m3fn and t.dtype is not torch.uint8:
+            raise ValueError(f"{name} must be torch.float8_e4m3fn or torch.uint8, got {t.dtype}")
+    _need(k_exps, "k_exps", torch.uint8, dev)
+    _need(v_exps, "v_exps", torch.uint8, dev)
+    shape = k_codes.shape
+    if len(shape) != 4 and not (stacked and len(shape) == 5):
+        layout = "[n_pages][Hkv][page][D]" if paged else "[B][Hkv][n_cap][D]"
+        raise ValueError(f"codes must be {layout}" + (f" or [L]{layout}" if stacked else ""))
+    if v_codes.shape != shape or k_exps.shape != shape[:-1] or v_exps.shape != shape[:-1]:
+        raise ValueError("k_codes and v_codes must have one shape, k_exps and v_exps that shape without D")
+    return shape
+
+
+def _need_table(page_table, dev, B):
+    _need(page_table, "page_table", torch.int32, dev)
+    if page_table.dim() != 2 or page_table.shape[0] != B:
+        raise ValueError("page_table must be [B][max_pages]")
+    return page_table.shape[1]
+
+
+def _append_q8(q, k_new, v_new, pos, ctx_len, cache, page_table, base, sections, q_out, status):
+    _need(q, "q", torch.bfloat16)
+    dev = q.device
+    _need(k_new, "k_new", torch.bfloat16, dev)
+    _need(v_new, "v_new", torch.bfloat16, dev)
+    n0, Hkv, rows, Dc = _need_q8(*cache, dev, page_table is not None)
+    _need(pos, "pos", torch.int32, dev)
+    _need(ctx_len, "ctx_len", torch.int32, dev)
+    if q.dim() != 4:
+        raise ValueError("q must be [B][T][Hq][D]")
+    B, T, Hq, D = q.shape
+    if k_new.shape != (B, T, Hkv, D) or v_new.shape != k_new.shape or Dc != D:
+        raise ValueError("k_new and v_new must be [B][T][Hkv][D] matching the cache")
+    if ctx_len.shape != (B,):
+        raise ValueError("ctx_len must be [B]")
+    want = (B, T) if sections is None else (3, B, T)
+    if pos.shape != want:
+        raise ValueError(f"pos must be {list(want)}")
+    if page_table is None and n0 != B:
+        raise ValueError("the cache must be [B][Hkv][n_cap][D]")
+    geom = (rows,) if page_table is None else (rows, _need_table(page_table, dev, B), n0)
+    if q_out is None:
+        q_out = torch.empty_like(q)
+    else:
+        _need(q_out, "q_out", torch.bfloat16, dev)
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must have q's shape")
+    sec = None if sections is None else (_c.c_int32 * 3)(*[int(x) for x in sections])
+    name = "pvlm_rope_append_q8" if page_table is None else "pvlm_rope_append_q8_paged"
+    rows_in = (q.data_ptr(), k_new.data_ptr(), v_new.data_ptr())
+    table = () if page_table is None else (page_table.data_ptr(),)
+    st = getattr(lib(), name)(PVLM_BF16, B, T, Hq, Hkv, D, *geom, float(base), sec, pos.data_ptr(), *rows_in,
+                              *table, ctx_len.data_ptr(), q_out.data_ptr(), *[t.data_ptr() for t in cache],
+                              _ptr(_status(status)), _stream())
+    _check(st, name)
+    return q_out
+
+
+def rope_append_q8(q, k_new, v_new, pos, ctx_len, k_codes, k_exps, v_codes, v_exps, *, base: float,
+                   sections=None, q_out=None, status=None):
+    """pvlm_rope_append_q8: as ``rope_append`` (bf16), writing the new rows in 8
+    bits: codes [B][Hkv][n_cap][D] and exponents [B][Hkv][n_cap], n_cap a
+    multiple of 32.  Returns q_out."""
+    return _append_q8(q, k_new, v_new, pos, ctx_len, (k_codes, k_exps, v_codes, v_exps), None, base,
+                      sections, q_out, status)
+
+
+def rope_append_q8_paged(q, k_new, v_new, pos, ctx_len, k_codes, k_exps, v_codes, v_exps, page_table, *,
+                         base: float, sections=None, q_out=None, status=None):
+    """pvlm_rope_append_q8_paged: the same into pools [n_pages][Hkv][page][D]
+    with exponents [n_pages][Hkv][page], through page_table [B][max_pages]."""
+    if page_table is None:
+        raise TypeError("page_table must be a torch.Tensor")
+    return _append_q8(q, k_new, v_new, pos, ctx_len, (k_codes, k_exps, v_codes, v_exps), page_table, base,
+                      sections, q_out, status)
+
+
+def _quantize(k, v, length, cache, page_table, status):
+    _need(k, "k")
+    dev = k.device
+    _need(v, "v", k.dtype, dev)
+    _need(length, "length", torch.int32, dev)
+    shape = _need_q8(*cache, dev, page_table is not None, stacked=True)
+    if k.dim() != len(shape) or v.shape != k.shape:
+        raise ValueError("k and v must be [B][Hkv][src_cap][D], or [L][...] with a stacked cache")
+    L = 1 if k.dim() == 4 else k.shape[0]
+    B, Hkv, src_cap, D = k.shape[-4:]
+    n0, H, rows, Dc = shape[-4:]
+    if (H, Dc) != (Hkv, D) or (len(shape) == 5 and shape[0] != L) or (page_table is None and n0 != B):
+        raise ValueError("the 8-bit cache does not match k and v")
+    if length.shape != (B,):
+        raise ValueError("length must be [B]")
+    codes = [t.data_ptr() for t in cache]
+    if page_table is None:
+        st = lib().pvlm_quantize_kv(_dt(k), L, B, Hkv, D, src_cap, k.data_ptr(), v.data_ptr(),
+                                    length.data_ptr(), rows, *codes, _ptr(_status(status)), _stream())
+        _check(st, "pvlm_quantize_kv")
+    else:
+        st = lib().pvlm_quantize_kv_paged(_dt(k), L, B, Hkv, D, rows, _need_table(page_table, dev, B), n0,
+                                          src_cap, k.data_ptr(), v.data_ptr(), length.data_ptr(),
+                                          page_table.data_ptr(), *codes, _ptr(_status(status)), _stream())
+        _check(st, "pvlm_quantize_kv_paged")
+
+
+def quantize_kv(k, v, length, k_codes, k_exps, v_codes, v_exps, *, status=None):
+    """pvlm_quantize_kv: rows 0 .. length[b] - 1 of a bf16 or fp32 cache
+    [B][Hkv][src_cap][D] (or [L][...]: every layer in one launch) into an 8-bit
+    one [B][Hkv][n_cap][D] (or [L][...]); its other rows stay as they are."""
+    _quantize(k, v, length, (k_codes, k_exps, v_codes, v_exps), None, status)
+
+
+def quantize_kv_paged(k, v, length, k_codes, k_exps, v_codes, v_exps, page_table, *, status=None):
+    """pvlm_quantize_kv_paged: the same into pools [n_pages][Hkv][page][D] (or
+    [L][...]; one page_table [B][max_pages] serves every layer)."""
+    if page_table is None:
+        raise TypeError("page_table must be a torch.Tensor")
+    _quantize(k, v, length, (k_codes, k_exps, v_codes, v_exps), page_table, status)
+
+
+def verify_attn_q8_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx) -> int:
+    return int(lib().pvlm_verify_attn_q8_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx))
+
+
+def _verify_q8(q, cache, page_table, ctx_len, scale, max_ctx, out, mass, lse, want_mass, want_lse, ws, status):
+    _need(q, "q", torch.bfloat16)
+    dev = q.device
+    n0, Hkv, rows, Dc = _need_q8(*cache, dev, page_table is not None)
+    _need(ctx_len, "ctx_len", torch.int32, dev)
+    if q.dim() != 4:
+        raise ValueError("q must be [B][T][Hq][D]")
+    B, T, Hq, D = q.shape
+    if Dc != D or ctx_len.shape != (B,) or (page_table is None and n0 != B):
+        raise ValueError("inconsistent verify_attn_q8 shapes")
+    if page_table is None:
+        n_cap, geom, table = rows, (rows,), ()
+    else:
+        max_pages = _need_table(page_table, dev, B)
+        n_cap, geom, table = max_pages * rows, (rows, max_pages, n0), (page_table.data_ptr(),)
+    if max_ctx is None:
+        max_ctx = n_cap - T
+    if out is None:
+        out = torch.empty_like(q)
+    elif _need(out, "out", torch.bfloat16, dev).shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if mass is None:
+        mass = torch.empty((B, n_cap), dtype=torch.float32, device=dev) if want_mass else None
+    elif _need(mass, "mass", torch.float32, dev).shape != (B, n_cap):
+        raise ValueError("mass must be [B][n_cap]")
+    if lse is None:
+        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=dev) if want_lse else None
+    elif _need(lse, "lse", torch.float32, dev).shape != (B, Hq, T):
+        raise ValueError("lse must be [B][Hq][T]")
+    L = lib()
+    wsb = (ws or _default_ws("verify_q8")).get(
+        L.pvlm_verify_attn_q8_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx))
+    name = "pvlm_verify_attn_q8" if page_table is None else "pvlm_verify_attn_q8_paged"
+    st = getattr(L, name)(PVLM_BF16, B, T, Hq, Hkv, D, *geom, max_ctx,
+                          float(D ** -0.5 if scale is None else scale), q.data_ptr(),
+                          *[t.data_ptr() for t in cache], *table, ctx_len.data_ptr(), out.data_ptr(), _ptr(mass),
+                          _ptr(lse), wsb.data_ptr(), wsb.numel(), _ptr(_status(status)), _stream())
+    _check(st, name)
+    return out, mass, lse
+
+
+def verify_attn_q8(q, k_codes, k_exps, v_codes, v_exps, ctx_len, *, scale: Optional[float] = None,
+                   max_ctx: Optional[int] = None, out=None, mass=None, lse=None, want_mass: bool = True,
+                   want_lse: bool = True, ws: Optional[Workspace] = None, status=None):
+    """pvlm_verify_attn_q8: ``verify_attn`` of bf16 queries [B][T][Hq][D] over an
+    8-bit cache [B][Hkv][n_cap][D]; T = 1 and want_mass=False for a decode step.
+    Returns (out, mass or None, lse or None)."""
+    return _verify_q8(q, (k_codes, k_exps, v_codes, v_exps), None, ctx_len, scale, max_ctx, out, mass, lse,
+                      want_mass, want_lse, ws, status)
+
+
+def verify_attn_q8_paged(q, k_codes, k_exps, v_codes, v_exps, page_table, ctx_len, *,
+                         scale: Optional[float] = None, max_ctx: Optional[int] = None, out=None, mass=None,
+                         lse=None, want_mass: bool = True, want_lse: bool = True,
+                         ws: Optional[Workspace] = None, status=None):
+    """pvlm_verify_attn_q8_paged: the same over pools [n_pages][Hkv][page][D]
+    through page_table [B][max_pages]; mass is [B][max_pages * page]."""
+    if page_table is None:
+        raise TypeError("page_table must be a torch.Tensor")
+    return _verify_q8(q, (k_codes, k_exps, v_codes, v_exps), page_table, ctx_len, scale, max_ctx, out, mass,
+                      lse, want_mass, want_lse, ws, status)
+
+
+def _gather_q8(cache, page_table, idx, k, tail_begin, tail_len, dst_cap, dtype, dst, status):
+    _need(cache[0], "k_codes")
+    dev = cache[0].device
+    shape = _need_q8(*cache, dev, page_table is not None, stacked=True)
+    for name, t in (("idx", idx), ("k", k), ("tail_begin", tail_begin), ("tail_len", tail_len)):
+        _need(t, name, torch.int32, dev)
+    L = 1 if len(shape) == 4 else shape[0]
+    n0, Hkv, rows, D = shape[-4:]
+    if idx.dim() != 2:
+        raise ValueError("idx must be [B][k_cap]")
+    B = idx.shape[0]
+    if page_table is None and n0 != B:
+        raise ValueError("idx must be [B][k_cap]")
+    if any(t.shape != (B,) for t in (k, tail_begin, tail_len)):
+        raise ValueError("k, tail_begin and tail_len must be [B]")
+    if dtype not in (torch.float8_e4m3fn, torch.bfloat16, torch.float32):
+        raise ValueError(f"unsupported dtype {dtype}")
+    q8 = dtype is torch.float8_e4m3fn
+    dst_cap = int(dst_cap)
+    want = tuple(shape[:-4]) + (B, Hkv, dst_cap, D)
+    fill = dst is None   # the call zeroes what it does not copy of a new destination
+    if fill and q8:
+        dst = [torch.empty(want[:n], dtype=dtype if n is None else torch.uint8, device=dev) for n in (None, -1) * 2]
+    elif fill:
+        dst = [torch.empty(want, dtype=dtype, device=dev) for _ in range(2)]
+    elif q8:
+        if len(dst) != 4 or _need_q8(*dst, dev, False, stacked=True) != want:
+            raise ValueError("destination shape mismatch")
+    elif len(dst) != 2 or any(_need(t, "dst", dtype, dev).shape != want for t in dst):
+        raise ValueError("destination shape mismatch")
+    kd, kde, vd, vde = [t.data_ptr() for t in dst] if q8 else (dst[0].data_ptr(), None, dst[1].data_ptr(), None)
+    to = PVLM_E4M3 if q8 else PVLM_BF16 if dtype is torch.bfloat16 else PVLM_F32
+    if page_table is None:
+        name, geom, table = "pvlm_gather_kv_q8", (rows,), ()
+    else:
+        name = "pvlm_gather_kv_q8_paged"
+        geom, table = (rows, _need_table(page_table, dev, B), n0), (page_table.data_ptr(),)
+    st = getattr(lib(), name)(to, L, B, Hkv, D, *geom, *[t.data_ptr() for t in cache], *table, idx.data_ptr(),
+                              k.data_ptr(), idx.shape[1], tail_begin.data_ptr(), tail_len.data_ptr(), dst_cap,
+                              int(fill), kd, kde, vd, vde, _ptr(_status(status)), _stream())
+    _check(st, name)
+    return tuple(dst)
+
+
+def gather_kv_q8(k_codes, k_exps, v_codes, v_exps, idx, k, tail_begin, tail_len, dst_cap: int, *,
+                 dtype=torch.float8_e4m3fn, dst=None, status=None):
+    """pvlm_gather_kv_q8: the draft's compact cache (``gather_kv``) from an 8-bit
+    cache [B][Hkv][n_cap][D] or [L][...].  dtype torch.float8_e4m3fn returns
+    (k_codes, k_exps, v_codes, v_exps) with dst_cap rows (a multiple of 32);
+    torch.bfloat16 or torch.float32 returns (k, v), the values that the rows
+    stand for.  ``dst``: those tensors, to be written in place."""
+    return _gather_q8((k_codes, k_exps, v_codes, v_exps), None, idx, k, tail_begin, tail_len, dst_cap, dtype,
+                      dst, status)
+
+
+def gather_kv_q8_paged(k_codes, k_exps, v_codes, v_exps, page_table, idx, k, tail_begin, tail_len,
+                       dst_cap: int, *, dtype=torch.float8_e4m3fn, dst=None, status=None):
+    """pvlm_gather_kv_q8_paged: the same from pools [n_pages][Hkv][page][D] or
+    [L][...]; one page_table [B][max_pages] serves every layer."""
+    if page_table is None:
+        raise TypeError("page_table must be a torch.Tensor")
+    return _gather_q8((k_codes, k_exps, v_codes, v_exps), page_table, idx, k, tail_begin, tail_len, dst_cap,
+                      dtype, dst, status)

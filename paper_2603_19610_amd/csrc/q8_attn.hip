@@ -25,8 +25,7 @@ namespace {
 typedef int intx2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kPageSlots = 512;  // page-table entries a workgroup stages in LDS
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLog2e = 1.4426950408889634;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNegInf = -__builtin_huge_valf();
 // A wave's running reference may trail its row maximum by this much (log2
@@ -34,19 +33,24 @@ constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kRefSlack = 8.f;
 constexpr int kFinWaves = kFinThreads / 64;
 
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
 struct QArgs {
   const uint16_t* q;
   Q8Cache c;
   const int32_t* ctx_len;
   int B, T, Hq, Hkv, G, R;
   unsigned g_magic;  // row / G == row * g_magic >> 20 for row < 640 (2^20 / G + 1; G <= 640)
-  int RTT, RG;
-  int max_ctx;
-  int splits, chunk, units;
+  int RTT, RG, HR;   // HR = Hkv * RG, the groups of a sequence
+  int max_ctx, wgs;
   float sl2;         // scale * log2(e)
-  float* mpart;      // [B][Hkv * RG][n_cap] mass of one workgroup's rows
-  float2* stats;     // [B * Hkv * RTT][splits][16] (log2-domain maximum, sum) of a chunk's rows
-  float* opart;      // [B * Hkv * RTT][splits][16][D] chunk sums relative to that maximum
+  float* mpart;      // [B][HR][waves][n_cap] mass of one wave's rows
+  float2* stats;     // [record][tile][token wave][16] (log2-domain maximum, sum) of rows
+  float* zt;         // the same sums of the probabilities as P . V takes them, rounded to bf16
+  float* opart;      // [record][tile][token wave][16][D] sums of P . V relative to that maximum
   uint16_t* out;
   float* lse;
   float* mass;
@@ -54,99 +58,126 @@ struct QArgs {
   int mass_wgs, mass_per, mass_rows;  // finish kernel: workgroups that sum the mass, of a sequence, rows of one
 };
 
-struct Unit {
-  int split, bg, b, g, rg, ctx, N, c0, c1;
-};
+typedef const __attribute__((address_space(4))) int32_t* ConstInts;  // (uniform loads go through the scalar cache)
+__device__ __forceinline__ int uniform_load(const int32_t* p, int64_t i) { return ((ConstInts)(uintptr_t)p)[i]; }
 
-__device__ __forceinline__ int seq_ctx(const QArgs& a, int b, bool flag) {
-  const int ctx = a.ctx_len[b];
-  if (ctx >= 0 && ctx <= a.max_ctx) return ctx;
-  if (flag) dev_flag(a.status, PVLM_DEV_RANGE);
-  return ctx < 0 ? 0 : a.max_ctx;
+__device__ __forceinline__ int clamp_ctx(const QArgs& a, int ctx) { return ctx < 0 ? 0 : min(ctx, a.max_ctx); }
+__device__ __forceinline__ int units_of(const QArgs& a, int ctx) { return (ctx + a.T + kQUnit - 1) / kQUnit; }
+
+// Where the groups lie in the row of units.  Every wave finds its place from
+// the lengths: sequence b's first group begins at HR * before.
+struct Shares {
+  int per;     // units of a workgroup
+  int before;  // units (of one group each) of the sequences ahead of b
+  int b, ctx;
+};
+// The sequence that holds unit `at` of share wg (b = B: none), or sequence `seq`.
+template <bool FIND_UNIT>
+__device__ __forceinline__ Shares find(const QArgs& a, int wg, int seq) {
+  const int lane = threadIdx.x & 63;
+  int total = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    int u = b0 + lane < a.B ? units_of(a, clamp_ctx(a, a.ctx_len[b0 + lane])) : 0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) u += __shfl_xor(u, o, 64);
+    total += u;
+  }
+  Shares s;
+  s.per = (total * a.HR + a.wgs - 1) / a.wgs;
+  if (s.per < kQMinUnits) s.per = kQMinUnits;
+  s.before = 0;
+  s.b = a.B;
+  s.ctx = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const int ctx = b0 + lane < a.B ? clamp_ctx(a, a.ctx_len[b0 + lane]) : 0;
+    const int u = b0 + lane < a.B ? units_of(a, ctx) : 0;
+    int upto = u;  // inclusive
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += v;
+    }
+    int hit;
+    if constexpr (FIND_UNIT) {
+      // (wg * per stays within 32 bits: per exceeds total / wgs by less than one, or is the least share of few units)
+      const uint64_t m = __ballot(b0 + lane < a.B && (s.before + upto) * a.HR > wg * s.per);
+      hit = m ? __builtin_ctzll(m) : -1;
+    } else {
+      hit = seq >= b0 && seq < b0 + 64 ? seq - b0 : -1;
+    }
+    if (hit >= 0) {
+      s.before += __shfl(upto - u, hit, 64);
+      s.b = b0 + hit;
+      s.ctx = __shfl(ctx, hit, 64);
+      break;
+    }
+    s.before += __shfl(upto, 63, 64);
+  }
+  s.per = __builtin_amdgcn_readfirstlane(s.per);
+  s.before = __builtin_amdgcn_readfirstlane(s.before);
+  s.b = __builtin_amdgcn_readfirstlane(s.b);
+  s.ctx = __builtin_amdgcn_readfirstlane(s.ctx);
+  return s;
 }
 
-// Workgroup i runs on XCD i % 8; consecutive units, whose row groups read the
-// same cache rows, go to one XCD and share its L2 (a matter of speed only).
-__device__ __forceinline__ bool decode_unit(const QArgs& a, Unit& u) {
-  const int per = gridDim.x / 8;
-  const int lg = ((int)blockIdx.x % 8) * per + (int)blockIdx.x / 8;
-  if (lg >= a.units) return false;
-  u.rg = lg % a.RG;
-  const int cs = lg / a.RG;
-  u.split = cs % a.splits;
-  u.bg = cs / a.splits;
-  u.g = u.bg % a.Hkv;
-  u.b = u.bg / a.Hkv;
-  u.ctx = seq_ctx(a, u.b, u.split == 0 && threadIdx.x == 0);
-  u.N = u.ctx + a.T;
-  u.c0 = u.split * a.chunk;
-  u.c1 = min(u.c0 + a.chunk, u.N);
-  return u.c0 < u.N;
+// A workgroup's share as pieces of groups, one after the other.
+struct Piece {
+  int b, g, rg, ctx;     // group: sequence, KV head, share of its row tiles
+  int c0, c1;            // its tokens (c0 opens a unit)
+  int left;              // units of the share from c0 on
+  int before, per;       // units of the sequences ahead of b; of a share
+  __device__ __forceinline__ void set(const QArgs& a) {
+    const int N = ctx + a.T, u = c0 / kQUnit + left;
+    c1 = u > N / kQUnit ? N : u * kQUnit;
+  }
+  // false where the share is empty
+  __device__ __forceinline__ bool first(const QArgs& a) {
+    const Shares s = find<true>(a, blockIdx.x, 0);
+    if (s.b >= a.B) return false;
+    b = s.b;
+    ctx = s.ctx;
+    before = s.before;
+    per = left = s.per;
+    const int u = units_of(a, ctx), off = (int)blockIdx.x * per - before * a.HR;
+    const int hr = __builtin_amdgcn_readfirstlane(off / u);
+    g = __builtin_amdgcn_readfirstlane(hr / a.RG);
+    rg = hr - g * a.RG;
+    c0 = (off - hr * u) * kQUnit;
+    set(a);
+    return true;
+  }
+  // false where the share ends
+  __device__ __forceinline__ bool next(const QArgs& a) {
+    left -= (c1 - c0 + kQUnit - 1) / kQUnit;
+    if (left <= 0) return false;
+    if (++rg == a.RG) {
+      rg = 0;
+      if (++g == a.Hkv) {
+        g = 0;
+        before += units_of(a, ctx);
+        if (++b == a.B) return false;
+        ctx = clamp_ctx(a, uniform_load(a.ctx_len, b));
+      }
+    }
+    c0 = 0;
+    set(a);
+    return true;
+  }
+  __device__ __forceinline__ int group(const QArgs& a) const { return (b * a.Hkv + g) * a.RG + rg; }
+};
+
+// The workgroups that hold pieces of a group (hr = g * RG + rg), and its first record.
+struct Holders {
+  int rec, count;
+};
+__device__ __forceinline__ Holders holders(const QArgs& a, int per, int before, int b, int hr, int ctx) {
+  const int u = units_of(a, ctx), start = before * a.HR + hr * u;
+  const int w0 = start / per, w1 = (start + u - 1) / per;
+  return {b * a.HR + hr + w0, w1 - w0 + 1};
 }
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ int row_t(const QArgs& a, int row) { return (int)((unsigned)row * a.g_magic >> 20); }
-
-// ------------------------------------------------------------ cache rows --
-// Rows of (b, g): row r of the chunk lies at index base + r (padded), or in
-// page `pages[...]` of the pool.  Entries are checked once, when they are
-// staged (every thread takes part); one outside the pool is flagged and
-// clamped into it.
-struct Rows {
-  int64_t base;            // padded: row index of logical row 0; paged: of the head's row 0 in pool page 0
-  int64_t page_rows;       // rows between pages, all heads
-  const int32_t* table;
-  const int32_t* staged;   // LDS copy from logical page page0, where the chunk's entries fit
-  int64_t n_pages;
-  int shift, page0;
-  bool paged, in_lds;
-};
-
-__device__ __forceinline__ Rows rows_setup(const QArgs& a, const Unit& u, int32_t* s_pages) {
-  Rows v;
-  v.paged = a.c.table != nullptr;
-  if (!v.paged) {
-    v.base = ((int64_t)u.b * a.Hkv + u.g) * a.c.n_cap;
-    v.page_rows = 0;
-    v.table = nullptr;
-    v.staged = nullptr;
-    v.n_pages = 0;
-    v.shift = v.page0 = 0;
-    v.in_lds = false;
-    return v;
-  }
-  v.shift = a.c.shift;
-  v.base = (int64_t)u.g << v.shift;
-  v.page_rows = (int64_t)a.Hkv << v.shift;
-  v.table = a.c.table + (int64_t)u.b * a.c.max_pages;
-  v.staged = s_pages;
-  v.n_pages = a.c.n_pages;
-  v.page0 = u.c0 >> v.shift;
-  const int p1 = (u.c1 - 1) >> v.shift;
-  v.in_lds = p1 - v.page0 < kPageSlots;
-  for (int pg = v.page0 + threadIdx.x; pg <= p1; pg += (int)blockDim.x) {
-    int e = v.table[pg];
-    if (e < 0 || e >= v.n_pages) {
-      dev_flag(a.status, PVLM_DEV_RANGE);
-      e = e < 0 ? 0 : (int)(v.n_pages - 1);
-    }
-    if (v.in_lds) s_pages[pg - v.page0] = e;
-  }
-  __syncthreads();
-  return v;
-}
-
-__device__ __forceinline__ int64_t row_index(const Rows& v, int r) {
-  if (!v.paged) return v.base + r;
-  int pg;
-  if (v.in_lds) {
-    pg = v.staged[(r >> v.shift) - v.page0];
-  } else {
-    pg = v.table[r >> v.shift];
-    pg = pg < 0 ? 0 : pg >= v.n_pages ? (int)(v.n_pages - 1) : pg;
-  }
-  return v.base + pg * v.page_rows + (r & ((1 << v.shift) - 1));
-}
 
 // --------------------------------------------------------------- layouts --
 // Tokens are the M side of the score tiles and query rows the N side.  A block
@@ -163,7 +194,7 @@ __device__ __forceinline__ int64_t row_index(const Rows& v, int r) {
 // of a transposed read over the positions.
 template <int D>
 struct Lay {
-  static constexpr int CH = D / 16, LR = 256 / D, ST = kQStageBytes / D, DPL = D / 16;
+  static constexpr int CH = D / 16, LR = 256 / D;
   static __device__ __forceinline__ int kkey(int line) { return (line * LR >> 2) & 15; }
   static __device__ __forceinline__ int vkey(int line) {
     if constexpr (D == 128) return (line & 3) | ((line >> 1) & 4);
@@ -173,15 +204,6 @@ struct Lay {
     return (r / LR) * 256 + ((((r % LR) * CH + c) ^ key) << 4);
   }
 };
-
-// One 16-byte piece of a stage: piece i of the LDS image, as (row, chunk).
-template <int D, bool IS_K>
-__device__ __forceinline__ void piece(int i, int& row, int& chunk) {
-  typedef Lay<D> L;
-  const int line = i >> 4, p = (i & 15) ^ (IS_K ? L::kkey(line) : L::vkey(line));
-  row = line * L::LR + p / L::CH;
-  chunk = p % L::CH;
-}
 
 // ---------------------------------------------------------------- operands --
 // A lane's d range of a row: 32 values at D = 128, 16 at 64, of which k-step s
@@ -208,10 +230,11 @@ __device__ __forceinline__ bf16x8 to_bf16(uint32_t lo, uint32_t hi, float unit) 
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// Scores of one block against a row tile: S[tt][i] is token 16 gq + 4 i + tt.
-template <int D>
-__device__ __forceinline__ void scores(const char* kb, uint32_t exps, int r0, int n, int gq, const Query<D>& q,
-                                       floatx4 (&S)[4]) {
+// Scores of one block against a wave's row tiles: S[x][tt][i] is token
+// 16 gq + 4 i + tt.  The keys are converted once for all tiles.
+template <int D, int TPW>
+__device__ __forceinline__ void scores(const char* kb, uint32_t exps, int r0, int n, int gq, const Query<D> (&q)[TPW],
+                                       floatx4 (&S)[TPW][4]) {
   typedef Lay<D> L;
   constexpr int NC = D / 64;  // 16-byte chunks of a lane's range
   uint4 k[4][NC];
@@ -222,14 +245,20 @@ __device__ __forceinline__ void scores(const char* kb, uint32_t exps, int r0, in
     for (int c = 0; c < NC; ++c) k[tt][c] = *reinterpret_cast<const uint4*>(kb + L::at(r, NC * gq + c, key));
   }
 #pragma unroll
-  for (int tt = 0; tt < 4; ++tt) S[tt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int x = 0; x < TPW; ++x)
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt) S[x][tt] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) {
       const float unit = q8_unit((exps >> (8 * tt)) & 0xffu);
-      S[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(to_bf16(k[tt][c].x, k[tt][c].y, unit), q.s[2 * c], S[tt], 0, 0, 0);
-      S[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(to_bf16(k[tt][c].z, k[tt][c].w, unit), q.s[2 * c + 1], S[tt], 0, 0, 0);
+      const bf16x8 k0 = to_bf16(k[tt][c].x, k[tt][c].y, unit), k1 = to_bf16(k[tt][c].z, k[tt][c].w, unit);
+#pragma unroll
+      for (int x = 0; x < TPW; ++x) {
+        S[x][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[x].s[2 * c], S[x][tt], 0, 0, 0);
+        S[x][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[x].s[2 * c + 1], S[x][tt], 0, 0, 0);
+      }
     }
 }
 
@@ -242,80 +271,134 @@ __device__ __forceinline__ intx2 read_v(const char* vb, int r, int jd, int n) {
   const uint32_t at = lds_addr(vb) + L::at(row, jd, L::vkey(row / L::LR)) + 8 * (n & 1);
   return __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2)at);
 }
-// O += P' . V over one block.  P'[j] is token 16 gq + j.
+// Two columns' operands of a block, as codes.
+struct VPair {
+  intx2 v[4];
+};
 template <int D>
-__device__ __forceinline__ void weigh(const char* vb, int r0, int n, int gq, const float (&P)[16],
-                                      floatx4 (&O)[D / 16]) {
+__device__ __forceinline__ VPair read_pair(const char* vb, int r0, int n, int gq, int pair) {
+  VPair p;
 #pragma unroll
-  for (int ks = 0; ks < 2; ++ks) {
-    bf16x8 pa;
+  for (int i = 0; i < 4; ++i) p.v[i] = read_v<D>(vb, r0 + 16 * gq + 8 * (i & 1), 2 * pair + i / 2, n);
+  return p;
+}
+
+// O += P' . V over one block; P'[x][ks] holds tokens 16 gq + 8 ks + j.  The next
+// two columns are read while two are multiplied; the barriers keep the compiler
+// from reading all of them at once, for which there are no registers.
+template <int D, int TPW>
+__device__ __forceinline__ void weigh(const char* vb, int r0, int n, int gq, const bf16x8 (&P)[TPW][2], VPair cur,
+                                      floatx4 (&O)[TPW][D / 16]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) pa[j] = static_cast<__bf16>(P[8 * ks + j]);
+  for (int pair = 0; pair < D / 32; ++pair) {
+    VPair next;
+    if (pair + 1 < D / 32) next = read_pair<D>(vb, r0, n, gq, pair + 1);
 #pragma unroll
-    for (int jd = 0; jd < D / 16; ++jd) {
-      const intx2 v = read_v<D>(vb, r0 + 16 * gq + 8 * ks, jd, n);
-      O[jd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, to_bf16(v[0], v[1], 1.f), O[jd], 0, 0, 0);
+    for (int i = 0; i < 4; ++i) {
+      const bf16x8 b = to_bf16(cur.v[i][0], cur.v[i][1], 1.f);
+      const int jd = 2 * pair + i / 2;
+#pragma unroll
+      for (int x = 0; x < TPW; ++x)
+        O[x][jd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][i & 1], b, O[x][jd], 0, 0, 0);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    cur = next;
   }
 }
 // The same for a block in which some rows see less than others: a NaN value
 // (0 times it is NaN) must not reach the rows that do not see it.  NaN codes
 // count as 0 in the product, and a second one, of the rows' visibility with
-// the NaN positions, says which results they belong to.  `seen` has bit j for
-// token 16 gq + j.
-template <int D>
-__device__ __forceinline__ void weigh_masked(const char* vb, int r0, int n, int gq, const float (&P)[16],
-                                             uint32_t seen, floatx4 (&O)[D / 16]) {
-  bf16x8 pa[2], va[2];
-#pragma unroll
-  for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      pa[ks][j] = static_cast<__bf16>(P[8 * ks + j]);
-      va[ks][j] = static_cast<__bf16>((seen >> (8 * ks + j)) & 1 ? 1.f : 0.f);
-    }
+// the NaN positions, says which results they belong to.  Bit j of seen[x] is
+// the visibility of token 16 gq + j.
+template <int D, int TPW>
+__device__ __forceinline__ void weigh_masked(const char* vb, int r0, int n, int gq, const bf16x8 (&P)[TPW][2],
+                                             const uint32_t (&seen)[TPW], floatx4 (&O)[TPW][D / 16]) {
 #pragma unroll
   for (int jd = 0; jd < D / 16; ++jd) {
-    floatx4 hit = {0.f, 0.f, 0.f, 0.f};
+    intx2 one[2];
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       const intx2 v = read_v<D>(vb, r0 + 16 * gq + 8 * ks, jd, n);
       const uint32_t b0 = nan_codes(v[0]), b1 = nan_codes(v[1]);
-      // a NaN byte's mask, and 0x38 (1.0) in its place
-      const intx2 clean = {(int)(v[0] & ~(b0 | (b0 - (b0 >> 7)))), (int)(v[1] & ~(b1 | (b1 - (b1 >> 7))))};
-      const intx2 one = {(int)((b0 >> 7) * 0x38u), (int)((b1 >> 7) * 0x38u)};
-      O[jd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa[ks], to_bf16(clean[0], clean[1], 1.f), O[jd], 0, 0, 0);
-      hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[ks], to_bf16(one[0], one[1], 1.f), hit, 0, 0, 0);
-    }
+      // without the NaN bytes, and 0x38 (1.0) in their places
+      const bf16x8 b = to_bf16(v[0] & ~(b0 | (b0 - (b0 >> 7))), v[1] & ~(b1 | (b1 - (b1 >> 7))), 1.f);
+      one[ks] = intx2{(int)((b0 >> 7) * 0x38u), (int)((b1 >> 7) * 0x38u)};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) O[jd][i] = hit[i] > 0.f ? __uint_as_float(0x7fc00000u) : O[jd][i];
+      for (int x = 0; x < TPW; ++x) O[x][jd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][ks], b, O[x][jd], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (!__any(one[0][0] | one[0][1] | one[1][0] | one[1][1])) continue;
+#pragma unroll
+    for (int x = 0; x < TPW; ++x) {
+      floatx4 hit = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        bf16x8 va;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) va[j] = static_cast<__bf16>((seen[x] >> (8 * ks + j)) & 1 ? 1.f : 0.f);
+        hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, to_bf16(one[ks][0], one[ks][1], 1.f), hit, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) O[x][jd][i] = hit[i] > 0.f ? __uint_as_float(0x7fc00000u) : O[x][jd][i];
+    }
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
-// log2-sum-exp of row n of a row tile over its nsp chunks, the lane groups
-// taking the chunks in turn (+inf for padding rows: their probabilities are 0).
+// (maximum, sum) of two sets of scores.  A sum of 0 belongs to one of which the
+// row sees nothing; NaN passes.
 __device__ __forceinline__ void join(float& m, float& z, float m2, float z2) {
   const float M = fmaxf(m, m2), r = M == kNegInf ? 0.f : M;
-  // (a sum of 0 belongs to a chunk in which the row sees nothing; NaN passes)
   z = (z != 0.f ? z * fast_exp2(m - r) : 0.f) + (z2 != 0.f ? z2 * fast_exp2(m2 - r) : 0.f);
   m = M;
 }
-__device__ __forceinline__ float tile_lse(const QArgs& a, int tile, bool real, int nsp, int n, int gq) {
-  const float2* st = a.stats + (size_t)tile * a.splits * 16 + n;
-  float M = kNegInf, Z = 0.f;
-  for (int s = gq; s < nsp; s += 4) {
-    const float2 v = st[(size_t)s * 16];
-    join(M, Z, v.x, v.y);
+// log2-sum-exp of row n of a wave's tiles over a group's records, the lane
+// groups taking them in turn, with many loads in flight (+inf for padding rows:
+// their probabilities are 0).
+template <int RT, int TPW>
+__device__ __forceinline__ void tile_lse(const QArgs& a, const Holders& h, int tile0, int tiles, const bool (&real)[TPW],
+                                         int n, int gq, float (&lse)[TPW]) {
+  constexpr int kU = TPW == 1 ? 8 : 4;  // records of every tile in flight
+  const int cnt = h.count * kQTokenWaves;
+  const float2* st = a.stats + (size_t)h.rec * RT * kQTokenWaves * 16 + n;
+  float M[TPW], Z[TPW];
+#pragma unroll
+  for (int x = 0; x < TPW; ++x) M[x] = kNegInf, Z[x] = 0.f;
+  for (int s0 = gq; s0 < cnt; s0 += 4 * kU) {
+    float2 v[kU][TPW];
+#pragma unroll
+    for (int j = 0; j < kU; ++j) {
+      const int s = min(s0 + 4 * j, cnt - 1);
+      const float2* r = st + (size_t)(s / kQTokenWaves * RT * kQTokenWaves + s % kQTokenWaves) * 16;
+#pragma unroll
+      for (int x = 0; x < TPW; ++x) v[j][x] = r[min(tile0 + x, tiles - 1) * kQTokenWaves * 16];
+    }
+#pragma unroll
+    for (int x = 0; x < TPW; ++x) {
+      float m = M[x];
+#pragma unroll
+      for (int j = 0; j < kU; ++j) m = fmaxf(m, v[j][x].x);
+      const float r = m == kNegInf ? 0.f : m;
+      float z = Z[x] != 0.f ? Z[x] * fast_exp2(M[x] - r) : 0.f;
+#pragma unroll
+      for (int j = 0; j < kU; ++j)
+        z += v[j][x].y != 0.f && s0 + 4 * j < cnt ? v[j][x].y * fast_exp2(v[j][x].x - r) : 0.f;
+      M[x] = m;
+      Z[x] = z;
+    }
   }
-  join(M, Z, lane_xor16(M), lane_xor16(Z));
-  join(M, Z, lane_xor32(M), lane_xor32(Z));
-  return real ? M + __log2f(Z) : __builtin_huge_valf();
+#pragma unroll
+  for (int x = 0; x < TPW; ++x) {
+    join(M[x], Z[x], lane_xor16(M[x]), lane_xor16(Z[x]));
+    join(M[x], Z[x], lane_xor32(M[x]), lane_xor32(Z[x]));
+    lse[x] = real[x] ? M[x] + __log2f(Z[x]) : __builtin_huge_valf();
+  }
 }
 
-// Sums of a block's probabilities over the 16 rows (lanes n) of a tile, token
-// `lane` of the block into dst[lane]: each step a lane keeps half of its values,
-// chosen by one bit of n, and adds its partner's copy of that half.
-__device__ __forceinline__ void rows_to_lds(const float (&p)[16], float* dst, int lane) {
+// Sum over the 16 rows (lanes n) of a block's values, of token `lane` of the
+// block: each step a lane keeps half of its values, chosen by one bit of n, and
+// adds its partner's copy of that half.
+__device__ __forceinline__ float row_sums(const float (&p)[16], int lane) {
   const bool h8 = lane & 8, h4 = lane & 4, h2 = lane & 2, h1 = lane & 1;
   float a8[8], a4[4], a2[2];
 #pragma unroll
@@ -324,319 +407,540 @@ __device__ __forceinline__ void rows_to_lds(const float (&p)[16], float* dst, in
   for (int k = 0; k < 4; ++k) a4[k] = (h4 ? a8[4 + k] : a8[k]) + lane_mirror8(h4 ? a8[k] : a8[4 + k]);
 #pragma unroll
   for (int k = 0; k < 2; ++k) a2[k] = (h2 ? a4[2 + k] : a4[k]) + lane_xor2(h2 ? a4[k] : a4[2 + k]);
-  dst[lane] = (h1 ? a2[1] : a2[0]) + lane_xor1(h1 ? a2[0] : a2[1]);
+  return (h1 ? a2[1] : a2[0]) + lane_xor1(h1 ? a2[0] : a2[1]);
 }
 
-// -------------------------------------------------------- partial kernel --
-template <int D, int RT>
-struct Shape {
-  static constexpr int TW = RT <= 2 ? 2 : 1;  // waves sharing a row tile's tokens
-  static constexpr int kThreads = RT * TW * 64;
-  static constexpr int ST = kQStageBytes / D, NB = ST / 64 / TW;  // tokens of a stage, blocks of it per wave
-  static constexpr int kStage = 2 * kQStageBytes + 2 * ST;        // K codes, V codes, their exponents
+// ------------------------------------------------------------------ ring --
+// A stage is 128 tokens' codes and exponents.  The loading waves copy stages
+// into an LDS ring by global->LDS loads of 1 KB (16 bytes a lane, in LDS order:
+// the lanes fetch permuted chunks), so loads stay in flight behind the other
+// waves' arithmetic.  One barrier a stage hands a landed slot over and an
+// emptied one back.
+template <int D>
+struct Ring {
+  static constexpr int ST = 128, KB = ST * D;          // tokens of a stage, bytes of its codes (K or V)
+  static constexpr int NI = KB / 1024;                 // load instructions for them
+  static constexpr int kSide = KB + 256;               // ... and exponents (ST bytes; a load writes 256)
+  static constexpr int RPI = 1024 / D, IPU = 32 / RPI; // rows of an instruction, instructions of a unit
 };
 
-// A stage's codes and exponents into LDS.  Rows past the chunk repeat its last
-// one; exponents are read in groups of four rows, which never leave a block of
-// 32 (capacities and pages are whole blocks).
-template <int D, bool WITH_V>
-__device__ __forceinline__ void load_stage(const QArgs& a, const Rows& v, int t0, int c1, char* s) {
-  constexpr int ST = kQStageBytes / D;
-  for (int i = threadIdx.x; i < kQStageBytes / 16; i += (int)blockDim.x) {
-    int row, chunk;
-    piece<D, true>(i, row, chunk);
-    *reinterpret_cast<uint4*>(s + 16 * i) =
-        *reinterpret_cast<const uint4*>(a.c.kc + row_index(v, min(t0 + row, c1 - 1)) * D + 16 * chunk);
-    if constexpr (WITH_V) {
-      piece<D, false>(i, row, chunk);
-      *reinterpret_cast<uint4*>(s + kQStageBytes + 16 * i) =
-          *reinterpret_cast<const uint4*>(a.c.vc + row_index(v, min(t0 + row, c1 - 1)) * D + 16 * chunk);
-    }
-  }
-  for (int i = threadIdx.x; i < ST / 4; i += (int)blockDim.x) {
-    const int64_t at = row_index(v, min(t0 + 4 * i, (c1 - 1) & ~3));
-    *reinterpret_cast<uint32_t*>(s + 2 * kQStageBytes + 4 * i) = *reinterpret_cast<const uint32_t*>(a.c.ke + at);
-    if constexpr (WITH_V)
-      *reinterpret_cast<uint32_t*>(s + 2 * kQStageBytes + ST + 4 * i) = *reinterpret_cast<const uint32_t*>(a.c.ve + at);
+// Loads as inline asm: the compiler neither counts them nor waits for them; the
+// loading wave, which issues no other vector memory operation (but to flag an
+// error, which only makes a wait longer), counts them itself.  An LDS load may
+// not directly follow the scalar write of M0 that gives its LDS address (one
+// wait state, hence the s_nop).
+__device__ __forceinline__ void lds_load16(int64_t base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void lds_load4(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds), "v"(p) : "memory", "m0");
+}
+// Wait until at most `stages` later stages' loads (N each) are in flight.
+template <int N, int MOST>
+__device__ __forceinline__ void wait_stage(int stages) {
+  static_assert(MOST * N < 64, "vmcnt holds 6 bits");
+  if constexpr (MOST == 0) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  } else {
+    if (stages >= MOST) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N * MOST) : "memory");
+    else wait_stage<N, MOST - 1>(stages);
   }
 }
 
-template <int D, int RT>
-__global__ void __launch_bounds__((Shape<D, RT>::kThreads)) q8_part_kernel(QArgs a) {
-  typedef Shape<D, RT> S_;
-  constexpr int DPL = D / 16, TW = S_::TW, ST = S_::ST, NB = S_::NB;
-  __shared__ int32_t s_pages[kPageSlots];
-  __shared__ __align__(256) char s_stage[S_::kStage];
+// The row index (in rows of codes) of the unit that token t opens.  A page entry
+// outside the pool is flagged and clamped into it.
+__device__ __forceinline__ int64_t unit_row(const QArgs& a, const Piece& p, int t) {
+  if (!a.c.table) return ((int64_t)p.b * a.Hkv + p.g) * a.c.n_cap + t;
+  int pg = uniform_load(a.c.table, (int64_t)p.b * a.c.max_pages + (t >> a.c.shift));
+  if (pg < 0 || pg >= a.c.n_pages) {
+    dev_flag(a.status, PVLM_DEV_RANGE);
+    pg = pg < 0 ? 0 : (int)(a.c.n_pages - 1);
+  }
+  return (((int64_t)pg * a.Hkv + p.g) << a.c.shift) + (t & ((1 << a.c.shift) - 1));
+}
 
-  Unit u;
-  if (!decode_unit(a, u)) return;
-  const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Rows rows = rows_setup(a, u, s_pages);
-  const int nst = (u.c1 - u.c0 + ST - 1) / ST;
-
-  const int rt = w / TW, tw = w % TW, gt = u.rg * RT + rt;  // row tile of the KV head
-  const bool live = gt < a.RTT;
-  const int row = gt * 16 + n;
-  const int lim = row < a.R ? min(u.c1 - 1, u.ctx + row_t(a, row)) : -1;  // last token the lane's row sees
-  const int vis_all = min(u.c1 - 1, u.ctx);                               // row 0 sees the least
-  Query<D> q;
-  load_query<D>(a, u.b, u.g, row, gq, q);
-  float ref = kNegInf, z = 0.f;
-  floatx4 O[DPL];
+// One side (K or V) of the stage at token t0 into LDS.  Rows past the piece repeat its last one;
+// exponents are read in groups of four rows, which never leave a unit.
+template <int D, bool IS_K>
+__device__ __forceinline__ void issue_stage(const QArgs& a, const Piece& p, int t0, const uint32_t (&off)[IS_K ? 2 : 1][Ring<D>::IPU],
+                                            uint32_t lds, int lane) {
+  typedef Ring<D> R_;
+  typedef Lay<D> L;
+  const uint8_t* codes = IS_K ? a.c.kc : a.c.vc;
+  const uint8_t* exps = IS_K ? a.c.ke : a.c.ve;
+  const int last = p.c1 - 1;
+  int64_t row[4];
 #pragma unroll
-  for (int jd = 0; jd < DPL; ++jd) O[jd] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int u = 0; u < 4; ++u) row[u] = unit_row(a, p, min(t0 + 32 * u, last & ~31));
+  const bool whole = t0 + R_::ST <= p.c1;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int64_t base = uniform64((int64_t)(uintptr_t)(codes + row[u] * D));
+#pragma unroll
+    for (int i = 0; i < R_::IPU; ++i) {
+      uint32_t o = off[IS_K ? u & 1 : 0][i];
+      if (!whole) {  // (offsets are row * D + 16 * chunk, rows counted from the unit)
+        const int most = max(0, last - (t0 + 32 * u));
+        const int at = t0 + 32 * u > last ? (last & 31) : min((int)(o / D), most);
+        o = at * D + o % D;
+      }
+      lds_load16(base, o, lds + (u * R_::IPU + i) * 1024);
+    }
+  }
+  // lane l: rows 4 l .. 4 l + 3 (lanes past the stage repeat)
+  const int l = lane & 31, u = l >> 3;
+  const int64_t r = u == 0 ? row[0] : u == 1 ? row[1] : u == 2 ? row[2] : row[3];
+  lds_load4(exps + r + 4 * (l & 7), lds + R_::KB);
+}
 
-  for (int s = 0; s < nst; ++s) {
-    __syncthreads();
-    load_stage<D, true>(a, rows, u.c0 + s * ST, u.c1, s_stage);
-    __syncthreads();
-    for (int x = 0; x < NB; ++x) {
-      const int r0 = (tw * NB + x) * 64, tb = u.c0 + s * ST + r0;
-      if (tb >= u.c1 || !live) break;
-      const char *kb = s_stage, *vb = s_stage + kQStageBytes, *eb = s_stage + 2 * kQStageBytes;
-      const uint32_t ke = *reinterpret_cast<const uint32_t*>(eb + r0 + 4 * n);
-      const uint4 ve4 = *reinterpret_cast<const uint4*>(eb + ST + r0 + 16 * gq);
-      const uint32_t ve[4] = {ve4.x, ve4.y, ve4.z, ve4.w};
-      floatx4 S[4];
-      scores<D>(kb, ke, r0, n, gq, q, S);
-      const bool tail = tb + 63 > vis_all;
-      uint32_t seen = 0xffffu;
-      if (tail) {
-        const int off = lim - tb - 16 * gq;  // the lane's token j is visible iff j <= off
-        seen = off < 0 ? 0u : off >= 15 ? 0xffffu : (2u << off) - 1u;
+// What a loading wave does: every stage of the workgroup's share, kSlots - 1
+// stages ahead, in STRIDE bytes a slot.
+template <int D, bool IS_K, int SLOTS, int STRIDE>
+__device__ __forceinline__ void load_share(const QArgs& a, Piece p, char* ring) {
+  typedef Ring<D> R_;
+  typedef Lay<D> L;
+  const int lane = threadIdx.x & 63;
+  // offsets of a lane's pieces in a unit; K's order repeats every two units, V's every one
+  uint32_t off[IS_K ? 2 : 1][R_::IPU];
+#pragma unroll
+  for (int u = 0; u < (IS_K ? 2 : 1); ++u)
+#pragma unroll
+    for (int i = 0; i < R_::IPU; ++i) {
+      const int line = (32 * u + i * R_::RPI) / L::LR + lane / 16;
+      const int at = (lane & 15) ^ (IS_K ? L::kkey(line) : L::vkey(line));
+      off[u][i] = (line * L::LR - 32 * u + at / L::CH) * D + 16 * (at % L::CH);
+    }
+  const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(ring));
+  __builtin_amdgcn_s_setprio(3);  // the loads go out before the other waves' arithmetic
+  __builtin_amdgcn_s_waitcnt(0);  // the counts start from zero
+  int issued = 0, t0 = p.c0;
+  bool more = true;
+  auto issue = [&]() {
+    issue_stage<D, IS_K>(a, p, t0, off, base + (issued % SLOTS) * STRIDE, lane);
+    ++issued;
+    t0 += R_::ST;
+    if (t0 >= p.c1) {
+      more = p.next(a);
+      t0 = p.c0;
+    }
+  };
+  for (int s = 0; s < SLOTS - 1 && more; ++s) issue();
+  for (int s = 0; s < issued; ++s) {
+    wait_stage<R_::NI + 1, SLOTS - 2>(issued - 1 - s);
+    lds_sync();  // stage s has landed; every wave is done with stage s - 1
+    if (more) issue();
+  }
+}
+
+template <int RT>
+struct Waves {
+  static constexpr int TPW = q8_waves(RT).tpw, RW = q8_waves(RT).rw;
+  static constexpr int kCompute = RW * kQTokenWaves;
+  static constexpr int per_eu(int loaders) { return (kCompute + loaders + 3) / 4; }
+};
+
+// -------------------------------------------------------- partial kernel --
+template <int D>
+struct PartRing {
+  static constexpr int kSlots = D == 128 ? 4 : 8, kStride = 2 * Ring<D>::kSide, kLds = kSlots * kStride;
+};
+
+// A wave's state: TPW row tiles against the tokens of its blocks.
+template <int D, int TPW>
+struct PartWave {
+  static constexpr int DPL = D / 16;
+  Query<D> q[TPW];
+  int lim[TPW];  // last token that the lane's row sees
+  float ref[TPW], z[TPW];
+  floatx4 O[TPW][DPL], zt[TPW];
+
+  __device__ __forceinline__ void begin(const QArgs& a, const Piece& p, int tile0, int tiles, int n, int gq) {
+#pragma unroll
+    for (int x = 0; x < TPW; ++x) {
+      const int row = (tile0 + x) * 16 + n;
+      load_query<D>(a, p.b, p.g, row, gq, q[x]);
+      lim[x] = x < tiles && row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
+      ref[x] = kNegInf;
+      z[x] = 0.f;
+      zt[x] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int jd = 0; jd < DPL; ++jd) O[x][jd] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // The block of tokens tb .. tb + 63, rows r0 .. r0 + 63 of the stage.  TAIL: some row does not see all of them.
+  template <bool TAIL>
+  __device__ __forceinline__ void block(const QArgs& a, const char* kb, int tb, int r0, int n, int gq) {
+    typedef Ring<D> R_;
+    const char* vb = kb + R_::kSide;
+    const uint32_t ke = *reinterpret_cast<const uint32_t*>(kb + R_::KB + r0 + 4 * n);
+    const uint4 ve4 = *reinterpret_cast<const uint4*>(vb + R_::KB + r0 + 16 * gq);
+    const uint32_t ve[4] = {ve4.x, ve4.y, ve4.z, ve4.w};
+    floatx4 S[TPW][4];
+    scores<D, TPW>(kb, ke, r0, n, gq, q, S);
+    uint32_t seen[TPW];
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int x = 0; x < TPW; ++x) {
+        const int o = lim[x] - tb - 16 * gq;  // the lane's token j is visible iff j <= o
+        seen[x] = o < 0 ? 0u : o >= 15 ? 0xffffu : (2u << o) - 1u;
 #pragma unroll
         for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (!((seen >> (4 * i + tt)) & 1)) S[tt][i] = kNegInf;
+            if (!((seen[x] >> (4 * i + tt)) & 1)) S[x][tt][i] = kNegInf;
       }
-      float mx = kNegInf;
+    }
+    float mx[TPW];
+    bool grow = false;
 #pragma unroll
-      for (int tt = 0; tt < 4; ++tt) mx = fmaxf(fmaxf(mx, fmaxf(S[tt][0], S[tt][1])), fmaxf(S[tt][2], S[tt][3]));
-      mx = rows4_max(mx) * a.sl2;
-      if (__any(mx > ref + kRefSlack)) {  // the first block, and seldom after it
-        const float nm = fmaxf(ref, mx);
-        const float al = ref == kNegInf ? 0.f : fast_exp2(ref - nm);
-        z *= al;
-        ref = nm;
+    for (int x = 0; x < TPW; ++x) {
+      float m = kNegInf;
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt)
+        m = fmaxf(fmaxf(m, fmaxf(S[x][tt][0], S[x][tt][1])), fmaxf(S[x][tt][2], S[x][tt][3]));
+      mx[x] = rows4_max(m) * a.sl2;
+      grow |= mx[x] > ref[x] + kRefSlack;
+    }
+    if (__any(grow)) {  // the first block, and seldom after it
+#pragma unroll
+      for (int x = 0; x < TPW; ++x) {
+        const float nm = fmaxf(ref[x], mx[x]);
+        const float al = ref[x] == kNegInf ? 0.f : fast_exp2(ref[x] - nm);
+        z[x] *= al;
+        ref[x] = nm;
         floatx4 f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = __shfl(al, 4 * gq + i, 64);
+        zt[x] = zt[x] * f;
 #pragma unroll
-        for (int jd = 0; jd < DPL; ++jd) O[jd] = O[jd] * f;
-      }
-      const float r = ref == kNegInf ? 0.f : ref;  // no visible token yet: P = 0
-      float P[16];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int tt = 0; tt < 4; ++tt) {
-          const float p = fast_exp2(fmaf(S[tt][i], a.sl2, -r));
-          z += p;
-          P[4 * i + tt] = p * q8_unit((ve[i] >> (8 * tt)) & 0xffu);
-        }
-      if (!tail) {
-        weigh<D>(vb, r0, n, gq, P, O);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (!((seen >> j) & 1)) P[j] = 0.f;  // (an unwritten row's exponent may be anything)
-        weigh_masked<D>(vb, r0, n, gq, P, seen, O);
+        for (int jd = 0; jd < DPL; ++jd) O[x][jd] = O[x][jd] * f;
       }
     }
+    const VPair v0 = read_pair<D>(vb, r0, n, gq, 0);
+    bf16x8 ones;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ones[j] = static_cast<__bf16>(1.f);
+    bf16x8 pv[TPW][2];
+#pragma unroll
+    for (int x = 0; x < TPW; ++x) {
+      const float r = ref[x] == kNegInf ? 0.f : ref[x];  // no visible token yet: P = 0
+      bf16x8 pz[2];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const float e = fast_exp2(fmaf(S[x][j % 4][j / 4], a.sl2, -r));
+        z[x] += e;
+        pz[j / 8][j % 8] = static_cast<__bf16>(e);
+        float y = e * q8_unit((ve[j / 4] >> (8 * (j % 4))) & 0xffu);
+        if constexpr (TAIL)
+          if (!((seen[x] >> j) & 1)) y = 0.f;  // (an unwritten row's exponent may be anything)
+        pv[x][j / 8][j % 8] = static_cast<__bf16>(y);
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) zt[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pz[ks], ones, zt[x], 0, 0, 0);
+    }
+    if constexpr (TAIL) weigh_masked<D, TPW>(vb, r0, n, gq, pv, seen, O);
+    else weigh<D, TPW>(vb, r0, n, gq, pv, v0, O);
   }
 
-  z = rows4_sum(z);
-  if constexpr (TW > 1) {  // the second token wave's sums join the first's
-    floatx4* xo = reinterpret_cast<floatx4*>(s_stage) + rt * (DPL * 64 + 64);
-    static_assert(RT * (DPL * 64 + 64) * 16 <= S_::kStage, "the exchange fits the stage");
-    __syncthreads();
-    if (tw == 1) {
+  __device__ __forceinline__ void end(const QArgs& a, size_t rec0, int tile0, int tiles, int n, int gq) {
 #pragma unroll
-      for (int jd = 0; jd < DPL; ++jd) xo[jd * 64 + lane] = O[jd];
-      xo[DPL * 64 + lane] = floatx4{ref, z, 0.f, 0.f};
+    for (int x = 0; x < TPW; ++x) {
+      if (x >= tiles) break;
+      const size_t rec = (rec0 + x * kQTokenWaves) * 16;
+      const float zz = rows4_sum(z[x]);
+      if (gq == 0) a.stats[rec + n] = make_float2(ref[x], zz);
+      if (n == 0) *reinterpret_cast<floatx4*>(a.zt + rec + 4 * gq) = zt[x];
+      // position DPL n + jd of a stored row holds column 16 jd + n
+      float* op = a.opart + rec * D;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if ((tile0 + x) * 16 + 4 * gq + i < a.R)
+#pragma unroll
+          for (int h = 0; h < DPL / 4; ++h)
+            *reinterpret_cast<float4*>(op + (4 * gq + i) * D + DPL * n + 4 * h) =
+                make_float4(O[x][4 * h][i], O[x][4 * h + 1][i], O[x][4 * h + 2][i], O[x][4 * h + 3][i]);
     }
-    __syncthreads();
-    if (tw == 1) return;
-    const floatx4 o = xo[DPL * 64 + lane];
-    const float M = fmaxf(ref, o[0]), r = M == kNegInf ? 0.f : M;
-    const float f0 = z != 0.f ? fast_exp2(ref - r) : 0.f, f1 = o[1] != 0.f ? fast_exp2(o[0] - r) : 0.f;
-    z = z * f0 + o[1] * f1;
-    ref = M;
-    floatx4 g0, g1;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      g0[i] = __shfl(f0, 4 * gq + i, 64);
-      g1[i] = __shfl(f1, 4 * gq + i, 64);
-    }
-#pragma unroll
-    for (int jd = 0; jd < DPL; ++jd) O[jd] = O[jd] * g0 + xo[jd * 64 + lane] * g1;
   }
-  if (!live) return;
-  const size_t rec = (size_t)(u.bg * a.RTT + gt) * a.splits + u.split;
-  if (gq == 0) a.stats[rec * 16 + n] = make_float2(ref, z);
-  // position DPL n + jd of a stored row holds column 16 jd + n
-  float* op = a.opart + rec * 16 * D;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int h = 0; h < DPL / 4; ++h)
-      *reinterpret_cast<float4*>(op + (4 * gq + i) * D + DPL * n + 4 * h) =
-          make_float4(O[4 * h][i], O[4 * h + 1][i], O[4 * h + 2][i], O[4 * h + 3][i]);
+};
+
+template <int D, int RT>
+__global__ void __launch_bounds__(((Waves<RT>::kCompute + 2) * 64))
+__attribute__((amdgpu_waves_per_eu(Waves<RT>::per_eu(2), Waves<RT>::per_eu(2)))) q8_part_kernel(QArgs a) {
+  typedef Waves<RT> W_;
+  typedef Ring<D> R_;
+  typedef PartRing<D> P_;
+  constexpr int TPW = W_::TPW;
+  extern __shared__ __align__(1024) char s_ring[];  // [slot][K, V][codes, exponents]
+
+  Piece p;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (blockIdx.x == 0 && w == 0)
+    for (int b = threadIdx.x; b < a.B; b += 64)
+      if (a.ctx_len[b] < 0 || a.ctx_len[b] > a.max_ctx) dev_flag(a.status, PVLM_DEV_RANGE);
+  if (!p.first(a)) return;
+  if (w == W_::kCompute) {
+    load_share<D, true, P_::kSlots, P_::kStride>(a, p, s_ring);
+    return;
+  }
+  if (w == W_::kCompute + 1) {
+    load_share<D, false, P_::kSlots, P_::kStride>(a, p, s_ring + R_::kSide);
+    return;
+  }
+  const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+  const int tw = w % kQTokenWaves, t_first = w / kQTokenWaves * TPW;  // its blocks, and its first tile
+  int slot = 0;
+  do {
+    const int tiles = min(RT, a.RTT - p.rg * RT) - t_first;  // of the wave; further ones are idle
+    PartWave<D, TPW> v;
+    v.begin(a, p, p.rg * RT + t_first, tiles, n, gq);
+    // stages before the first of which some row does not see all
+    const int vis_all = min(p.c1 - 1, p.ctx);
+    const char* base = s_ring;
+    int t0 = p.c0;
+    for (; t0 < p.c1; t0 += R_::ST) {
+      lds_sync();
+      base = s_ring + slot * P_::kStride;
+      slot = slot + 1 == P_::kSlots ? 0 : slot + 1;
+      const int tb = t0 + 64 * tw;
+      if (tb >= p.c1 || tiles <= 0) continue;
+      if (tb + 63 <= vis_all) v.template block<false>(a, base, tb, 64 * tw, n, gq);
+      else v.template block<true>(a, base, tb, 64 * tw, n, gq);
+    }
+    v.end(a, ((size_t)(p.group(a) + blockIdx.x) * RT + t_first) * kQTokenWaves + tw, p.rg * RT + t_first, tiles, n, gq);
+  } while (p.next(a));
 }
 
 // ----------------------------------------------------------- mass kernel --
-// The partial kernel's units again, every row's log-sum-exp known.
-template <int D, int RT>
-__global__ void __launch_bounds__((Shape<D, RT>::kThreads)) q8_mass_kernel(QArgs a) {
-  typedef Shape<D, RT> S_;
-  constexpr int TW = S_::TW, ST = S_::ST, NB = S_::NB;
-  __shared__ int32_t s_pages[kPageSlots];
-  __shared__ __align__(256) char s_stage[S_::kStage];
-  __shared__ float s_sum[RT][ST];
+// The partial kernel's shares again, every row's log-sum-exp known.
+template <int D>
+struct MassRing {
+  static constexpr int kSlots = D == 128 ? 4 : 8, kStride = Ring<D>::kSide, kLds = kSlots * kStride;
+};
 
-  Unit u;
-  if (!decode_unit(a, u)) return;
-  const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+template <int D, int RT>
+__global__ void __launch_bounds__(((Waves<RT>::kCompute + 1) * 64))
+__attribute__((amdgpu_waves_per_eu(Waves<RT>::per_eu(1), Waves<RT>::per_eu(1)))) q8_mass_kernel(QArgs a) {
+  typedef Waves<RT> W_;
+  typedef Ring<D> R_;
+  typedef MassRing<D> P_;
+  constexpr int TPW = W_::TPW;
+  extern __shared__ __align__(1024) char s_ring[];
+
+  Piece p;
+  if (!p.first(a)) return;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Rows rows = rows_setup(a, u, s_pages);
-  const int nst = (u.c1 - u.c0 + ST - 1) / ST;
-  const int rt = w / TW, tw = w % TW, gt = u.rg * RT + rt;
-  const int row = gt * 16 + n;
-  const int lim = row < a.R ? min(u.c1 - 1, u.ctx + row_t(a, row)) : -1;
-  Query<D> q;
-  load_query<D>(a, u.b, u.g, row, gq, q);
-  const float lse = tile_lse(a, u.bg * a.RTT + min(gt, a.RTT - 1), row < a.R, (u.N + a.chunk - 1) / a.chunk, n, gq);
-  float* mp = a.mpart + ((size_t)u.bg * a.RG + u.rg) * a.c.n_cap;
-  for (int s = 0; s < nst; ++s) {
-    __syncthreads();
-    load_stage<D, false>(a, rows, u.c0 + s * ST, u.c1, s_stage);
-    __syncthreads();
-    for (int x = 0; x < NB; ++x) {
-      const int r0 = (tw * NB + x) * 64, tb = u.c0 + s * ST + r0;
-      if (tb >= u.c1) break;
-      const uint32_t ke = *reinterpret_cast<const uint32_t*>(s_stage + 2 * kQStageBytes + r0 + 4 * n);
-      floatx4 S[4];
-      scores<D>(s_stage, ke, r0, n, gq, q, S);
-      const int off = lim - tb - 16 * gq;
-      float P[16];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int tt = 0; tt < 4; ++tt)
-          P[4 * i + tt] = 4 * i + tt <= off ? fast_exp2(fmaf(S[tt][i], a.sl2, -lse)) : 0.f;
-      rows_to_lds(P, &s_sum[rt][r0], lane);
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < ST; i += (int)blockDim.x) {
-      const int t = u.c0 + s * ST + i;
-      if (t < u.c1) {
-        float sum = s_sum[0][i];
-#pragma unroll
-        for (int k = 1; k < RT; ++k) sum += s_sum[k][i];
-        mp[t] = sum;
-      }
-    }
+  if (w == W_::kCompute) {
+    load_share<D, true, P_::kSlots, P_::kStride>(a, p, s_ring);
+    return;
   }
+  const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
+  const int tw = w % kQTokenWaves, rw = w / kQTokenWaves, t_first = rw * TPW;
+  int slot = 0;
+  do {
+    const int tiles = min(RT, a.RTT - p.rg * RT);
+    const Holders h = holders(a, p.per, p.before, p.b, p.g * a.RG + p.rg, p.ctx);
+    Query<D> q[TPW];
+    int lim[TPW];
+    float lse[TPW];
+    bool real[TPW];
+#pragma unroll
+    for (int x = 0; x < TPW; ++x) {
+      const int row = (p.rg * RT + t_first + x) * 16 + n;
+      real[x] = t_first + x < tiles && row < a.R;
+      load_query<D>(a, p.b, p.g, row, gq, q[x]);
+      lim[x] = real[x] ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
+    }
+    tile_lse<RT, TPW>(a, h, t_first, tiles, real, n, gq, lse);
+    const int vis_all = min(p.c1 - 1, p.ctx);
+    float* mp = a.mpart + ((size_t)p.group(a) * W_::RW + rw) * a.c.n_cap;
+    for (int t0 = p.c0; t0 < p.c1; t0 += R_::ST) {
+      lds_sync();
+      const char* kb = s_ring + slot * P_::kStride;
+      slot = slot + 1 == P_::kSlots ? 0 : slot + 1;
+      const int r0 = 64 * tw, tb = t0 + r0;
+      if (tb >= p.c1) continue;
+      const uint32_t ke = *reinterpret_cast<const uint32_t*>(kb + R_::KB + r0 + 4 * n);
+      floatx4 S[TPW][4];
+      scores<D, TPW>(kb, ke, r0, n, gq, q, S);
+      const bool tail = tb + 63 > vis_all || t_first + TPW > tiles;
+      float sum[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) sum[j] = 0.f;
+#pragma unroll
+      for (int x = 0; x < TPW; ++x) {
+        const int o = lim[x] - tb - 16 * gq;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float e = fast_exp2(fmaf(S[x][j % 4][j / 4], a.sl2, -lse[x]));
+          sum[j] += !tail || j <= o ? e : 0.f;
+        }
+      }
+      const float m = row_sums(sum, lane);
+      if (tb + lane < p.c1) mp[tb + lane] = m;
+    }
+  } while (p.next(a));
 }
 
 // --------------------------------------------------------- finish kernel --
-// One wave per row of O: the sum over its chunks of the partials weighted by
-// exp2(chunk maximum - row maximum) / row sum, and the row's log-sum-exp.
-template <int D>
-__device__ __forceinline__ void combine_row(const QArgs& a, int64_t id) {
-  constexpr int LPR = D / 4, SG = 64 / LPR;  // lanes of a row, chunks side by side
-  if (id >= (int64_t)a.B * a.Hkv * a.R) return;
-  const int lane = threadIdx.x & 63, sg = lane / LPR, col = lane % LPR;
-  const int bg = (int)(id / a.R), row = (int)(id - (int64_t)bg * a.R);
-  const int b = bg / a.Hkv, g = bg - b * a.Hkv;
-  const int nsp = (seq_ctx(a, b, false) + a.T + a.chunk - 1) / a.chunk;
-  const size_t rec = ((size_t)bg * a.RTT + row / 16) * a.splits * 16 + row % 16;
-  const float2* st = a.stats + rec;
-  const float* op = a.opart + rec * D + 4 * col;
-  float M = kNegInf, Z = 0.f;
-  for (int s = lane; s < nsp; s += 64) join(M, Z, st[(size_t)s * 16].x, st[(size_t)s * 16].y);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) join(M, Z, __shfl_xor(M, o, 64), __shfl_xor(Z, o, 64));
-  const float r = M == kNegInf ? 0.f : M, inv = 1.f / Z;
-  float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = sg; s < nsp; s += SG) {
-    const float2 v = st[(size_t)s * 16];
-    const float wt = v.y != 0.f ? fast_exp2(v.x - r) * inv : 0.f;
-    const float4 p = *reinterpret_cast<const float4*>(op + (size_t)s * 16 * D);
-    if (v.y != 0.f) {
-      acc[0] = fmaf(wt, p.x, acc[0]);
-      acc[1] = fmaf(wt, p.y, acc[1]);
-      acc[2] = fmaf(wt, p.z, acc[2]);
-      acc[3] = fmaf(wt, p.w, acc[3]);
-    }
-  }
-#pragma unroll
-  for (int o = LPR; o < 64; o <<= 1)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) acc[k] += __shfl_xor(acc[k], o, 64);
-  const int t = row_t(a, row), h = g * a.G + row - t * a.G;
-  if (sg == 0) {
-    constexpr int DPL = D / 16;
-    uint16_t* o = a.out + (((size_t)b * a.T + t) * a.Hq + h) * D;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int at = 4 * col + k;
-      o[16 * (at % DPL) + at / DPL] = f32_to_bf16(acc[k]);
-    }
-  }
-  if (a.lse && lane == 0) a.lse[((size_t)b * a.Hq + h) * a.T + t] = (M + __log2f(Z)) * kLn2;
+// A row of O: the sum over its records of the partials weighted by
+// exp2(record's maximum - row maximum), over the rounded probabilities' sum, and
+// the row's log-sum-exp.  Dividing by the sum of what P . V took in, and not of
+// the unrounded probabilities, leaves a row that one token dominates with the
+// rounding of its result alone.
+//
+// D / 4 lanes take a record, four columns each.  Every such set joins its own
+// records (kU in flight: the kernel is bound by these round trips), then the
+// sets of a wave and, with WPR waves a row, the waves through LDS.
+struct RowSum {
+  float m, z, zt;
+  floatx4 o;
+};
+__device__ __forceinline__ void join(RowSum& a, float m, float z, float zt, floatx4 o) {
+  const float M = fmaxf(a.m, m), r = M == kNegInf ? 0.f : M;
+  const float f = a.z != 0.f ? fast_exp2(a.m - r) : 0.f, g = z != 0.f ? fast_exp2(m - r) : 0.f;
+  a.z = (a.z != 0.f ? a.z * f : 0.f) + (z != 0.f ? z * g : 0.f);
+  a.zt = a.zt * f + zt * g;
+  a.o = a.o * f + o * g;
+  a.m = M;
 }
 
-// The mass of every cache row: the sum of its KV heads' and row groups'
-// partials in order (0 past the sequence).
+template <int D, int RT, int WPR>
+__device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_row)[D / 4]) {
+  constexpr int LPR = D / 4, SG = 64 / LPR, TW = kQTokenWaves, kU = 8;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane % LPR;
+  const int id = wg * (kFinWaves / WPR) + w / WPR;  // (fewer than 2^22 rows)
+  const bool row_here = id < a.B * a.Hkv * a.R;
+  RowSum t{kNegInf, 0.f, 0.f, floatx4{0.f, 0.f, 0.f, 0.f}};
+  int b = 0, g = 0, row = 0;
+  if (row_here) {
+    const int bg = __builtin_amdgcn_readfirstlane(id / a.R);
+    row = id - bg * a.R;
+    b = bg / a.Hkv;
+    g = bg - b * a.Hkv;
+    const Shares s_ = find<false>(a, 0, b);
+    const int rg = row / (16 * RT), tile = row / 16 - rg * RT;
+    const Holders h = holders(a, s_.per, s_.before, b, g * a.RG + rg, s_.ctx);
+    const size_t rec = ((size_t)h.rec * RT + tile) * TW * 16 + row % 16;
+    const int cnt = h.count * TW, sets = SG * WPR;
+    for (int s0 = lane / LPR + SG * (w % WPR); s0 < cnt; s0 += kU * sets) {
+      float2 v[kU];
+      float zt[kU];
+      floatx4 o[kU];
+#pragma unroll
+      for (int j = 0; j < kU; ++j) {
+        const int s = min(s0 + j * sets, cnt - 1);
+        const size_t i = rec + (size_t)(s / TW * RT * TW + s % TW) * 16;
+        v[j] = a.stats[i];
+        zt[j] = a.zt[i];
+        o[j] = *reinterpret_cast<const floatx4*>(a.opart + i * D + 4 * col);
+      }
+      float m = t.m;
+#pragma unroll
+      for (int j = 0; j < kU; ++j) m = fmaxf(m, v[j].x);
+      const float r = m == kNegInf ? 0.f : m, f = t.z != 0.f ? fast_exp2(t.m - r) : 0.f;
+      t.z = t.z != 0.f ? t.z * f : 0.f;
+      t.zt *= f;
+      t.o = t.o * f;
+      t.m = m;
+#pragma unroll
+      for (int j = 0; j < kU; ++j)
+        if (s0 + j * sets < cnt && v[j].y != 0.f) {  // (0: nothing that the row sees)
+          const float e = fast_exp2(v[j].x - r);
+          t.z = fmaf(v[j].y, e, t.z);
+          t.zt = fmaf(zt[j], e, t.zt);
+          t.o = t.o + o[j] * e;
+        }
+    }
+#pragma unroll
+    for (int o = LPR; o < 64; o <<= 1) {
+      floatx4 y;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] = __shfl_xor(t.o[k], o, 64);
+      join(t, __shfl_xor(t.m, o, 64), __shfl_xor(t.z, o, 64), __shfl_xor(t.zt, o, 64), y);
+    }
+  }
+  if constexpr (WPR > 1) {
+    if (lane < LPR) s_row[w][lane] = t;
+    __syncthreads();
+    if (w % WPR) return;
+    for (int k = 1; k < WPR; ++k) {
+      const RowSum y = s_row[w + k][col];
+      join(t, y.m, y.z, y.zt, y.o);
+    }
+  }
+  if (!row_here || lane >= LPR) return;
+  const int tt = row_t(a, row), head = g * a.G + row - tt * a.G;
+  constexpr int DPL = D / 16;
+  const float inv = 1.f / t.zt;
+  uint16_t* o = a.out + (((size_t)b * a.T + tt) * a.Hq + head) * D;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int c = 4 * col + k;
+    o[16 * (c % DPL) + c / DPL] = f32_to_bf16(t.o[k] * inv);
+  }
+  if (a.lse && lane == 0) a.lse[((size_t)b * a.Hq + head) * a.T + tt] = (t.m + __log2f(t.z)) * kLn2;
+}
+
+// The mass of every cache row: the sum of its groups' and waves' partials in
+// order (0 past the sequence).
+template <int RT>
 __device__ __forceinline__ void sum_mass(const QArgs& a, int id) {
-  const int P = a.Hkv * a.RG;
+  const int P = a.HR * Waves<RT>::RW;
   const int b = id / a.mass_per;
   const int64_t t0 = (int64_t)(id - b * a.mass_per) * a.mass_rows;
-  const int N = seq_ctx(a, b, false) + a.T;
+  const int N = clamp_ctx(a, a.ctx_len[b]) + a.T;
   const float* mp = a.mpart + (size_t)b * P * a.c.n_cap;
   float* mass = a.mass + (size_t)b * a.c.n_cap;
   for (int64_t t = t0 + threadIdx.x; t < min(t0 + a.mass_rows, a.c.n_cap); t += kFinThreads) {
+    constexpr int kU = 8;  // partials in flight
     float sum = 0.f;
     if (t < N)
-      for (int p = 0; p < P; ++p) sum += mp[(size_t)p * a.c.n_cap + t];
+      for (int p0 = 0; p0 < P; p0 += kU) {
+        float v[kU];
+#pragma unroll
+        for (int j = 0; j < kU; ++j) v[j] = mp[(size_t)min(p0 + j, P - 1) * a.c.n_cap + t];
+#pragma unroll
+        for (int j = 0; j < kU; ++j)
+          if (p0 + j < P) sum += v[j];
+      }
     mass[t] = sum;
   }
 }
 
-template <int D>
+template <int D, int RT, int WPR>
 __global__ void __launch_bounds__(kFinThreads) q8_finish_kernel(QArgs a) {
+  __shared__ RowSum s_row[WPR > 1 ? kFinWaves : 1][D / 4];
   const int id = blockIdx.x;
-  if (id < a.mass_wgs) sum_mass(a, id);
-  else combine_row<D>(a, (int64_t)(id - a.mass_wgs) * kFinWaves + (threadIdx.x >> 6));
+  if (id < a.mass_wgs) sum_mass<RT>(a, id);
+  else combine_rows<D, RT, WPR>(a, id - a.mass_wgs, s_row);
 }
 
 // ------------------------------------------------------------------ host --
 typedef void (*QKernel)(QArgs);
 struct QKernels {
-  QKernel part, mass, finish;
-  int threads;
+  QKernel part, mass, finish[2];  // finish: one wave, or a workgroup, for a row
+  int part_threads, mass_threads, part_lds, mass_lds;
 };
 
+template <int D, int RT>
+QKernels kernels() {
+  return {q8_part_kernel<D, RT>, q8_mass_kernel<D, RT>, {q8_finish_kernel<D, RT, 1>, q8_finish_kernel<D, RT, kFinWaves>}, (Waves<RT>::kCompute + 2) * 64,
+          (Waves<RT>::kCompute + 1) * 64, PartRing<D>::kLds, MassRing<D>::kLds};
+}
 template <int D>
 QKernels pick(int RT) {
-#define PVLM_Q8_RT(n) \
-  case n: return {q8_part_kernel<D, n>, q8_mass_kernel<D, n>, q8_finish_kernel<D>, Shape<D, n>::kThreads};
   switch (RT) {
-    PVLM_Q8_RT(1)
-    PVLM_Q8_RT(2)
-    PVLM_Q8_RT(3)
-    PVLM_Q8_RT(4)
-    PVLM_Q8_RT(5)
-    PVLM_Q8_RT(6)
-    PVLM_Q8_RT(7)
-    PVLM_Q8_RT(8)
-    default:
-    PVLM_Q8_RT(9)
+    case 1: return kernels<D, 1>();
+    case 2: return kernels<D, 2>();
+    case 3: return kernels<D, 3>();
+    case 4: return kernels<D, 4>();
+    case 5: return kernels<D, 5>();
+    case 6: return kernels<D, 6>();
+    case 7: return kernels<D, 7>();
+    case 8: return kernels<D, 8>();
+    default: return kernels<D, 9>();
   }
-#undef PVLM_Q8_RT
 }
 
 pvlm_status verify_q8_run(int B, int T, int Hq, int Hkv, int D, int64_t max_ctx, float scale, const void* q,
@@ -669,13 +973,13 @@ pvlm_status verify_q8_run(int B, int T, int Hq, int Hkv, int D, int64_t max_ctx,
   a.g_magic = (1u << 20) / (unsigned)p.G + 1u;
   a.RTT = p.RTT;
   a.RG = p.RG;
+  a.HR = Hkv * p.RG;
   a.max_ctx = (int)max_ctx;
-  a.splits = p.splits;
-  a.chunk = p.chunk;
-  a.units = B * Hkv * p.RG * p.splits;
-  a.sl2 = scale * kLog2e;
+  a.wgs = p.wgs;
+  a.sl2 = (float)((double)scale * kLog2e);
   a.mpart = reinterpret_cast<float*>(wsb + p.off_mpart);
   a.stats = reinterpret_cast<float2*>(wsb + p.off_stats);
+  a.zt = reinterpret_cast<float*>(wsb + p.off_zt);
   a.opart = reinterpret_cast<float*>(wsb + p.off_opart);
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
@@ -685,15 +989,19 @@ pvlm_status verify_q8_run(int B, int T, int Hq, int Hkv, int D, int64_t max_ctx,
   a.mass_per = (int)mass_workgroups(c.n_cap, a.mass_rows);
   a.mass_wgs = mass ? B * a.mass_per : 0;
   const QKernels k = D == 128 ? pick<128>(p.RT) : pick<64>(p.RT);
-  const dim3 grid((a.units + 7) / 8 * 8);
-  hipLaunchKernelGGL(k.part, grid, dim3(k.threads), 0, stream, a);
+  PVLM_HIP(allow_dynamic_lds(reinterpret_cast<const void*>(k.part), k.part_lds));
+  hipLaunchKernelGGL(k.part, dim3(p.wgs), dim3(k.part_threads), k.part_lds, stream, a);
   PVLM_LAUNCHED();
   if (mass) {
-    hipLaunchKernelGGL(k.mass, grid, dim3(k.threads), 0, stream, a);
+    PVLM_HIP(allow_dynamic_lds(reinterpret_cast<const void*>(k.mass), k.mass_lds));
+    hipLaunchKernelGGL(k.mass, dim3(p.wgs), dim3(k.mass_threads), k.mass_lds, stream, a);
     PVLM_LAUNCHED();
   }
-  const int combine_wgs = (int)(((int64_t)B * Hkv * p.R + kFinWaves - 1) / kFinWaves);
-  hipLaunchKernelGGL(k.finish, dim3(a.mass_wgs + combine_wgs), dim3(kFinThreads), 0, stream, a);
+  // a wave joins 16 records (8 at D = 64: 32) in one round of loads
+  const bool wide = p.recs * kQTokenWaves > (size_t)B * a.HR * 2 * 16;
+  const int per_wg = wide ? 1 : kFinWaves, row_count = B * Hkv * p.R;
+  hipLaunchKernelGGL(k.finish[wide], dim3(a.mass_wgs + (row_count + per_wg - 1) / per_wg), dim3(kFinThreads), 0, stream,
+                     a);
   PVLM_LAUNCHED();
   return PVLM_OK;
 }

@@ -1,5 +1,5 @@
 // Launch plan of verify attention over an 8-bit cache: how its row tiles and
-// tokens are split over workgroups, and where the workspace's areas lie.  Plain
+// tokens are spread over workgroups, and where the workspace's areas lie.  Plain
 // C++, so that the plan can be run over all sizes without a GPU.
 #pragma once
 
@@ -7,32 +7,48 @@
 
 namespace pvlm {
 
-// A stage of the partial and mass kernels: 16 KB of K codes and 16 KB of V codes.
-constexpr int kQStageBytes = 16384;
-constexpr int kQMaxRT = 9;  // 16-row tiles of a workgroup
-inline int q8_stage_rows(int D) { return kQStageBytes / D; }
+// The tokens of every group (sequence, KV head, share of its query rows) are
+// counted in units of 32 (a page holds whole ones), all groups in a row, and
+// every workgroup takes an equal share of that row, whatever the lengths are:
+// a ragged batch keeps no compute unit idle, and a workgroup may end one
+// group and begin the next.  The shares follow from the lengths on the device.
+constexpr int kQUnit = 32;
+constexpr int kQMinUnits = 2;  // least share: one 64-token block
+constexpr int kQMaxRT = 9;     // 16-row tiles of a workgroup
+
+// How a workgroup's waves share its row tiles: TPW tiles a wave (which convert
+// a block's codes once for all of them), RW waves for the tiles, each of them
+// twice, for the two 64-token blocks of a stage.
+struct QWaves {
+  int tpw, rw;
+};
+constexpr QWaves q8_waves(int RT) {
+  return RT <= 3 ? QWaves{RT, 1} : RT == 4 ? QWaves{2, 2} : RT <= 6 ? QWaves{2, 3} : QWaves{3, 3};
+}
+constexpr int kQTokenWaves = 2;
 
 struct QSplit {
-  int G, R;            // query heads of a KV head, and its query rows G * T
-  int RTT, RG, RT;     // their 16-row tiles, the workgroups that share them, and the tiles of one
-  int chunk, splits;   // tokens of a workgroup, and the chunks of the longest sequence
-  size_t off_mpart, off_stats, off_opart, bytes;
+  int G, R;         // query heads of a KV head, and its query rows G * T
+  int RTT, RG, RT;  // their 16-row tiles, the workgroups that share them, and the tiles of one
+  int wgs;          // workgroups of the partial and mass kernels
+  size_t recs;      // partial results of RT tiles: group x of workgroup w is number x + w
+  size_t off_mpart, off_stats, off_zt, off_opart, bytes;
 };
 
 inline pvlm_status check_verify_q8(int B, int T, int Hq, int Hkv, int D, int64_t n_cap, int64_t max_ctx) {
   const pvlm_status st = check_verify(PVLM_BF16, B, T, Hq, Hkv, D, n_cap, max_ctx);
   if (st != PVLM_OK) return st;
   if (n_cap % 32 != 0) return PVLM_ERR_SHAPE;
-  // launches of fewer than 2^32 work-items: at most 704 for each 16-row tile
-  // and 64 for each row
-  return (int64_t)B * Hq * T > ((int64_t)1 << 22) ? PVLM_ERR_SHAPE : PVLM_OK;
+  // the finish kernel has 64 work-items for each row, in one launch of fewer than 2^32
+  if ((int64_t)B * Hq * T > ((int64_t)1 << 22)) return PVLM_ERR_SHAPE;
+  // units are counted in 32 bits (at most 5 workgroups share 40 tiles)
+  const int64_t units = (max_ctx + T + kQUnit - 1) / kQUnit;
+  return (int64_t)B * Hkv * 5 * units > INT32_MAX - 65536 ? PVLM_ERR_SHAPE : PVLM_OK;
 }
 
-// The plan for arguments that check_verify_q8 takes, on `cus` compute units.  A
-// workgroup's ring takes most of a unit's LDS, so one of them runs on each; the
-// tokens of a KV head are cut into as many chunks of whole stages as its share
-// of the units.  Fewer units never make more chunks, so the bytes planned for
-// the whole device are enough under every budget.
+// The plan for arguments that check_verify_q8 takes, on `cus` compute units (a
+// workgroup's ring takes most of a unit's LDS).  It grows with `cus`, so the
+// bytes planned for the whole device are enough under every budget.
 inline void split_verify_q8(int B, int T, int Hq, int Hkv, int D, int64_t n_cap, int64_t max_ctx, int cus,
                             QSplit* p) {
   p->G = Hq / Hkv;
@@ -40,17 +56,17 @@ inline void split_verify_q8(int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
   p->RTT = (p->R + 15) / 16;
   p->RG = (p->RTT + kQMaxRT - 1) / kQMaxRT;
   p->RT = (p->RTT + p->RG - 1) / p->RG;
-  const int64_t groups = (int64_t)B * Hkv * p->RG, rows = q8_stage_rows(D);
-  const int64_t stages = (max_ctx + T + rows - 1) / rows;
-  const int64_t most = cus > groups ? cus / groups : 1;
-  const int64_t per = (stages + most - 1) / most;
-  p->chunk = (int)(per * rows);
-  p->splits = (int)((stages + per - 1) / per);
-  const size_t tiles = (size_t)B * Hkv * p->RTT;
+  const int64_t groups = (int64_t)B * Hkv * p->RG;
+  const int64_t units = groups * ((max_ctx + T + kQUnit - 1) / kQUnit);
+  const int64_t shares = (units + kQMinUnits - 1) / kQMinUnits;
+  p->wgs = (int)(shares < cus ? shares : cus);
+  p->recs = (size_t)(groups + p->wgs);
+  const size_t rows = p->recs * p->RT * kQTokenWaves * 16;
   p->off_mpart = kSyncRegion;  // (the region at the start is other calls')
-  p->off_stats = align_up(p->off_mpart + 4 * (size_t)groups * n_cap, 256);
-  p->off_opart = align_up(p->off_stats + 128 * tiles * p->splits, 256);
-  p->bytes = align_up(p->off_opart + 64 * tiles * p->splits * D, 256);
+  p->off_stats = align_up(p->off_mpart + 4 * (size_t)groups * q8_waves(p->RT).rw * n_cap, 256);
+  p->off_zt = align_up(p->off_stats + 8 * rows, 256);
+  p->off_opart = align_up(p->off_zt + 4 * rows, 256);
+  p->bytes = align_up(p->off_opart + 4 * rows * D, 256);
 }
 
 }  // namespace pvlm

@@ -128,7 +128,7 @@ struct Piece {
   int before, per;       // units of the sequences ahead of b; of a share
   __device__ __forceinline__ void set(const QArgs& a) {
     const int N = ctx + a.T, u = c0 / kQUnit + left;
-    c1 = u > N / kQUnit ? N : u * kQUnit;
+    c1 = __builtin_amdgcn_readfirstlane(u > N / kQUnit ? N : u * kQUnit);
   }
   // false where the share is empty
   __device__ __forceinline__ bool first(const QArgs& a) {
@@ -142,7 +142,7 @@ struct Piece {
     const int hr = __builtin_amdgcn_readfirstlane(off / u);
     g = __builtin_amdgcn_readfirstlane(hr / a.RG);
     rg = hr - g * a.RG;
-    c0 = (off - hr * u) * kQUnit;
+    c0 = __builtin_amdgcn_readfirstlane((off - hr * u) * kQUnit);
     set(a);
     return true;
   }
@@ -156,7 +156,7 @@ struct Piece {
         g = 0;
         before += units_of(a, ctx);
         if (++b == a.B) return false;
-        ctx = clamp_ctx(a, uniform_load(a.ctx_len, b));
+        ctx = __builtin_amdgcn_readfirstlane(clamp_ctx(a, uniform_load(a.ctx_len, b)));
       }
     }
     c0 = 0;
@@ -595,10 +595,9 @@ struct PartWave {
     bool grow = false;
 #pragma unroll
     for (int x = 0; x < TPW; ++x) {
-      float m = kNegInf;
+      float m = kNegInf;  // (the maximum that passes NaN on: the other one has every operand canonicalised first)
 #pragma unroll
-      for (int tt = 0; tt < 4; ++tt)
-        m = fmaxf(fmaxf(m, fmaxf(S[x][tt][0], S[x][tt][1])), fmaxf(S[x][tt][2], S[x][tt][3]));
+      for (int j = 0; j < 16; ++j) m = __builtin_elementwise_maximum(m, S[x][j / 4][j % 4]);
       mx[x] = rows4_max(m) * a.sl2;
       grow |= mx[x] > ref[x] + kRefSlack;
     }

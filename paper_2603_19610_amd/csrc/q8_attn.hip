@@ -29,8 +29,10 @@ constexpr double kLog2e = 1.4426950408889634;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNegInf = -__builtin_huge_valf();
 // A wave's running reference may trail its row maximum by this much (log2
-// domain): O is rescaled only when a block's maximum exceeds it.
-constexpr float kRefSlack = 8.f;
+// domain): O is rescaled only when a block's maximum exceeds it, which a few
+// blocks in a thousand do (with 8, one in six of a workgroup of 45 rows and one
+// in three of 72).  Probabilities then reach 2^24 in a type of bf16's range.
+constexpr float kRefSlack = 24.f;
 constexpr int kFinWaves = kFinThreads / 64;
 
 __device__ __forceinline__ int64_t uniform64(int64_t x) {
@@ -221,6 +223,14 @@ __device__ __forceinline__ void load_query(const QArgs& a, int b, int g, int row
   for (int s = 0; s < D / 32; ++s) q.s[s] = src[s];
 }
 
+// Maximum over the four lanes l, l^16, l^32, l^48; NaN if one is.
+__device__ __forceinline__ float rows4_maximum(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const float y = __builtin_elementwise_maximum(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+  return __builtin_elementwise_maximum(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // Eight codes as bf16, times a power of two.
 __device__ __forceinline__ bf16x8 to_bf16(uint32_t lo, uint32_t hi, float unit) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, unit, false);
@@ -286,16 +296,29 @@ __device__ __forceinline__ VPair read_pair(const char* vb, int r0, int n, int gq
 // O += P' . V over one block; P'[x][ks] holds tokens 16 gq + 8 ks + j.  The next
 // two columns are read while two are multiplied; the barriers keep the compiler
 // from reading all of them at once, for which there are no registers.
-template <int D, int TPW>
-__device__ __forceinline__ void weigh(const char* vb, int r0, int n, int gq, const bf16x8 (&P)[TPW][2], VPair cur,
-                                      floatx4 (&O)[TPW][D / 16]) {
+//
+// MASKED: of the tokens that not every row sees, NaN codes count as 0 (0 times
+// NaN would be NaN for rows that do not see them); mask has 0xff in the bytes
+// of those tokens.  Returns whether there were any: the finish kernel then
+// gives the rows that see them their NaN.
+template <int D, int TPW, bool MASKED>
+__device__ __forceinline__ uint32_t weigh(const char* vb, int r0, int n, int gq, const bf16x8 (&P)[TPW][2], VPair cur,
+                                          const uint32_t (&mask)[4], floatx4 (&O)[TPW][D / 16]) {
+  uint32_t bad = 0;
 #pragma unroll
   for (int pair = 0; pair < D / 32; ++pair) {
     VPair next;
     if (pair + 1 < D / 32) next = read_pair<D>(vb, r0, n, gq, pair + 1);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const bf16x8 b = to_bf16(cur.v[i][0], cur.v[i][1], 1.f);
+      uint32_t v0 = cur.v[i][0], v1 = cur.v[i][1];
+      if constexpr (MASKED) {
+        const uint32_t b0 = nan_codes(v0) & mask[2 * (i & 1)], b1 = nan_codes(v1) & mask[2 * (i & 1) + 1];
+        bad |= b0 | b1;
+        v0 &= ~(b0 | (b0 - (b0 >> 7)));
+        v1 &= ~(b1 | (b1 - (b1 >> 7)));
+      }
+      const bf16x8 b = to_bf16(v0, v1, 1.f);
       const int jd = 2 * pair + i / 2;
 #pragma unroll
       for (int x = 0; x < TPW; ++x)
@@ -304,45 +327,7 @@ __device__ __forceinline__ void weigh(const char* vb, int r0, int n, int gq, con
     __builtin_amdgcn_sched_barrier(0);
     cur = next;
   }
-}
-// The same for a block in which some rows see less than others: a NaN value
-// (0 times it is NaN) must not reach the rows that do not see it.  NaN codes
-// count as 0 in the product, and a second one, of the rows' visibility with
-// the NaN positions, says which results they belong to.  Bit j of seen[x] is
-// the visibility of token 16 gq + j.
-template <int D, int TPW>
-__device__ __forceinline__ void weigh_masked(const char* vb, int r0, int n, int gq, const bf16x8 (&P)[TPW][2],
-                                             const uint32_t (&seen)[TPW], floatx4 (&O)[TPW][D / 16]) {
-#pragma unroll
-  for (int jd = 0; jd < D / 16; ++jd) {
-    intx2 one[2];
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const intx2 v = read_v<D>(vb, r0 + 16 * gq + 8 * ks, jd, n);
-      const uint32_t b0 = nan_codes(v[0]), b1 = nan_codes(v[1]);
-      // without the NaN bytes, and 0x38 (1.0) in their places
-      const bf16x8 b = to_bf16(v[0] & ~(b0 | (b0 - (b0 >> 7))), v[1] & ~(b1 | (b1 - (b1 >> 7))), 1.f);
-      one[ks] = intx2{(int)((b0 >> 7) * 0x38u), (int)((b1 >> 7) * 0x38u)};
-#pragma unroll
-      for (int x = 0; x < TPW; ++x) O[x][jd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][ks], b, O[x][jd], 0, 0, 0);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    if (!__any(one[0][0] | one[0][1] | one[1][0] | one[1][1])) continue;
-#pragma unroll
-    for (int x = 0; x < TPW; ++x) {
-      floatx4 hit = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        bf16x8 va;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) va[j] = static_cast<__bf16>((seen[x] >> (8 * ks + j)) & 1 ? 1.f : 0.f);
-        hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, to_bf16(one[ks][0], one[ks][1], 1.f), hit, 0, 0, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) O[x][jd][i] = hit[i] > 0.f ? __uint_as_float(0x7fc00000u) : O[x][jd][i];
-    }
-    __builtin_amdgcn_sched_barrier(0);
-  }
+  return bad;
 }
 
 // (maximum, sum) of two sets of scores.  A sum of 0 belongs to one of which the
@@ -355,12 +340,12 @@ __device__ __forceinline__ void join(float& m, float& z, float m2, float z2) {
 // log2-sum-exp of row n of a wave's tiles over a group's records, the lane
 // groups taking them in turn, with many loads in flight (+inf for padding rows:
 // their probabilities are 0).
-template <int RT, int TPW>
+template <int RT, int TPW, int TW>
 __device__ __forceinline__ void tile_lse(const QArgs& a, const Holders& h, int tile0, int tiles, const bool (&real)[TPW],
                                          int n, int gq, float (&lse)[TPW]) {
   constexpr int kU = TPW == 1 ? 8 : 4;  // records of every tile in flight
-  const int cnt = h.count * kQTokenWaves;
-  const float2* st = a.stats + (size_t)h.rec * RT * kQTokenWaves * 16 + n;
+  const int cnt = h.count * TW;
+  const float2* st = a.stats + (size_t)h.rec * RT * TW * 16 + n;
   float M[TPW], Z[TPW];
 #pragma unroll
   for (int x = 0; x < TPW; ++x) M[x] = kNegInf, Z[x] = 0.f;
@@ -369,9 +354,9 @@ __device__ __forceinline__ void tile_lse(const QArgs& a, const Holders& h, int t
 #pragma unroll
     for (int j = 0; j < kU; ++j) {
       const int s = min(s0 + 4 * j, cnt - 1);
-      const float2* r = st + (size_t)(s / kQTokenWaves * RT * kQTokenWaves + s % kQTokenWaves) * 16;
+      const float2* r = st + (size_t)(s / TW * RT * TW + s % TW) * 16;
 #pragma unroll
-      for (int x = 0; x < TPW; ++x) v[j][x] = r[min(tile0 + x, tiles - 1) * kQTokenWaves * 16];
+      for (int x = 0; x < TPW; ++x) v[j][x] = r[min(tile0 + x, tiles - 1) * TW * 16];
     }
 #pragma unroll
     for (int x = 0; x < TPW; ++x) {
@@ -449,14 +434,14 @@ __device__ __forceinline__ void wait_stage(int stages) {
 
 // The row index (in rows of codes) of the unit that token t opens.  A page entry
 // outside the pool is flagged and clamped into it.
-__device__ __forceinline__ int64_t unit_row(const QArgs& a, const Piece& p, int t) {
-  if (!a.c.table) return ((int64_t)p.b * a.Hkv + p.g) * a.c.n_cap + t;
-  int pg = uniform_load(a.c.table, (int64_t)p.b * a.c.max_pages + (t >> a.c.shift));
+__device__ __forceinline__ int64_t unit_row(const QArgs& a, int b, int g, int t) {
+  if (!a.c.table) return ((int64_t)b * a.Hkv + g) * a.c.n_cap + t;
+  int pg = uniform_load(a.c.table, (int64_t)b * a.c.max_pages + (t >> a.c.shift));
   if (pg < 0 || pg >= a.c.n_pages) {
     dev_flag(a.status, PVLM_DEV_RANGE);
     pg = pg < 0 ? 0 : (int)(a.c.n_pages - 1);
   }
-  return (((int64_t)pg * a.Hkv + p.g) << a.c.shift) + (t & ((1 << a.c.shift) - 1));
+  return (((int64_t)pg * a.Hkv + g) << a.c.shift) + (t & ((1 << a.c.shift) - 1));
 }
 
 // One side (K or V) of the stage at token t0 into LDS.  Rows past the piece repeat its last one;
@@ -471,7 +456,7 @@ __device__ __forceinline__ void issue_stage(const QArgs& a, const Piece& p, int 
   const int last = p.c1 - 1;
   int64_t row[4];
 #pragma unroll
-  for (int u = 0; u < 4; ++u) row[u] = unit_row(a, p, min(t0 + 32 * u, last & ~31));
+  for (int u = 0; u < 4; ++u) row[u] = unit_row(a, p.b, p.g, min(t0 + 32 * u, last & ~31));
   const bool whole = t0 + R_::ST <= p.c1;
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
@@ -534,9 +519,9 @@ __device__ __forceinline__ void load_share(const QArgs& a, Piece p, char* ring) 
 
 template <int RT>
 struct Waves {
-  static constexpr int TPW = q8_waves(RT).tpw, RW = q8_waves(RT).rw;
-  static constexpr int kCompute = RW * kQTokenWaves;
-  static constexpr int per_eu(int loaders) { return (kCompute + loaders + 3) / 4; }
+  static constexpr int TPW = q8_waves(RT).tpw, RW = q8_waves(RT).rw, TW = q8_waves(RT).tw;
+  static constexpr int kCompute = RW * TW, NB = 2 / TW;  // computing waves, blocks of a stage for one of them
+  static_assert(kCompute + 2 <= 8, "two waves per SIMD: 256 registers each");
 };
 
 // -------------------------------------------------------- partial kernel --
@@ -551,10 +536,14 @@ struct PartWave {
   static constexpr int DPL = D / 16;
   Query<D> q[TPW];
   int lim[TPW];  // last token that the lane's row sees
+  int ctx;       // last token that every row sees
   float ref[TPW], z[TPW];
   floatx4 O[TPW][DPL], zt[TPW];
+  uint32_t bad;  // a NaN value that not every row sees
 
   __device__ __forceinline__ void begin(const QArgs& a, const Piece& p, int tile0, int tiles, int n, int gq) {
+    ctx = p.ctx;
+    bad = 0;
 #pragma unroll
     for (int x = 0; x < TPW; ++x) {
       const int row = (tile0 + x) * 16 + n;
@@ -578,18 +567,12 @@ struct PartWave {
     const uint32_t ve[4] = {ve4.x, ve4.y, ve4.z, ve4.w};
     floatx4 S[TPW][4];
     scores<D, TPW>(kb, ke, r0, n, gq, q, S);
-    uint32_t seen[TPW];
-    if constexpr (TAIL) {
+    if constexpr (TAIL) {  // the lane's token j is visible iff j <= lim - tb - 16 gq
 #pragma unroll
-      for (int x = 0; x < TPW; ++x) {
-        const int o = lim[x] - tb - 16 * gq;  // the lane's token j is visible iff j <= o
-        seen[x] = o < 0 ? 0u : o >= 15 ? 0xffffu : (2u << o) - 1u;
+      for (int x = 0; x < TPW; ++x)
 #pragma unroll
-        for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (!((seen[x] >> (4 * i + tt)) & 1)) S[x][tt][i] = kNegInf;
-      }
+        for (int j = 0; j < 16; ++j)
+          if (j > lim[x] - tb - 16 * gq) S[x][j % 4][j / 4] = kNegInf;
     }
     float mx[TPW];
     bool grow = false;
@@ -598,7 +581,7 @@ struct PartWave {
       float m = kNegInf;  // (the maximum that passes NaN on: the other one has every operand canonicalised first)
 #pragma unroll
       for (int j = 0; j < 16; ++j) m = __builtin_elementwise_maximum(m, S[x][j / 4][j % 4]);
-      mx[x] = rows4_max(m) * a.sl2;
+      mx[x] = rows4_maximum(m) * a.sl2;
       grow |= mx[x] > ref[x] + kRefSlack;
     }
     if (__any(grow)) {  // the first block, and seldom after it
@@ -632,24 +615,33 @@ struct PartWave {
         pz[j / 8][j % 8] = static_cast<__bf16>(e);
         float y = e * q8_unit((ve[j / 4] >> (8 * (j % 4))) & 0xffu);
         if constexpr (TAIL)
-          if (!((seen[x] >> j) & 1)) y = 0.f;  // (an unwritten row's exponent may be anything)
+          if (j > lim[x] - tb - 16 * gq) y = 0.f;  // (an unwritten row's exponent may be anything)
         pv[x][j / 8][j % 8] = static_cast<__bf16>(y);
       }
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) zt[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pz[ks], ones, zt[x], 0, 0, 0);
     }
-    if constexpr (TAIL) weigh_masked<D, TPW>(vb, r0, n, gq, pv, seen, O);
-    else weigh<D, TPW>(vb, r0, n, gq, pv, v0, O);
+    uint32_t mask[4] = {0u, 0u, 0u, 0u};
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int o = ctx - tb - 16 * gq - 4 * k;  // tokens 4 k + j, j <= o, are seen by every row
+        mask[k] = o >= 3 ? 0u : o < 0 ? ~0u : ~0u << (8 * (o + 1));
+      }
+    }
+    bad |= weigh<D, TPW, TAIL>(vb, r0, n, gq, pv, v0, mask, O);
   }
 
-  __device__ __forceinline__ void end(const QArgs& a, size_t rec0, int tile0, int tiles, int n, int gq) {
+  __device__ __forceinline__ void end(const QArgs& a, size_t rec0, int tw_count, int tile0, int tiles, int n, int gq) {
+    const bool nan = __any(bad);
 #pragma unroll
     for (int x = 0; x < TPW; ++x) {
       if (x >= tiles) break;
-      const size_t rec = (rec0 + x * kQTokenWaves) * 16;
+      const size_t rec = (rec0 + x * tw_count) * 16;
       const float zz = rows4_sum(z[x]);
       if (gq == 0) a.stats[rec + n] = make_float2(ref[x], zz);
-      if (n == 0) *reinterpret_cast<floatx4*>(a.zt + rec + 4 * gq) = zt[x];
+      // (a negative sum: the rows' values hold a NaN that not every row sees)
+      if (n == 0) *reinterpret_cast<floatx4*>(a.zt + rec + 4 * gq) = nan ? -zt[x] : zt[x];
       // position DPL n + jd of a stored row holds column 16 jd + n
       float* op = a.opart + rec * D;
 #pragma unroll
@@ -665,11 +657,11 @@ struct PartWave {
 
 template <int D, int RT>
 __global__ void __launch_bounds__(((Waves<RT>::kCompute + 2) * 64))
-__attribute__((amdgpu_waves_per_eu(Waves<RT>::per_eu(2), Waves<RT>::per_eu(2)))) q8_part_kernel(QArgs a) {
+__attribute__((amdgpu_waves_per_eu(2, 2))) q8_part_kernel(QArgs a) {
   typedef Waves<RT> W_;
   typedef Ring<D> R_;
   typedef PartRing<D> P_;
-  constexpr int TPW = W_::TPW;
+  constexpr int TPW = W_::TPW, TW = W_::TW;
   extern __shared__ __align__(1024) char s_ring[];  // [slot][K, V][codes, exponents]
 
   Piece p;
@@ -687,26 +679,44 @@ __attribute__((amdgpu_waves_per_eu(Waves<RT>::per_eu(2), Waves<RT>::per_eu(2))))
     return;
   }
   const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-  const int tw = w % kQTokenWaves, t_first = w / kQTokenWaves * TPW;  // its blocks, and its first tile
+  const int tw = w % TW, t_first = w / TW * TPW;  // its first block, and its first tile
   int slot = 0;
   do {
     const int tiles = min(RT, a.RTT - p.rg * RT) - t_first;  // of the wave; further ones are idle
     PartWave<D, TPW> v;
     v.begin(a, p, p.rg * RT + t_first, tiles, n, gq);
-    // stages before the first of which some row does not see all
-    const int vis_all = min(p.c1 - 1, p.ctx);
-    const char* base = s_ring;
-    int t0 = p.c0;
-    for (; t0 < p.c1; t0 += R_::ST) {
+    // the wave's stages whose blocks every row sees whole, then the others (two
+    // loops with their test at the end: joined, or with the test ahead, the
+    // compiler copies all of O in every round)
+    const int nst = __builtin_amdgcn_readfirstlane((p.c1 - p.c0 + R_::ST - 1) / R_::ST);
+    const int last = 64 * (W_::NB - 1 + tw) + 63;  // of the wave's tokens in a stage
+    const int whole =
+        __builtin_amdgcn_readfirstlane(tiles <= 0 ? 0 : (min(p.c1 - 1, p.ctx) - last - p.c0 + R_::ST) / R_::ST);
+    auto stage = [&]() {
       lds_sync();
-      base = s_ring + slot * P_::kStride;
+      const char* base = s_ring + slot * P_::kStride;
       slot = slot + 1 == P_::kSlots ? 0 : slot + 1;
-      const int tb = t0 + 64 * tw;
-      if (tb >= p.c1 || tiles <= 0) continue;
-      if (tb + 63 <= vis_all) v.template block<false>(a, base, tb, 64 * tw, n, gq);
-      else v.template block<true>(a, base, tb, 64 * tw, n, gq);
+      return base;
+    };
+    int s = 0;
+    if (whole > 0) {
+      do {
+        const char* base = stage();
+#pragma unroll
+        for (int x = 0; x < W_::NB; ++x) v.template block<false>(a, base, 0, 64 * (x + tw), n, gq);
+      } while (++s < whole);
     }
-    v.end(a, ((size_t)(p.group(a) + blockIdx.x) * RT + t_first) * kQTokenWaves + tw, p.rg * RT + t_first, tiles, n, gq);
+    if (s < nst) {
+      do {
+        const char* base = stage();
+        if (tiles > 0)
+          for (int x = 0; x < W_::NB; ++x) {
+            const int r0 = 64 * (x + tw), tb = p.c0 + s * R_::ST + r0;
+            if (tb < p.c1) v.template block<true>(a, base, tb, r0, n, gq);
+          }
+      } while (++s < nst);
+    }
+    v.end(a, ((size_t)(p.group(a) + blockIdx.x) * RT + t_first) * TW + tw, TW, p.rg * RT + t_first, tiles, n, gq);
   } while (p.next(a));
 }
 
@@ -719,11 +729,11 @@ struct MassRing {
 
 template <int D, int RT>
 __global__ void __launch_bounds__(((Waves<RT>::kCompute + 1) * 64))
-__attribute__((amdgpu_waves_per_eu(Waves<RT>::per_eu(1), Waves<RT>::per_eu(1)))) q8_mass_kernel(QArgs a) {
+__attribute__((amdgpu_waves_per_eu(2, 2))) q8_mass_kernel(QArgs a) {
   typedef Waves<RT> W_;
   typedef Ring<D> R_;
   typedef MassRing<D> P_;
-  constexpr int TPW = W_::TPW;
+  constexpr int TPW = W_::TPW, TW = W_::TW;
   extern __shared__ __align__(1024) char s_ring[];
 
   Piece p;
@@ -734,7 +744,7 @@ __attribute__((amdgpu_waves_per_eu(Waves<RT>::per_eu(1), Waves<RT>::per_eu(1))))
     return;
   }
   const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-  const int tw = w % kQTokenWaves, rw = w / kQTokenWaves, t_first = rw * TPW;
+  const int tw = w % TW, rw = w / TW, t_first = rw * TPW;
   int slot = 0;
   do {
     const int tiles = min(RT, a.RTT - p.rg * RT);
@@ -750,33 +760,39 @@ __attribute__((amdgpu_waves_per_eu(Waves<RT>::per_eu(1), Waves<RT>::per_eu(1))))
       load_query<D>(a, p.b, p.g, row, gq, q[x]);
       lim[x] = real[x] ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
     }
-    tile_lse<RT, TPW>(a, h, t_first, tiles, real, n, gq, lse);
+    tile_lse<RT, TPW, TW>(a, h, t_first, tiles, real, n, gq, lse);
     const int vis_all = min(p.c1 - 1, p.ctx);
     float* mp = a.mpart + ((size_t)p.group(a) * W_::RW + rw) * a.c.n_cap;
     for (int t0 = p.c0; t0 < p.c1; t0 += R_::ST) {
       lds_sync();
       const char* kb = s_ring + slot * P_::kStride;
       slot = slot + 1 == P_::kSlots ? 0 : slot + 1;
-      const int r0 = 64 * tw, tb = t0 + r0;
-      if (tb >= p.c1) continue;
-      const uint32_t ke = *reinterpret_cast<const uint32_t*>(kb + R_::KB + r0 + 4 * n);
-      floatx4 S[TPW][4];
-      scores<D, TPW>(kb, ke, r0, n, gq, q, S);
-      const bool tail = tb + 63 > vis_all || t_first + TPW > tiles;
-      float sum[16];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) sum[j] = 0.f;
+      for (int b = 0; b < W_::NB; ++b) {
+        const int r0 = 64 * (b + tw), tb = t0 + r0;
+        if (__builtin_amdgcn_readfirstlane(tb - p.c1) >= 0) break;
+        const uint32_t ke = *reinterpret_cast<const uint32_t*>(kb + R_::KB + r0 + 4 * n);
+        floatx4 S[TPW][4];
+        scores<D, TPW>(kb, ke, r0, n, gq, q, S);
+        if (__builtin_amdgcn_readfirstlane(tb + 63 - vis_all) > 0) {
 #pragma unroll
-      for (int x = 0; x < TPW; ++x) {
-        const int o = lim[x] - tb - 16 * gq;
+          for (int x = 0; x < TPW; ++x)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const float e = fast_exp2(fmaf(S[x][j % 4][j / 4], a.sl2, -lse[x]));
-          sum[j] += !tail || j <= o ? e : 0.f;
+            for (int j = 0; j < 16; ++j)
+              if (j > lim[x] - tb - 16 * gq) S[x][j % 4][j / 4] = kNegInf;
         }
+        // (NaN scores of padding rows, whose q is a real row's, make a token's sum NaN that the real row makes so)
+        float sum[16];
+#pragma unroll
+        for (int x = 0; x < TPW; ++x)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const float e = fast_exp2(fmaf(S[x][j % 4][j / 4], a.sl2, -lse[x]));
+            sum[j] = x ? sum[j] + e : e;
+          }
+        const float m = row_sums(sum, lane);
+        if (tb + lane < p.c1) mp[tb + lane] = m;
       }
-      const float m = row_sums(sum, lane);
-      if (tb + lane < p.c1) mp[tb + lane] = m;
     }
   } while (p.next(a));
 }
@@ -794,8 +810,10 @@ __attribute__((amdgpu_waves_per_eu(Waves<RT>::per_eu(1), Waves<RT>::per_eu(1))))
 struct RowSum {
   float m, z, zt;
   floatx4 o;
+  bool nan;  // a record's values hold a NaN that not every row sees
 };
-__device__ __forceinline__ void join(RowSum& a, float m, float z, float zt, floatx4 o) {
+__device__ __forceinline__ void join(RowSum& a, float m, float z, float zt, floatx4 o, bool nan) {
+  a.nan |= nan;
   const float M = fmaxf(a.m, m), r = M == kNegInf ? 0.f : M;
   const float f = a.z != 0.f ? fast_exp2(a.m - r) : 0.f, g = z != 0.f ? fast_exp2(m - r) : 0.f;
   a.z = (a.z != 0.f ? a.z * f : 0.f) + (z != 0.f ? z * g : 0.f);
@@ -806,18 +824,19 @@ __device__ __forceinline__ void join(RowSum& a, float m, float z, float zt, floa
 
 template <int D, int RT, int WPR>
 __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_row)[D / 4]) {
-  constexpr int LPR = D / 4, SG = 64 / LPR, TW = kQTokenWaves, kU = 8;
+  constexpr int LPR = D / 4, SG = 64 / LPR, TW = Waves<RT>::TW, kU = 8;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane % LPR;
   const int id = wg * (kFinWaves / WPR) + w / WPR;  // (fewer than 2^22 rows)
   const bool row_here = id < a.B * a.Hkv * a.R;
-  RowSum t{kNegInf, 0.f, 0.f, floatx4{0.f, 0.f, 0.f, 0.f}};
-  int b = 0, g = 0, row = 0;
+  RowSum t{kNegInf, 0.f, 0.f, floatx4{0.f, 0.f, 0.f, 0.f}, false};
+  int b = 0, g = 0, row = 0, ctx = 0;
   if (row_here) {
     const int bg = __builtin_amdgcn_readfirstlane(id / a.R);
     row = id - bg * a.R;
     b = bg / a.Hkv;
     g = bg - b * a.Hkv;
     const Shares s_ = find<false>(a, 0, b);
+    ctx = s_.ctx;
     const int rg = row / (16 * RT), tile = row / 16 - rg * RT;
     const Holders h = holders(a, s_.per, s_.before, b, g * a.RG + rg, s_.ctx);
     const size_t rec = ((size_t)h.rec * RT + tile) * TW * 16 + row % 16;
@@ -847,7 +866,8 @@ __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_
         if (s0 + j * sets < cnt && v[j].y != 0.f) {  // (0: nothing that the row sees)
           const float e = fast_exp2(v[j].x - r);
           t.z = fmaf(v[j].y, e, t.z);
-          t.zt = fmaf(zt[j], e, t.zt);
+          t.zt = fmaf(fabsf(zt[j]), e, t.zt);
+          t.nan |= zt[j] < 0.f;
           t.o = t.o + o[j] * e;
         }
     }
@@ -856,7 +876,7 @@ __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_
       floatx4 y;
 #pragma unroll
       for (int k = 0; k < 4; ++k) y[k] = __shfl_xor(t.o[k], o, 64);
-      join(t, __shfl_xor(t.m, o, 64), __shfl_xor(t.z, o, 64), __shfl_xor(t.zt, o, 64), y);
+      join(t, __shfl_xor(t.m, o, 64), __shfl_xor(t.z, o, 64), __shfl_xor(t.zt, o, 64), y, __shfl_xor(t.nan, o, 64));
     }
   }
   if constexpr (WPR > 1) {
@@ -865,12 +885,22 @@ __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_
     if (w % WPR) return;
     for (int k = 1; k < WPR; ++k) {
       const RowSum y = s_row[w + k][col];
-      join(t, y.m, y.z, y.zt, y.o);
+      join(t, y.m, y.z, y.zt, y.o, y.nan);
     }
   }
   if (!row_here || lane >= LPR) return;
   const int tt = row_t(a, row), head = g * a.G + row - tt * a.G;
   constexpr int DPL = D / 16;
+  if (t.nan) {  // the values past the context that the row sees, whose NaN codes counted as 0
+    for (int j = ctx + 1; j <= ctx + tt; ++j) {
+      const int64_t r = unit_row(a, b, g, j & ~31) + (j & 31);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int c = 4 * col + k;
+        if ((a.c.vc[r * D + 16 * (c % DPL) + c / DPL] & 0x7f) == 0x7f) t.o[k] = __uint_as_float(0x7fc00000u);
+      }
+    }
+  }
   const float inv = 1.f / t.zt;
   uint16_t* o = a.out + (((size_t)b * a.T + tt) * a.Hq + head) * D;
 #pragma unroll
@@ -997,7 +1027,7 @@ pvlm_status verify_q8_run(int B, int T, int Hq, int Hkv, int D, int64_t max_ctx,
     PVLM_LAUNCHED();
   }
   // a wave joins 16 records (8 at D = 64: 32) in one round of loads
-  const bool wide = p.recs * kQTokenWaves > (size_t)B * a.HR * 2 * 16;
+  const bool wide = p.recs * q8_waves(p.RT).tw > (size_t)B * a.HR * 2 * 16;
   const int per_wg = wide ? 1 : kFinWaves, row_count = B * Hkv * p.R;
   hipLaunchKernelGGL(k.finish[wide], dim3(a.mass_wgs + (row_count + per_wg - 1) / per_wg), dim3(kFinThreads), 0, stream,
                      a);

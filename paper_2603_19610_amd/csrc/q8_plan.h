@@ -16,16 +16,14 @@ constexpr int kQUnit = 32;
 constexpr int kQMinUnits = 2;  // least share: one 64-token block
 constexpr int kQMaxRT = 9;     // 16-row tiles of a workgroup
 
-// How a workgroup's waves share its row tiles: TPW tiles a wave (which convert
-// a block's codes once for all of them), RW waves for the tiles, each of them
-// twice, for the two 64-token blocks of a stage.
+// How a workgroup's waves share its row tiles and a stage's two blocks of 64
+// tokens: TPW tiles a wave (which converts a block's codes once for all of
+// them; a third tile has no registers), RW waves for the tiles, TW of each for
+// the blocks.  Two waves a SIMD at most, the two loading waves among them.
 struct QWaves {
-  int tpw, rw;
+  int tpw, rw, tw;
 };
-constexpr QWaves q8_waves(int RT) {
-  return RT <= 3 ? QWaves{RT, 1} : RT == 4 ? QWaves{2, 2} : RT <= 6 ? QWaves{2, 3} : QWaves{3, 3};
-}
-constexpr int kQTokenWaves = 2;
+constexpr QWaves q8_waves(int RT) { return {RT == 1 ? 1 : 2, (RT + 1) / 2, RT <= 6 ? 2 : 1}; }
 
 struct QSplit {
   int G, R;         // query heads of a KV head, and its query rows G * T
@@ -61,7 +59,7 @@ inline void split_verify_q8(int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
   const int64_t shares = (units + kQMinUnits - 1) / kQMinUnits;
   p->wgs = (int)(shares < cus ? shares : cus);
   p->recs = (size_t)(groups + p->wgs);
-  const size_t rows = p->recs * p->RT * kQTokenWaves * 16;
+  const size_t rows = p->recs * p->RT * q8_waves(p->RT).tw * 16;
   p->off_mpart = kSyncRegion;  // (the region at the start is other calls')
   p->off_stats = align_up(p->off_mpart + 4 * (size_t)groups * q8_waves(p->RT).rw * n_cap, 256);
   p->off_zt = align_up(p->off_stats + 8 * rows, 256);

@@ -73,52 +73,56 @@ struct Shares {
   int before;  // units (of one group each) of the sequences ahead of b
   int b, ctx;
 };
-// The sequence that holds unit `at` of share wg (b = B: none), or sequence `seq`.
+// Inclusive sum over the wave's lanes.
+__device__ __forceinline__ int wave_scan(int x) {
+#define PVLM_SCAN(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, false)
+  PVLM_SCAN(0x111, 0xf);  // row_shr:1, 2, 4, 8: within 16 lanes
+  PVLM_SCAN(0x112, 0xf);
+  PVLM_SCAN(0x114, 0xf);
+  PVLM_SCAN(0x118, 0xf);
+  PVLM_SCAN(0x142, 0xa);  // lane 15 of a row to the next: rows 1 and 3
+  PVLM_SCAN(0x143, 0xc);  // lane 31 to rows 2 and 3
+#undef PVLM_SCAN
+  return x;
+}
+
+// The sequence that holds the first unit of share wg (b = B: none), or sequence `seq`.
 template <bool FIND_UNIT>
 __device__ __forceinline__ Shares find(const QArgs& a, int wg, int seq) {
   const int lane = threadIdx.x & 63;
-  int total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    int u = b0 + lane < a.B ? units_of(a, clamp_ctx(a, a.ctx_len[b0 + lane])) : 0;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) u += __shfl_xor(u, o, 64);
-    total += u;
-  }
   Shares s;
-  s.per = (total * a.HR + a.wgs - 1) / a.wgs;
-  if (s.per < kQMinUnits) s.per = kQMinUnits;
+  int total = 0, ctx = 0, u = 0, upto = 0;
+  auto load = [&](int b0) {
+    const bool here = b0 + lane < a.B;
+    ctx = here ? clamp_ctx(a, a.ctx_len[b0 + lane]) : 0;
+    u = here ? units_of(a, ctx) : 0;
+    upto = wave_scan(u);
+  };
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    load(b0);
+    total += __builtin_amdgcn_readlane(upto, 63);
+  }
+  s.per = max((total * a.HR + a.wgs - 1) / a.wgs, kQMinUnits);
   s.before = 0;
   s.b = a.B;
   s.ctx = 0;
+  // (wg * per stays within 32 bits: per exceeds total / wgs by less than one, or is the least share of few units)
+  const int at = wg * s.per;
   for (int b0 = 0; b0 < a.B; b0 += 64) {
-    const int ctx = b0 + lane < a.B ? clamp_ctx(a, a.ctx_len[b0 + lane]) : 0;
-    const int u = b0 + lane < a.B ? units_of(a, ctx) : 0;
-    int upto = u;  // inclusive
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += v;
-    }
-    int hit;
+    if (a.B > 64) load(b0);
+    int hit = seq - b0;
     if constexpr (FIND_UNIT) {
-      // (wg * per stays within 32 bits: per exceeds total / wgs by less than one, or is the least share of few units)
-      const uint64_t m = __ballot(b0 + lane < a.B && (s.before + upto) * a.HR > wg * s.per);
+      const uint64_t m = __ballot(b0 + lane < a.B && (s.before + upto) * a.HR > at);
       hit = m ? __builtin_ctzll(m) : -1;
-    } else {
-      hit = seq >= b0 && seq < b0 + 64 ? seq - b0 : -1;
     }
-    if (hit >= 0) {
-      s.before += __shfl(upto - u, hit, 64);
+    if (hit >= 0 && hit < 64) {
+      s.before += __builtin_amdgcn_readlane(upto - u, hit);
       s.b = b0 + hit;
-      s.ctx = __shfl(ctx, hit, 64);
+      s.ctx = __builtin_amdgcn_readlane(ctx, hit);
       break;
     }
-    s.before += __shfl(upto, 63, 64);
+    s.before += __builtin_amdgcn_readlane(upto, 63);
   }
-  s.per = __builtin_amdgcn_readfirstlane(s.per);
-  s.before = __builtin_amdgcn_readfirstlane(s.before);
-  s.b = __builtin_amdgcn_readfirstlane(s.b);
-  s.ctx = __builtin_amdgcn_readfirstlane(s.ctx);
   return s;
 }
 
@@ -293,7 +297,7 @@ __device__ __forceinline__ VPair read_pair(const char* vb, int r0, int n, int gq
   return p;
 }
 
-// O += P' . V over one block; P'[x][ks] holds tokens 16 gq + 8 ks + j.  The next
+// O += P' . V over one block; P'[ks] holds tokens 16 gq + 8 ks + j.  The next
 // two columns are read while two are multiplied; the barriers keep the compiler
 // from reading all of them at once, for which there are no registers.
 //
@@ -301,9 +305,9 @@ __device__ __forceinline__ VPair read_pair(const char* vb, int r0, int n, int gq
 // NaN would be NaN for rows that do not see them); mask has 0xff in the bytes
 // of those tokens.  Returns whether there were any: the finish kernel then
 // gives the rows that see them their NaN.
-template <int D, int TPW, bool MASKED>
-__device__ __forceinline__ uint32_t weigh(const char* vb, int r0, int n, int gq, const bf16x8 (&P)[TPW][2], VPair cur,
-                                          const uint32_t (&mask)[4], floatx4 (&O)[TPW][D / 16]) {
+template <int D, bool MASKED>
+__device__ __forceinline__ uint32_t weigh(const char* vb, int r0, int n, int gq, const bf16x8 (&P)[2], VPair cur,
+                                          const uint32_t (&mask)[4], floatx4 (&O)[D / 16]) {
   uint32_t bad = 0;
 #pragma unroll
   for (int pair = 0; pair < D / 32; ++pair) {
@@ -320,9 +324,7 @@ __device__ __forceinline__ uint32_t weigh(const char* vb, int r0, int n, int gq,
       }
       const bf16x8 b = to_bf16(v0, v1, 1.f);
       const int jd = 2 * pair + i / 2;
-#pragma unroll
-      for (int x = 0; x < TPW; ++x)
-        O[x][jd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][i & 1], b, O[x][jd], 0, 0, 0);
+      O[jd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[i & 1], b, O[jd], 0, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
     cur = next;
@@ -340,12 +342,12 @@ __device__ __forceinline__ void join(float& m, float& z, float m2, float z2) {
 // log2-sum-exp of row n of a wave's tiles over a group's records, the lane
 // groups taking them in turn, with many loads in flight (+inf for padding rows:
 // their probabilities are 0).
-template <int RT, int TPW, int TW>
+template <int RT, int TPW>
 __device__ __forceinline__ void tile_lse(const QArgs& a, const Holders& h, int tile0, int tiles, const bool (&real)[TPW],
                                          int n, int gq, float (&lse)[TPW]) {
   constexpr int kU = TPW == 1 ? 8 : 4;  // records of every tile in flight
-  const int cnt = h.count * TW;
-  const float2* st = a.stats + (size_t)h.rec * RT * TW * 16 + n;
+  const int cnt = 2 * h.count;  // (of a tile that one wave has the first of every two)
+  const float2* st = a.stats + (size_t)h.rec * RT * 2 * 16 + n;
   float M[TPW], Z[TPW];
 #pragma unroll
   for (int x = 0; x < TPW; ++x) M[x] = kNegInf, Z[x] = 0.f;
@@ -354,9 +356,12 @@ __device__ __forceinline__ void tile_lse(const QArgs& a, const Holders& h, int t
 #pragma unroll
     for (int j = 0; j < kU; ++j) {
       const int s = min(s0 + 4 * j, cnt - 1);
-      const float2* r = st + (size_t)(s / TW * RT * TW + s % TW) * 16;
+      const float2* r = st + (size_t)(s / 2 * RT * 2 + s % 2) * 16;
 #pragma unroll
-      for (int x = 0; x < TPW; ++x) v[j][x] = r[min(tile0 + x, tiles - 1) * TW * 16];
+      for (int x = 0; x < TPW; ++x) {
+        const int tile = min(tile0 + x, tiles - 1);
+        v[j][x] = tile < q8_full_tiles(RT) && s % 2 ? make_float2(kNegInf, 0.f) : r[tile * 2 * 16];
+      }
     }
 #pragma unroll
     for (int x = 0; x < TPW; ++x) {
@@ -517,44 +522,53 @@ __device__ __forceinline__ void load_share(const QArgs& a, Piece p, char* ring) 
   }
 }
 
-template <int RT>
-struct Waves {
-  static constexpr int TPW = q8_waves(RT).tpw, RW = q8_waves(RT).rw, TW = q8_waves(RT).tw;
-  static constexpr int kCompute = RW * TW, NB = 2 / TW;  // computing waves, blocks of a stage for one of them
-  static_assert(kCompute + 2 <= 8, "two waves per SIMD: 256 registers each");
-};
-
 // -------------------------------------------------------- partial kernel --
 template <int D>
 struct PartRing {
   static constexpr int kSlots = D == 128 ? 4 : 8, kStride = 2 * Ring<D>::kSide, kLds = kSlots * kStride;
 };
 
-// A wave's state: TPW row tiles against the tokens of its blocks.
-template <int D, int TPW>
+// A computing wave's tile and blocks.  Wave w runs on SIMD w mod 4, the loading
+// waves on SIMDs 2 and 3 of three that hold ten others: waves of whole tiles
+// are placed first on those, then on 0 and 1 (RT = 6: 2 + 2 half tiles a SIMD).
+struct Role {
+  int tile, block, blocks;
+};
+template <int RT>
+__device__ __forceinline__ Role role(int w) {
+  constexpr int full = q8_full_tiles(RT);
+  constexpr int order[8] = {2, 3, 0, 1, 6, 7, 4, 5};
+  int ahead = 0;  // waves of whole tiles before w
+#pragma unroll
+  for (int k = 0; k < full; ++k) {
+    if (order[k] == w) return {k, 0, 2};
+    ahead += order[k] < w;
+  }
+  return {full + (w - ahead) / 2, (w - ahead) % 2, 1};
+}
+
+// A wave's state: a row tile against the tokens of its blocks.
+template <int D>
 struct PartWave {
   static constexpr int DPL = D / 16;
-  Query<D> q[TPW];
-  int lim[TPW];  // last token that the lane's row sees
-  int ctx;       // last token that every row sees
-  float ref[TPW], z[TPW];
-  floatx4 O[TPW][DPL], zt[TPW];
+  Query<D> q[1];
+  int lim;  // last token that the lane's row sees
+  int ctx;  // last token that every row sees
+  float ref, z;
+  floatx4 O[DPL], zt;
   uint32_t bad;  // a NaN value that not every row sees
 
-  __device__ __forceinline__ void begin(const QArgs& a, const Piece& p, int tile0, int tiles, int n, int gq) {
+  __device__ __forceinline__ void begin(const QArgs& a, const Piece& p, int tile, int n, int gq) {
     ctx = p.ctx;
     bad = 0;
+    const int row = tile * 16 + n;
+    load_query<D>(a, p.b, p.g, row, gq, q[0]);
+    lim = row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
+    ref = kNegInf;
+    z = 0.f;
+    zt = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int x = 0; x < TPW; ++x) {
-      const int row = (tile0 + x) * 16 + n;
-      load_query<D>(a, p.b, p.g, row, gq, q[x]);
-      lim[x] = x < tiles && row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
-      ref[x] = kNegInf;
-      z[x] = 0.f;
-      zt[x] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int jd = 0; jd < DPL; ++jd) O[x][jd] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int jd = 0; jd < DPL; ++jd) O[jd] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
 
   // The block of tokens tb .. tb + 63, rows r0 .. r0 + 63 of the stage.  TAIL: some row does not see all of them.
@@ -565,62 +579,48 @@ struct PartWave {
     const uint32_t ke = *reinterpret_cast<const uint32_t*>(kb + R_::KB + r0 + 4 * n);
     const uint4 ve4 = *reinterpret_cast<const uint4*>(vb + R_::KB + r0 + 16 * gq);
     const uint32_t ve[4] = {ve4.x, ve4.y, ve4.z, ve4.w};
-    floatx4 S[TPW][4];
-    scores<D, TPW>(kb, ke, r0, n, gq, q, S);
+    floatx4 S1[1][4];
+    scores<D, 1>(kb, ke, r0, n, gq, q, S1);
+    floatx4(&S)[4] = S1[0];
     if constexpr (TAIL) {  // the lane's token j is visible iff j <= lim - tb - 16 gq
 #pragma unroll
-      for (int x = 0; x < TPW; ++x)
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (j > lim[x] - tb - 16 * gq) S[x][j % 4][j / 4] = kNegInf;
+      for (int j = 0; j < 16; ++j)
+        if (j > lim - tb - 16 * gq) S[j % 4][j / 4] = kNegInf;
     }
-    float mx[TPW];
-    bool grow = false;
+    float mx = kNegInf;  // (the maximum that passes NaN on: the other one has every operand canonicalised first)
 #pragma unroll
-    for (int x = 0; x < TPW; ++x) {
-      float m = kNegInf;  // (the maximum that passes NaN on: the other one has every operand canonicalised first)
+    for (int j = 0; j < 16; ++j) mx = __builtin_elementwise_maximum(mx, S[j / 4][j % 4]);
+    mx = rows4_maximum(mx) * a.sl2;
+    if (__any(mx > ref + kRefSlack)) {  // the first block, and seldom after it
+      const float nm = fmaxf(ref, mx);
+      const float al = ref == kNegInf ? 0.f : fast_exp2(ref - nm);
+      z *= al;
+      ref = nm;
+      floatx4 f;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) m = __builtin_elementwise_maximum(m, S[x][j / 4][j % 4]);
-      mx[x] = rows4_maximum(m) * a.sl2;
-      grow |= mx[x] > ref[x] + kRefSlack;
-    }
-    if (__any(grow)) {  // the first block, and seldom after it
+      for (int i = 0; i < 4; ++i) f[i] = __shfl(al, 4 * gq + i, 64);
+      zt = zt * f;
 #pragma unroll
-      for (int x = 0; x < TPW; ++x) {
-        const float nm = fmaxf(ref[x], mx[x]);
-        const float al = ref[x] == kNegInf ? 0.f : fast_exp2(ref[x] - nm);
-        z[x] *= al;
-        ref[x] = nm;
-        floatx4 f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = __shfl(al, 4 * gq + i, 64);
-        zt[x] = zt[x] * f;
-#pragma unroll
-        for (int jd = 0; jd < DPL; ++jd) O[x][jd] = O[x][jd] * f;
-      }
+      for (int jd = 0; jd < DPL; ++jd) O[jd] = O[jd] * f;
     }
     const VPair v0 = read_pair<D>(vb, r0, n, gq, 0);
     bf16x8 ones;
 #pragma unroll
     for (int j = 0; j < 8; ++j) ones[j] = static_cast<__bf16>(1.f);
-    bf16x8 pv[TPW][2];
+    const float r = ref == kNegInf ? 0.f : ref;  // no visible token yet: P = 0
+    bf16x8 pz[2], pv[2];
 #pragma unroll
-    for (int x = 0; x < TPW; ++x) {
-      const float r = ref[x] == kNegInf ? 0.f : ref[x];  // no visible token yet: P = 0
-      bf16x8 pz[2];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const float e = fast_exp2(fmaf(S[x][j % 4][j / 4], a.sl2, -r));
-        z[x] += e;
-        pz[j / 8][j % 8] = static_cast<__bf16>(e);
-        float y = e * q8_unit((ve[j / 4] >> (8 * (j % 4))) & 0xffu);
-        if constexpr (TAIL)
-          if (j > lim[x] - tb - 16 * gq) y = 0.f;  // (an unwritten row's exponent may be anything)
-        pv[x][j / 8][j % 8] = static_cast<__bf16>(y);
-      }
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) zt[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pz[ks], ones, zt[x], 0, 0, 0);
+    for (int j = 0; j < 16; ++j) {
+      const float e = fast_exp2(fmaf(S[j % 4][j / 4], a.sl2, -r));
+      z += e;
+      pz[j / 8][j % 8] = static_cast<__bf16>(e);
+      float y = e * q8_unit((ve[j / 4] >> (8 * (j % 4))) & 0xffu);
+      if constexpr (TAIL)
+        if (j > lim - tb - 16 * gq) y = 0.f;  // (an unwritten row's exponent may be anything)
+      pv[j / 8][j % 8] = static_cast<__bf16>(y);
     }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) zt = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pz[ks], ones, zt, 0, 0, 0);
     uint32_t mask[4] = {0u, 0u, 0u, 0u};
     if constexpr (TAIL) {
 #pragma unroll
@@ -629,39 +629,41 @@ struct PartWave {
         mask[k] = o >= 3 ? 0u : o < 0 ? ~0u : ~0u << (8 * (o + 1));
       }
     }
-    bad |= weigh<D, TPW, TAIL>(vb, r0, n, gq, pv, v0, mask, O);
+    bad |= weigh<D, TAIL>(vb, r0, n, gq, pv, v0, mask, O);
   }
 
-  __device__ __forceinline__ void end(const QArgs& a, size_t rec0, int tw_count, int tile0, int tiles, int n, int gq) {
+  __device__ __forceinline__ void end(const QArgs& a, size_t rec, int tile, int n, int gq) {
     const bool nan = __any(bad);
+    const float zz = rows4_sum(z);
+    rec *= 16;
+    if (gq == 0) a.stats[rec + n] = make_float2(ref, zz);
+    // (a negative sum: the rows' values hold a NaN that not every row sees)
+    if (n == 0) *reinterpret_cast<floatx4*>(a.zt + rec + 4 * gq) = nan ? -zt : zt;
+    // position DPL n + jd of a stored row holds column 16 jd + n
+    float* op = a.opart + rec * D;
 #pragma unroll
-    for (int x = 0; x < TPW; ++x) {
-      if (x >= tiles) break;
-      const size_t rec = (rec0 + x * tw_count) * 16;
-      const float zz = rows4_sum(z[x]);
-      if (gq == 0) a.stats[rec + n] = make_float2(ref[x], zz);
-      // (a negative sum: the rows' values hold a NaN that not every row sees)
-      if (n == 0) *reinterpret_cast<floatx4*>(a.zt + rec + 4 * gq) = nan ? -zt[x] : zt[x];
-      // position DPL n + jd of a stored row holds column 16 jd + n
-      float* op = a.opart + rec * D;
+    for (int i = 0; i < 4; ++i)
+      if (tile * 16 + 4 * gq + i < a.R)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if ((tile0 + x) * 16 + 4 * gq + i < a.R)
-#pragma unroll
-          for (int h = 0; h < DPL / 4; ++h)
-            *reinterpret_cast<float4*>(op + (4 * gq + i) * D + DPL * n + 4 * h) =
-                make_float4(O[x][4 * h][i], O[x][4 * h + 1][i], O[x][4 * h + 2][i], O[x][4 * h + 3][i]);
-    }
+        for (int h = 0; h < DPL / 4; ++h)
+          *reinterpret_cast<float4*>(op + (4 * gq + i) * D + DPL * n + 4 * h) =
+              make_float4(O[4 * h][i], O[4 * h + 1][i], O[4 * h + 2][i], O[4 * h + 3][i]);
   }
 };
 
+template <int RT>
+struct PartShape {
+  static constexpr int kCompute = q8_part_waves(RT), kThreads = (kCompute + 2) * 64;
+  // waves of a SIMD; two at least, so that a wave's registers are all of one kind
+  static constexpr int kPerEu = kCompute <= 6 ? 2 : 3;
+};
+
 template <int D, int RT>
-__global__ void __launch_bounds__(((Waves<RT>::kCompute + 2) * 64))
-__attribute__((amdgpu_waves_per_eu(2, 2))) q8_part_kernel(QArgs a) {
-  typedef Waves<RT> W_;
+__global__ void __launch_bounds__((PartShape<RT>::kThreads))
+__attribute__((amdgpu_waves_per_eu(PartShape<RT>::kPerEu, PartShape<RT>::kPerEu))) q8_part_kernel(QArgs a) {
   typedef Ring<D> R_;
   typedef PartRing<D> P_;
-  constexpr int TPW = W_::TPW, TW = W_::TW;
+  constexpr int kCompute = PartShape<RT>::kCompute;
   extern __shared__ __align__(1024) char s_ring[];  // [slot][K, V][codes, exponents]
 
   Piece p;
@@ -670,28 +672,28 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) q8_part_kernel(QArgs a) {
     for (int b = threadIdx.x; b < a.B; b += 64)
       if (a.ctx_len[b] < 0 || a.ctx_len[b] > a.max_ctx) dev_flag(a.status, PVLM_DEV_RANGE);
   if (!p.first(a)) return;
-  if (w == W_::kCompute) {
+  if (w == kCompute) {
     load_share<D, true, P_::kSlots, P_::kStride>(a, p, s_ring);
     return;
   }
-  if (w == W_::kCompute + 1) {
+  if (w == kCompute + 1) {
     load_share<D, false, P_::kSlots, P_::kStride>(a, p, s_ring + R_::kSide);
     return;
   }
   const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-  const int tw = w % TW, t_first = w / TW * TPW;  // its first block, and its first tile
+  const Role my = role<RT>(w);
   int slot = 0;
   do {
-    const int tiles = min(RT, a.RTT - p.rg * RT) - t_first;  // of the wave; further ones are idle
-    PartWave<D, TPW> v;
-    v.begin(a, p, p.rg * RT + t_first, tiles, n, gq);
+    const int tile = p.rg * RT + my.tile;  // of the KV head
+    const bool live = tile < a.RTT;
+    PartWave<D> v;
+    v.begin(a, p, tile, n, gq);
     // the wave's stages whose blocks every row sees whole, then the others (two
     // loops with their test at the end: joined, or with the test ahead, the
     // compiler copies all of O in every round)
     const int nst = __builtin_amdgcn_readfirstlane((p.c1 - p.c0 + R_::ST - 1) / R_::ST);
-    const int last = 64 * (W_::NB - 1 + tw) + 63;  // of the wave's tokens in a stage
-    const int whole =
-        __builtin_amdgcn_readfirstlane(tiles <= 0 ? 0 : (min(p.c1 - 1, p.ctx) - last - p.c0 + R_::ST) / R_::ST);
+    const int last = 64 * (my.block + my.blocks) - 1;  // of the wave's tokens in a stage
+    const int whole = __builtin_amdgcn_readfirstlane(live ? (min(p.c1 - 1, p.ctx) - last - p.c0 + R_::ST) / R_::ST : 0);
     auto stage = [&]() {
       lds_sync();
       const char* base = s_ring + slot * P_::kStride;
@@ -702,21 +704,24 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) q8_part_kernel(QArgs a) {
     if (whole > 0) {
       do {
         const char* base = stage();
-#pragma unroll
-        for (int x = 0; x < W_::NB; ++x) v.template block<false>(a, base, 0, 64 * (x + tw), n, gq);
+        int x = 0;
+        do v.template block<false>(a, base, 0, 64 * (my.block + x), n, gq);
+        while (++x < my.blocks);
       } while (++s < whole);
     }
     if (s < nst) {
       do {
         const char* base = stage();
-        if (tiles > 0)
-          for (int x = 0; x < W_::NB; ++x) {
-            const int r0 = 64 * (x + tw), tb = p.c0 + s * R_::ST + r0;
+        if (live) {
+          int x = 0;
+          do {
+            const int r0 = 64 * (my.block + x), tb = p.c0 + s * R_::ST + r0;
             if (tb < p.c1) v.template block<true>(a, base, tb, r0, n, gq);
-          }
+          } while (++x < my.blocks);
+        }
       } while (++s < nst);
     }
-    v.end(a, ((size_t)(p.group(a) + blockIdx.x) * RT + t_first) * TW + tw, TW, p.rg * RT + t_first, tiles, n, gq);
+    if (live) v.end(a, ((size_t)(p.group(a) + blockIdx.x) * RT + my.tile) * 2 + my.block, tile, n, gq);
   } while (p.next(a));
 }
 
@@ -727,24 +732,28 @@ struct MassRing {
   static constexpr int kSlots = D == 128 ? 4 : 8, kStride = Ring<D>::kSide, kLds = kSlots * kStride;
 };
 
+template <int RT>
+struct MassShape {
+  static constexpr int TPW = q8_mass_tiles(RT), RW = q8_mass_rows(RT), kCompute = 2 * RW, kThreads = (kCompute + 1) * 64;
+};
+
 template <int D, int RT>
-__global__ void __launch_bounds__(((Waves<RT>::kCompute + 1) * 64))
-__attribute__((amdgpu_waves_per_eu(2, 2))) q8_mass_kernel(QArgs a) {
-  typedef Waves<RT> W_;
+__global__ void __launch_bounds__((MassShape<RT>::kThreads)) __attribute__((amdgpu_waves_per_eu(2, 2)))
+q8_mass_kernel(QArgs a) {
   typedef Ring<D> R_;
   typedef MassRing<D> P_;
-  constexpr int TPW = W_::TPW, TW = W_::TW;
+  constexpr int TPW = MassShape<RT>::TPW, RW = MassShape<RT>::RW, kCompute = MassShape<RT>::kCompute;
   extern __shared__ __align__(1024) char s_ring[];
 
   Piece p;
   if (!p.first(a)) return;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (w == W_::kCompute) {
+  if (w == kCompute) {
     load_share<D, true, P_::kSlots, P_::kStride>(a, p, s_ring);
     return;
   }
   const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-  const int tw = w % TW, rw = w / TW, t_first = rw * TPW;
+  const int tw = w % 2, rw = w / 2, t_first = rw * TPW;
   int slot = 0;
   do {
     const int tiles = min(RT, a.RTT - p.rg * RT);
@@ -760,39 +769,36 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) q8_mass_kernel(QArgs a) {
       load_query<D>(a, p.b, p.g, row, gq, q[x]);
       lim[x] = real[x] ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
     }
-    tile_lse<RT, TPW, TW>(a, h, t_first, tiles, real, n, gq, lse);
+    tile_lse<RT, TPW>(a, h, t_first, tiles, real, n, gq, lse);
     const int vis_all = min(p.c1 - 1, p.ctx);
-    float* mp = a.mpart + ((size_t)p.group(a) * W_::RW + rw) * a.c.n_cap;
+    float* mp = a.mpart + ((size_t)p.group(a) * RW + rw) * a.c.n_cap;
     for (int t0 = p.c0; t0 < p.c1; t0 += R_::ST) {
       lds_sync();
       const char* kb = s_ring + slot * P_::kStride;
       slot = slot + 1 == P_::kSlots ? 0 : slot + 1;
-#pragma unroll
-      for (int b = 0; b < W_::NB; ++b) {
-        const int r0 = 64 * (b + tw), tb = t0 + r0;
-        if (__builtin_amdgcn_readfirstlane(tb - p.c1) >= 0) break;
-        const uint32_t ke = *reinterpret_cast<const uint32_t*>(kb + R_::KB + r0 + 4 * n);
-        floatx4 S[TPW][4];
-        scores<D, TPW>(kb, ke, r0, n, gq, q, S);
-        if (__builtin_amdgcn_readfirstlane(tb + 63 - vis_all) > 0) {
-#pragma unroll
-          for (int x = 0; x < TPW; ++x)
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-              if (j > lim[x] - tb - 16 * gq) S[x][j % 4][j / 4] = kNegInf;
-        }
-        // (NaN scores of padding rows, whose q is a real row's, make a token's sum NaN that the real row makes so)
-        float sum[16];
+      const int r0 = 64 * tw, tb = t0 + r0;
+      if (__builtin_amdgcn_readfirstlane(tb - p.c1) >= 0) continue;
+      const uint32_t ke = *reinterpret_cast<const uint32_t*>(kb + R_::KB + r0 + 4 * n);
+      floatx4 S[TPW][4];
+      scores<D, TPW>(kb, ke, r0, n, gq, q, S);
+      if (__builtin_amdgcn_readfirstlane(tb + 63 - vis_all) > 0) {
 #pragma unroll
         for (int x = 0; x < TPW; ++x)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float e = fast_exp2(fmaf(S[x][j % 4][j / 4], a.sl2, -lse[x]));
-            sum[j] = x ? sum[j] + e : e;
-          }
-        const float m = row_sums(sum, lane);
-        if (tb + lane < p.c1) mp[tb + lane] = m;
+          for (int j = 0; j < 16; ++j)
+            if (j > lim[x] - tb - 16 * gq) S[x][j % 4][j / 4] = kNegInf;
       }
+      // (NaN scores of padding rows, whose q is a real row's, make a token's sum NaN that the real row makes so)
+      float sum[16];
+#pragma unroll
+      for (int x = 0; x < TPW; ++x)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float e = fast_exp2(fmaf(S[x][j % 4][j / 4], a.sl2, -lse[x]));
+          sum[j] = x ? sum[j] + e : e;
+        }
+      const float m = row_sums(sum, lane);
+      if (tb + lane < p.c1) mp[tb + lane] = m;
     }
   } while (p.next(a));
 }
@@ -824,7 +830,7 @@ __device__ __forceinline__ void join(RowSum& a, float m, float z, float zt, floa
 
 template <int D, int RT, int WPR>
 __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_row)[D / 4]) {
-  constexpr int LPR = D / 4, SG = 64 / LPR, TW = Waves<RT>::TW, kU = 8;
+  constexpr int LPR = D / 4, SG = 64 / LPR, kU = 8;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane % LPR;
   const int id = wg * (kFinWaves / WPR) + w / WPR;  // (fewer than 2^22 rows)
   const bool row_here = id < a.B * a.Hkv * a.R;
@@ -839,8 +845,9 @@ __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_
     ctx = s_.ctx;
     const int rg = row / (16 * RT), tile = row / 16 - rg * RT;
     const Holders h = holders(a, s_.per, s_.before, b, g * a.RG + rg, s_.ctx);
-    const size_t rec = ((size_t)h.rec * RT + tile) * TW * 16 + row % 16;
-    const int cnt = h.count * TW, sets = SG * WPR;
+    const int tw = tile < q8_full_tiles(RT) ? 1 : 2;  // records of a tile in each of the group's
+    const size_t rec = ((size_t)h.rec * RT + tile) * 2 * 16 + row % 16;
+    const int cnt = h.count * tw, sets = SG * WPR;
     for (int s0 = lane / LPR + SG * (w % WPR); s0 < cnt; s0 += kU * sets) {
       float2 v[kU];
       float zt[kU];
@@ -848,7 +855,7 @@ __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_
 #pragma unroll
       for (int j = 0; j < kU; ++j) {
         const int s = min(s0 + j * sets, cnt - 1);
-        const size_t i = rec + (size_t)(s / TW * RT * TW + s % TW) * 16;
+        const size_t i = rec + (size_t)(tw == 1 ? 2 * RT * s : s / 2 * RT * 2 + s % 2) * 16;
         v[j] = a.stats[i];
         zt[j] = a.zt[i];
         o[j] = *reinterpret_cast<const floatx4*>(a.opart + i * D + 4 * col);
@@ -915,7 +922,7 @@ __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_
 // order (0 past the sequence).
 template <int RT>
 __device__ __forceinline__ void sum_mass(const QArgs& a, int id) {
-  const int P = a.HR * Waves<RT>::RW;
+  const int P = a.HR * q8_mass_rows(RT);
   const int b = id / a.mass_per;
   const int64_t t0 = (int64_t)(id - b * a.mass_per) * a.mass_rows;
   const int N = clamp_ctx(a, a.ctx_len[b]) + a.T;
@@ -954,8 +961,8 @@ struct QKernels {
 
 template <int D, int RT>
 QKernels kernels() {
-  return {q8_part_kernel<D, RT>, q8_mass_kernel<D, RT>, {q8_finish_kernel<D, RT, 1>, q8_finish_kernel<D, RT, kFinWaves>}, (Waves<RT>::kCompute + 2) * 64,
-          (Waves<RT>::kCompute + 1) * 64, PartRing<D>::kLds, MassRing<D>::kLds};
+  return {q8_part_kernel<D, RT>, q8_mass_kernel<D, RT>, {q8_finish_kernel<D, RT, 1>, q8_finish_kernel<D, RT, kFinWaves>}, PartShape<RT>::kThreads,
+          MassShape<RT>::kThreads, PartRing<D>::kLds, MassRing<D>::kLds};
 }
 template <int D>
 QKernels pick(int RT) {
@@ -1027,7 +1034,7 @@ pvlm_status verify_q8_run(int B, int T, int Hq, int Hkv, int D, int64_t max_ctx,
     PVLM_LAUNCHED();
   }
   // a wave joins 16 records (8 at D = 64: 32) in one round of loads
-  const bool wide = p.recs * q8_waves(p.RT).tw > (size_t)B * a.HR * 2 * 16;
+  const bool wide = p.recs * 2 > (size_t)B * a.HR * 2 * 16;
   const int per_wg = wide ? 1 : kFinWaves, row_count = B * Hkv * p.R;
   hipLaunchKernelGGL(k.finish[wide], dim3(a.mass_wgs + (row_count + per_wg - 1) / per_wg), dim3(kFinThreads), 0, stream,
                      a);

@@ -16,14 +16,17 @@ constexpr int kQUnit = 32;
 constexpr int kQMinUnits = 2;  // least share: one 64-token block
 constexpr int kQMaxRT = 9;     // 16-row tiles of a workgroup
 
-// How a workgroup's waves share its row tiles and a stage's two blocks of 64
-// tokens: TPW tiles a wave (which converts a block's codes once for all of
-// them; a third tile has no registers), RW waves for the tiles, TW of each for
-// the blocks.  Two waves a SIMD at most, the two loading waves among them.
-struct QWaves {
-  int tpw, rw, tw;
-};
-constexpr QWaves q8_waves(int RT) { return {RT == 1 ? 1 : 2, (RT + 1) / 2, RT <= 6 ? 2 : 1}; }
+// The partial kernel's computing waves: one for each row tile and stage (two
+// blocks of 64 tokens), and one for each block where there are waves left: three
+// waves a SIMD with the two that load.  Tiles 0 .. full - 1 have one wave, the
+// others two, each with records of its own.
+constexpr int kQWaves = 10;
+constexpr int q8_full_tiles(int RT) { return RT <= kQWaves / 2 ? 0 : 2 * RT - kQWaves; }
+constexpr int q8_part_waves(int RT) { return 2 * RT - q8_full_tiles(RT); }
+// The mass kernel's: up to three tiles a wave, which convert a block's keys and
+// sum their rows together, and one wave for each block.
+constexpr int q8_mass_rows(int RT) { return (RT + 2) / 3; }
+constexpr int q8_mass_tiles(int RT) { return (RT + q8_mass_rows(RT) - 1) / q8_mass_rows(RT); }
 
 struct QSplit {
   int G, R;         // query heads of a KV head, and its query rows G * T
@@ -59,9 +62,9 @@ inline void split_verify_q8(int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
   const int64_t shares = (units + kQMinUnits - 1) / kQMinUnits;
   p->wgs = (int)(shares < cus ? shares : cus);
   p->recs = (size_t)(groups + p->wgs);
-  const size_t rows = p->recs * p->RT * q8_waves(p->RT).tw * 16;
+  const size_t rows = p->recs * p->RT * 2 * 16;
   p->off_mpart = kSyncRegion;  // (the region at the start is other calls')
-  p->off_stats = align_up(p->off_mpart + 4 * (size_t)groups * q8_waves(p->RT).rw * n_cap, 256);
+  p->off_stats = align_up(p->off_mpart + 4 * (size_t)groups * q8_mass_rows(p->RT) * n_cap, 256);
   p->off_zt = align_up(p->off_stats + 8 * rows, 256);
   p->off_opart = align_up(p->off_zt + 4 * rows, 256);
   p->bytes = align_up(p->off_opart + 4 * rows * D, 256);

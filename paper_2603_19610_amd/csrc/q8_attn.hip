@@ -23,6 +23,7 @@ namespace pvlm {
 namespace {
 
 typedef int intx2 __attribute__((ext_vector_type(2)));
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr double kLog2e = 1.4426950408889634;
@@ -200,16 +201,39 @@ __device__ __forceinline__ int row_t(const QArgs& a, int row) { return (int)((un
 // of a transposed read over the positions.
 template <int D>
 struct Lay {
-  static constexpr int CH = D / 16, LR = 256 / D;
+  static constexpr int CH = D / 16, LR = 256 / D;  // chunks of a row, rows of a line
   static __device__ __forceinline__ int kkey(int line) { return (line * LR >> 2) & 15; }
   static __device__ __forceinline__ int vkey(int line) {
     if constexpr (D == 128) return (line & 3) | ((line >> 1) & 4);
     else return line & 3;
   }
-  static __device__ __forceinline__ int at(int r, int c, int key) {
-    return (r / LR) * 256 + ((((r % LR) * CH + c) ^ key) << 4);
+  // Where a lane's reads of a block begin (of K's chunk NC gq of row 4 n, and of
+  // V's first column pair of rows 16 gq + ...), from the block's own start.  The
+  // others differ by a few bits of the position, so by an exclusive or of the
+  // address (blocks start at multiples of 256 bytes), and by whole lines.
+  static constexpr int NC = D / 64;  // 16-byte chunks of a lane's part of a key row
+  static __device__ __forceinline__ uint32_t k_lane(int n, int gq) {
+    const int line = 4 * n / LR;
+    return line * 256 + ((NC * gq ^ kkey(line)) << 4);
+  }
+  static __device__ __forceinline__ uint32_t k_at(uint32_t first, int tt, int c) {
+    return (first ^ (((tt % LR) * CH + c) << 4)) + tt / LR * 256;
+  }
+  static __device__ __forceinline__ uint32_t v_lane(int n, int gq) {
+    const int row = 16 * gq + n / 2, line = row / LR;
+    return line * 256 + ((((row % LR) * CH) ^ vkey(line)) << 4) + 8 * (n & 1);
+  }
+  // rows 8 ks on, column 16 jd + n: 8 ks rows are 8 / LR lines, which change V's key at D = 64
+  static __device__ __forceinline__ uint32_t v_at(uint32_t first, int ks, int jd) {
+    const int key = D == 128 ? 0 : vkey(8 * ks / LR);
+    return (first ^ ((jd ^ key) << 4)) + ks * (8 / LR) * 256;
   }
 };
+
+template <typename T>
+__device__ __forceinline__ T lds_read(uint32_t at) {
+  return *(const __attribute__((address_space(3))) T*)at;
+}
 
 // ---------------------------------------------------------------- operands --
 // A lane's d range of a row: 32 values at D = 128, 16 at 64, of which k-step s
@@ -247,17 +271,13 @@ __device__ __forceinline__ bf16x8 to_bf16(uint32_t lo, uint32_t hi, float unit) 
 // Scores of one block against a wave's row tiles: S[x][tt][i] is token
 // 16 gq + 4 i + tt.  The keys are converted once for all tiles.
 template <int D, int TPW>
-__device__ __forceinline__ void scores(const char* kb, uint32_t exps, int r0, int n, int gq, const Query<D> (&q)[TPW],
-                                       floatx4 (&S)[TPW][4]) {
-  typedef Lay<D> L;
-  constexpr int NC = D / 64;  // 16-byte chunks of a lane's range
-  uint4 k[4][NC];
+__device__ __forceinline__ void scores(uint32_t k_first, uint32_t exps, const Query<D> (&q)[TPW], floatx4 (&S)[TPW][4]) {
+  constexpr int NC = Lay<D>::NC;
+  uintx4 k[4][NC];
 #pragma unroll
-  for (int tt = 0; tt < 4; ++tt) {
-    const int r = r0 + 4 * n + tt, key = L::kkey(r / L::LR);
+  for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
-    for (int c = 0; c < NC; ++c) k[tt][c] = *reinterpret_cast<const uint4*>(kb + L::at(r, NC * gq + c, key));
-  }
+    for (int c = 0; c < NC; ++c) k[tt][c] = lds_read<uintx4>(Lay<D>::k_at(k_first, tt, c));
 #pragma unroll
   for (int x = 0; x < TPW; ++x)
 #pragma unroll
@@ -276,24 +296,22 @@ __device__ __forceinline__ void scores(const char* kb, uint32_t exps, int r0, in
     }
 }
 
-// Eight consecutive tokens (rows r .. r + 7 of the lane group) of column 16 jd + n.
+// Eight consecutive tokens (rows 16 gq + 8 ks on) of column 16 jd + n.
 template <int D>
-__device__ __forceinline__ intx2 read_v(const char* vb, int r, int jd, int n) {
-  typedef Lay<D> L;
+__device__ __forceinline__ intx2 read_v(uint32_t v_first, int ks, int jd) {
   typedef __attribute__((address_space(3))) intx2* lds_v2;
-  const int row = r + n / 2;
-  const uint32_t at = lds_addr(vb) + L::at(row, jd, L::vkey(row / L::LR)) + 8 * (n & 1);
-  return __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2)at);
+  return __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2)Lay<D>::v_at(v_first, ks, jd));
 }
+
 // Two columns' operands of a block, as codes.
 struct VPair {
   intx2 v[4];
 };
 template <int D>
-__device__ __forceinline__ VPair read_pair(const char* vb, int r0, int n, int gq, int pair) {
+__device__ __forceinline__ VPair read_pair(uint32_t v_first, int pair) {
   VPair p;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) p.v[i] = read_v<D>(vb, r0 + 16 * gq + 8 * (i & 1), 2 * pair + i / 2, n);
+  for (int i = 0; i < 4; ++i) p.v[i] = read_v<D>(v_first, i & 1, 2 * pair + i / 2);
   return p;
 }
 
@@ -306,13 +324,13 @@ __device__ __forceinline__ VPair read_pair(const char* vb, int r0, int n, int gq
 // of those tokens.  Returns whether there were any: the finish kernel then
 // gives the rows that see them their NaN.
 template <int D, bool MASKED>
-__device__ __forceinline__ uint32_t weigh(const char* vb, int r0, int n, int gq, const bf16x8 (&P)[2], VPair cur,
+__device__ __forceinline__ uint32_t weigh(uint32_t v_first, const bf16x8 (&P)[2], VPair cur,
                                           const uint32_t (&mask)[4], floatx4 (&O)[D / 16]) {
   uint32_t bad = 0;
 #pragma unroll
   for (int pair = 0; pair < D / 32; ++pair) {
     VPair next;
-    if (pair + 1 < D / 32) next = read_pair<D>(vb, r0, n, gq, pair + 1);
+    if (pair + 1 < D / 32) next = read_pair<D>(v_first, pair + 1);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t v0 = cur.v[i][0], v1 = cur.v[i][1];
@@ -557,10 +575,13 @@ struct PartWave {
   float ref, z;
   floatx4 O[DPL], zt;
   uint32_t bad;  // a NaN value that not every row sees
+  uint32_t k_lane, v_lane;
 
   __device__ __forceinline__ void begin(const QArgs& a, const Piece& p, int tile, int n, int gq) {
     ctx = p.ctx;
     bad = 0;
+    k_lane = Lay<D>::k_lane(n, gq);
+    v_lane = Lay<D>::v_lane(n, gq);
     const int row = tile * 16 + n;
     load_query<D>(a, p.b, p.g, row, gq, q[0]);
     lim = row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
@@ -571,16 +592,15 @@ struct PartWave {
     for (int jd = 0; jd < DPL; ++jd) O[jd] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // The block of tokens tb .. tb + 63, rows r0 .. r0 + 63 of the stage.  TAIL: some row does not see all of them.
+  // The block of tokens tb .. tb + 63, block x of the stage at LDS address `at`.  TAIL: some row does not see all of them.
   template <bool TAIL>
-  __device__ __forceinline__ void block(const QArgs& a, const char* kb, int tb, int r0, int n, int gq) {
+  __device__ __forceinline__ void block(const QArgs& a, uint32_t at, int tb, int x, int n, int gq) {
     typedef Ring<D> R_;
-    const char* vb = kb + R_::kSide;
-    const uint32_t ke = *reinterpret_cast<const uint32_t*>(kb + R_::KB + r0 + 4 * n);
-    const uint4 ve4 = *reinterpret_cast<const uint4*>(vb + R_::KB + r0 + 16 * gq);
-    const uint32_t ve[4] = {ve4.x, ve4.y, ve4.z, ve4.w};
+    const uint32_t kb = at + x * 64 * D, vb = kb + R_::kSide, eb = at + R_::KB + x * 64;
+    const uint32_t ke = lds_read<uint32_t>(eb + 4 * n);
+    const uintx4 ve = lds_read<uintx4>(eb + R_::kSide + 16 * gq);
     floatx4 S1[1][4];
-    scores<D, 1>(kb, ke, r0, n, gq, q, S1);
+    scores<D, 1>(kb + k_lane, ke, q, S1);
     floatx4(&S)[4] = S1[0];
     if constexpr (TAIL) {  // the lane's token j is visible iff j <= lim - tb - 16 gq
 #pragma unroll
@@ -603,7 +623,7 @@ struct PartWave {
 #pragma unroll
       for (int jd = 0; jd < DPL; ++jd) O[jd] = O[jd] * f;
     }
-    const VPair v0 = read_pair<D>(vb, r0, n, gq, 0);
+    const VPair v0 = read_pair<D>(vb + v_lane, 0);
     bf16x8 ones;
 #pragma unroll
     for (int j = 0; j < 8; ++j) ones[j] = static_cast<__bf16>(1.f);
@@ -629,7 +649,7 @@ struct PartWave {
         mask[k] = o >= 3 ? 0u : o < 0 ? ~0u : ~0u << (8 * (o + 1));
       }
     }
-    bad |= weigh<D, TAIL>(vb, r0, n, gq, pv, v0, mask, O);
+    bad |= weigh<D, TAIL>(vb + v_lane, pv, v0, mask, O);
   }
 
   __device__ __forceinline__ void end(const QArgs& a, size_t rec, int tile, int n, int gq) {
@@ -682,6 +702,7 @@ __attribute__((amdgpu_waves_per_eu(PartShape<RT>::kPerEu, PartShape<RT>::kPerEu)
   }
   const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
   const Role my = role<RT>(w);
+  const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_addr(s_ring));
   int slot = 0;
   do {
     const int tile = p.rg * RT + my.tile;  // of the KV head
@@ -696,27 +717,27 @@ __attribute__((amdgpu_waves_per_eu(PartShape<RT>::kPerEu, PartShape<RT>::kPerEu)
     const int whole = __builtin_amdgcn_readfirstlane(live ? (min(p.c1 - 1, p.ctx) - last - p.c0 + R_::ST) / R_::ST : 0);
     auto stage = [&]() {
       lds_sync();
-      const char* base = s_ring + slot * P_::kStride;
+      const uint32_t at = ring + slot * P_::kStride;
       slot = slot + 1 == P_::kSlots ? 0 : slot + 1;
-      return base;
+      return at;
     };
     int s = 0;
     if (whole > 0) {
       do {
-        const char* base = stage();
+        const uint32_t at = stage();
         int x = 0;
-        do v.template block<false>(a, base, 0, 64 * (my.block + x), n, gq);
+        do v.template block<false>(a, at, 0, my.block + x, n, gq);
         while (++x < my.blocks);
       } while (++s < whole);
     }
     if (s < nst) {
       do {
-        const char* base = stage();
+        const uint32_t at = stage();
         if (live) {
           int x = 0;
           do {
-            const int r0 = 64 * (my.block + x), tb = p.c0 + s * R_::ST + r0;
-            if (tb < p.c1) v.template block<true>(a, base, tb, r0, n, gq);
+            const int tb = p.c0 + s * R_::ST + 64 * (my.block + x);
+            if (tb < p.c1) v.template block<true>(a, at, tb, my.block + x, n, gq);
           } while (++x < my.blocks);
         }
       } while (++s < nst);
@@ -754,6 +775,7 @@ q8_mass_kernel(QArgs a) {
   }
   const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
   const int tw = w % 2, rw = w / 2, t_first = rw * TPW;
+  const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_addr(s_ring)), k_lane = Lay<D>::k_lane(n, gq);
   int slot = 0;
   do {
     const int tiles = min(RT, a.RTT - p.rg * RT);
@@ -774,13 +796,13 @@ q8_mass_kernel(QArgs a) {
     float* mp = a.mpart + ((size_t)p.group(a) * RW + rw) * a.c.n_cap;
     for (int t0 = p.c0; t0 < p.c1; t0 += R_::ST) {
       lds_sync();
-      const char* kb = s_ring + slot * P_::kStride;
+      const uint32_t at = ring + slot * P_::kStride;
       slot = slot + 1 == P_::kSlots ? 0 : slot + 1;
-      const int r0 = 64 * tw, tb = t0 + r0;
+      const int tb = t0 + 64 * tw;
       if (__builtin_amdgcn_readfirstlane(tb - p.c1) >= 0) continue;
-      const uint32_t ke = *reinterpret_cast<const uint32_t*>(kb + R_::KB + r0 + 4 * n);
+      const uint32_t ke = lds_read<uint32_t>(at + R_::KB + 64 * tw + 4 * n);
       floatx4 S[TPW][4];
-      scores<D, TPW>(kb, ke, r0, n, gq, q, S);
+      scores<D, TPW>(at + tw * 64 * D + k_lane, ke, q, S);
       if (__builtin_amdgcn_readfirstlane(tb + 63 - vis_all) > 0) {
 #pragma unroll
         for (int x = 0; x < TPW; ++x)

@@ -53,6 +53,7 @@ struct QArgs {
   float* mpart;      // [B][HR][waves][n_cap] mass of one wave's rows
   float2* stats;     // [record][tile][token wave][16] (log2-domain maximum, sum) of rows
   float* zt;         // the same sums of the probabilities as P . V takes them, rounded to bf16
+  uint32_t* nan;     // [record][CW] the values hold a NaN that not every row sees
   float* opart;      // [record][tile][token wave][16][D] sums of P . V relative to that maximum
   uint16_t* out;
   float* lse;
@@ -186,78 +187,49 @@ __device__ __forceinline__ Holders holders(const QArgs& a, int per, int before, 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ int row_t(const QArgs& a, int row) { return (int)((unsigned)row * a.g_magic >> 20); }
 
-// --------------------------------------------------------------- layouts --
-// Tokens are the M side of the score tiles and query rows the N side.  A block
-// is 64 tokens: tile tt holds tokens 4 n + tt, so lane (n, gq) = (lane & 15,
-// lane >> 4), which owns rows 4 gq .. 4 gq + 3 of each tile's result, gets the
-// 16 consecutive tokens 16 gq + 4 i + tt: the order P.V wants for its A
-// operand, and one 16-byte read of their exponents.  The exponents of a
-// lane's four key rows are one 4-byte word.
-//
-// LDS holds a stage's codes as lines of 256 bytes (2 rows at D = 128, 4 at 64):
-// 16-byte chunk c of row r lies at position ((r mod rows-per-line) * CH + c) ^
-// key(r) of its line.  K's key is (r / 4) mod 16: the 16 rows 4 n + tt of an
-// operand read fall on 16 positions.  V's key spreads the 8 consecutive rows
-// of a transposed read over the positions.
+// ------------------------------------------------------------- the blocks --
+// The row index (in rows of codes) of the unit that token t opens.  A page entry
+// outside the pool sets bad and is clamped into it.
+__device__ __forceinline__ int64_t unit_row(const QArgs& a, int b, int g, int t, bool& bad) {
+  if (!a.c.table) return ((int64_t)b * a.Hkv + g) * a.c.n_cap + t;
+  int pg = uniform_load(a.c.table, (int64_t)b * a.c.max_pages + (t >> a.c.shift));
+  if (pg < 0 || pg >= a.c.n_pages) {
+    bad = true;
+    pg = pg < 0 ? 0 : (int)(a.c.n_pages - 1);
+  }
+  return (((int64_t)pg * a.Hkv + g) << a.c.shift) + (t & ((1 << a.c.shift) - 1));
+}
+
+// LDS holds a block of 64 tokens as bf16 rows, of K and of V: 16-byte chunk c
+// of row r lies at chunk c ^ swz(r) of the row.  swz permutes the bits of r mod 16
+// so that over the 64 banks (256 bytes: one row, or two of D = 64) 16 rows' same
+// chunk, and 8 rows' same two chunks, are apart: what the reads of K and V take
+// at a time.  (r mod CH in its place: a third of all LDS cycles were conflicts.)
 template <int D>
 struct Lay {
-  static constexpr int CH = D / 16, LR = 256 / D;  // chunks of a row, rows of a line
-  static __device__ __forceinline__ int kkey(int line) { return (line * LR >> 2) & 15; }
-  static __device__ __forceinline__ int vkey(int line) {
-    if constexpr (D == 128) return (line & 3) | ((line >> 1) & 4);
-    else return line & 3;
+  static constexpr int CH = D / 8, kSide = 64 * D * 2;  // chunks of a row, bytes of a block's K or V
+  // Where a lane's reads of a block begin: K's chunk gq of row n (the others are
+  // 4 ks chunks and 16 tt rows on), and V's 8 bytes of row 4 gq + n / 4 (32 jd
+  // bytes, and 16 and 32 rows on).  Chunks differ by an exclusive or of the
+  // address: blocks start at multiples of 256 bytes.
+  static constexpr __host__ __device__ int swz(int r) {
+    const int m = D == 64 ? (r & 15) >> 1 : r & 15;
+    return ((m << 1) | (m >> (D == 64 ? 2 : 3))) & (CH - 1);
   }
-  // Where a lane's reads of a block begin (of K's chunk NC gq of row 4 n, and of
-  // V's first column pair of rows 16 gq + ...), from the block's own start.  The
-  // others differ by a few bits of the position, so by an exclusive or of the
-  // address (blocks start at multiples of 256 bytes), and by whole lines.
-  static constexpr int NC = D / 64;  // 16-byte chunks of a lane's part of a key row
-  static __device__ __forceinline__ uint32_t k_lane(int n, int gq) {
-    const int line = 4 * n / LR;
-    return line * 256 + ((NC * gq ^ kkey(line)) << 4);
-  }
-  static __device__ __forceinline__ uint32_t k_at(uint32_t first, int tt, int c) {
-    return (first ^ (((tt % LR) * CH + c) << 4)) + tt / LR * 256;
-  }
+  static __device__ __forceinline__ uint32_t k_lane(int n, int gq) { return n * D * 2 + ((gq ^ swz(n)) << 4); }
+  static __device__ __forceinline__ uint32_t k_at(uint32_t lane, int ks, int tt) { return (lane ^ (ks << 6)) + tt * 32 * D; }
   static __device__ __forceinline__ uint32_t v_lane(int n, int gq) {
-    const int row = 16 * gq + n / 2, line = row / LR;
-    return line * 256 + ((((row % LR) * CH) ^ vkey(line)) << 4) + 8 * (n & 1);
+    const int row = 4 * gq + n / 4;
+    return row * D * 2 + ((((n >> 1) & 1) ^ swz(row)) << 4) + 8 * (n & 1);
   }
-  // rows 8 ks on, column 16 jd + n: 8 ks rows are 8 / LR lines, which change V's key at D = 64
-  static __device__ __forceinline__ uint32_t v_at(uint32_t first, int ks, int jd) {
-    const int key = D == 128 ? 0 : vkey(8 * ks / LR);
-    return (first ^ ((jd ^ key) << 4)) + ks * (8 / LR) * 256;
-  }
+  static __device__ __forceinline__ uint32_t v_at(uint32_t lane, int jd, int rows) { return (lane ^ (jd << 5)) + rows * D * 2; }
 };
 
 template <typename T>
 __device__ __forceinline__ T lds_read(uint32_t at) {
   return *(const __attribute__((address_space(3))) T*)at;
 }
-
-// ---------------------------------------------------------------- operands --
-// A lane's d range of a row: 32 values at D = 128, 16 at 64, of which k-step s
-// takes values 8 s .. 8 s + 7 (the same assignment on both sides).
-template <int D>
-struct Query {
-  bf16x8 s[D / 32];
-};
-
-template <int D>
-__device__ __forceinline__ void load_query(const QArgs& a, int b, int g, int row, int gq, Query<D>& q) {
-  const int r = min(row, a.R - 1), t = row_t(a, r), h = g * a.G + r - t * a.G;
-  const bf16x8* src = reinterpret_cast<const bf16x8*>(a.q + (((size_t)b * a.T + t) * a.Hq + h) * D + D / 4 * gq);
-#pragma unroll
-  for (int s = 0; s < D / 32; ++s) q.s[s] = src[s];
-}
-
-// Maximum over the four lanes l, l^16, l^32, l^48; NaN if one is.
-__device__ __forceinline__ float rows4_maximum(float x) {
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  const float y = __builtin_elementwise_maximum(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
-  return __builtin_elementwise_maximum(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
+__device__ __forceinline__ void lds_write(uint32_t at, bf16x8 x) { *(__attribute__((address_space(3))) bf16x8*)at = x; }
 
 // Eight codes as bf16, times a power of two.
 __device__ __forceinline__ bf16x8 to_bf16(uint32_t lo, uint32_t hi, float unit) {
@@ -268,86 +240,174 @@ __device__ __forceinline__ bf16x8 to_bf16(uint32_t lo, uint32_t hi, float unit) 
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// Scores of one block against a wave's row tiles: S[x][tt][i] is token
-// 16 gq + 4 i + tt.  The keys are converted once for all tiles.
+// What a converting wave does: one side (K or V) of the workgroup's blocks (of
+// a round's blocks those from number `first` on, CW apart), from memory through
+// registers into LDS as bf16, a row's power of two taken in.  Each conversion
+// happens once for all row tiles.
+// DEPTH blocks are on their way at any time, by ordinary loads that the
+// compiler waits for one block at a time.  TW blocks make a round, for which
+// LDS has two slots of ROUND bytes: one barrier a round hands a filled one over
+// and an emptied one back.
+//
+// Rows past the piece become zeros (their tokens' probabilities are 0, and 0
+// times what an unwritten row holds may be NaN).  So do NaN values of rows that
+// not every query row sees; the record's flag has the finish kernel look for
+// them.
+template <int D, int TW, int CW, int DEPTH, int ROUND, int BLOCK, bool IS_V>
+__device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first, uint32_t ring) {
+  constexpr int PER = TW / CW;  // blocks of a round
+  constexpr int NI = D / 16;  // lanes of a row, and rows of a lane: consecutive ones, whose exponents it reads at once
+  typedef uint32_t Exps __attribute__((ext_vector_type(NI / 4)));
+  const uint8_t* codes = IS_V ? a.c.vc : a.c.kc;
+  const uint8_t* exps = IS_V ? a.c.ve : a.c.ke;
+  const int lane = threadIdx.x & 63, c = lane % NI, row0 = NI * (lane / NI);
+  const uint32_t lds0 = row0 * D * 2 + (((2 * c) ^ Lay<D>::swz(row0)) << 4);
+
+  uintx4 v[DEPTH][NI];
+  Exps e[DEPTH];
+  int tb[DEPTH], c1[DEPTH], ctx[DEPTH], last_of[DEPTH];  // its tokens; its record if it is its piece's last block, else -1
+  int t0 = p.c0 + 64 * first, x = 0, total = 0;
+  bool more = true, bad_page = false;
+  // nothing of another path is under way (the compiler would wait for it at every block)
+  __builtin_amdgcn_s_waitcnt(0x0f70);
+  // (always loads, so that the compiler knows how many loads are under way: past
+  // the share, the rows of its last block again)
+  auto issue = [&](int k) {
+    const int last = (p.c1 - 1) & ~31;  // the piece's last unit; of a whole unit every row may be read
+    const int64_t u0 = unit_row(a, p.b, p.g, min(t0, last), bad_page);
+    const int64_t u1 = unit_row(a, p.b, p.g, min(t0 + 32, last), bad_page);
+    const int64_t r = row0 < 32 ? u0 + row0 : u1 + (row0 - 32);
+    const uint8_t* src = codes + r * D + 16 * c;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) v[k][i] = *reinterpret_cast<const uintx4*>(src + i * D);
+    e[k] = *reinterpret_cast<const Exps*>(exps + r);
+    if (!more) return;
+    tb[k] = t0;
+    c1[k] = p.c1;
+    ctx[k] = p.ctx;
+    last_of[k] = -1;
+    ++total;
+    t0 += 64 * CW;
+    if (++x == PER) {
+      x = 0;
+      if (t0 - 64 * first >= p.c1) {
+        last_of[k] = (p.group(a) + blockIdx.x) * CW + first;
+        Piece next = p;
+        more = next.next(a);
+        if (more) {
+          p = next;
+          t0 = p.c0 + 64 * first;
+        }
+      }
+    }
+  };
+  uint32_t bad = 0;
+  auto convert = [&](int k, uint32_t at) {
+    const int whole = IS_V ? min(c1[k] - 1, ctx[k]) : c1[k] - 1;
+    if (__builtin_amdgcn_readfirstlane(tb[k] + 63 - whole) > 0) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int t = tb[k] + row0 + i;
+        if (t >= c1[k]) {
+          v[k][i] = uintx4{0, 0, 0, 0};
+          e[k][i / 4] = (e[k][i / 4] & ~(0xffu << 8 * (i % 4))) | 127u << 8 * (i % 4);
+        }
+        if (IS_V && t > ctx[k])
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t m = nan_codes(v[k][i][j]);
+            bad |= m;
+            v[k][i][j] &= ~(m | (m - (m >> 7)));
+          }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const float unit = q8_unit((e[k][i / 4] >> (8 * (i % 4))) & 0xffu);
+      lds_write((at ^ (Lay<D>::swz(i) << 4)) + i * D * 2, to_bf16(v[k][i][0], v[k][i][1], unit));
+      lds_write((at ^ ((Lay<D>::swz(i) ^ 1) << 4)) + i * D * 2, to_bf16(v[k][i][2], v[k][i][3], unit));
+    }
+    if (IS_V && last_of[k] >= 0) {
+      const bool any = __any(bad);
+      if (lane == 0) a.nan[last_of[k]] = any;
+      bad = 0;
+    }
+  };
+  // (one loop body and no way out of its middle, for the same reason)
+  int done = -DEPTH;
+  do {
+#pragma unroll
+    for (int k = 0; k < DEPTH; ++k) {
+      const bool now = done >= 0 && done < total;
+      if (now) convert(k, ring + lds0 + (done / PER % 2) * ROUND + (done % PER * CW + first) * BLOCK);
+      issue(k);
+      ++done;
+      if (now && done % PER == 0) lds_sync();  // the round is there; every wave is done with the one before
+    }
+  } while (done < total);
+  if (bad_page && lane == 0) dev_flag(a.status, PVLM_DEV_RANGE);
+}
+
+// ---------------------------------------------------------------- operands --
+// Tokens are the M side of 16-row score tiles and query rows the N side (lane
+// (n, gq) = (lane & 15, lane >> 4) owns row n and tokens 16 tt + 4 gq + i of tile
+// tt), which is the layout P . V needs as its A operand.
+template <int D>
+struct Query {
+  bf16x8 s[D / 32];  // chunk 4 ks + gq of the row
+};
+
+template <int D>
+__device__ __forceinline__ void load_query(const QArgs& a, int b, int g, int row, int gq, Query<D>& q) {
+  const int r = min(row, a.R - 1), t = row_t(a, r), h = g * a.G + r - t * a.G;
+  const bf16x8* src = reinterpret_cast<const bf16x8*>(a.q + (((size_t)b * a.T + t) * a.Hq + h) * D) + gq;
+#pragma unroll
+  for (int ks = 0; ks < D / 32; ++ks) q.s[ks] = src[4 * ks];
+}
+
+// Maximum over the four lanes l, l^16, l^32, l^48; NaN if one is.
+__device__ __forceinline__ float rows4_maximum(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const float y = __builtin_elementwise_maximum(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+  return __builtin_elementwise_maximum(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// Scores of a block (its K at LDS address k plus the lane's offset) against a wave's row tiles.
 template <int D, int TPW>
-__device__ __forceinline__ void scores(uint32_t k_first, uint32_t exps, const Query<D> (&q)[TPW], floatx4 (&S)[TPW][4]) {
-  constexpr int NC = Lay<D>::NC;
-  uintx4 k[4][NC];
-#pragma unroll
-  for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-    for (int c = 0; c < NC; ++c) k[tt][c] = lds_read<uintx4>(Lay<D>::k_at(k_first, tt, c));
+__device__ __forceinline__ void scores(uint32_t k, const Query<D> (&q)[TPW], floatx4 (&S)[TPW][4]) {
 #pragma unroll
   for (int x = 0; x < TPW; ++x)
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) S[x][tt] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
+  for (int ks = 0; ks < D / 32; ++ks)
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) {
-      const float unit = q8_unit((exps >> (8 * tt)) & 0xffu);
-      const bf16x8 k0 = to_bf16(k[tt][c].x, k[tt][c].y, unit), k1 = to_bf16(k[tt][c].z, k[tt][c].w, unit);
+      const bf16x8 kr = lds_read<bf16x8>(Lay<D>::k_at(k, ks, tt));
 #pragma unroll
-      for (int x = 0; x < TPW; ++x) {
-        S[x][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[x].s[2 * c], S[x][tt], 0, 0, 0);
-        S[x][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[x].s[2 * c + 1], S[x][tt], 0, 0, 0);
-      }
+      for (int x = 0; x < TPW; ++x) S[x][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr, q[x].s[ks], S[x][tt], 0, 0, 0);
     }
 }
 
-// Eight consecutive tokens (rows 16 gq + 8 ks on) of column 16 jd + n.
-template <int D>
-__device__ __forceinline__ intx2 read_v(uint32_t v_first, int ks, int jd) {
-  typedef __attribute__((address_space(3))) intx2* lds_v2;
-  return __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2)Lay<D>::v_at(v_first, ks, jd));
-}
-
-// Two columns' operands of a block, as codes.
-struct VPair {
-  intx2 v[4];
-};
-template <int D>
-__device__ __forceinline__ VPair read_pair(uint32_t v_first, int pair) {
-  VPair p;
+// O += P . V over a block; P[x][h] holds tokens 32 h + 4 gq + {0..3, 16..19}.
+// Transposed LDS reads: each 16 lanes fetch 16 columns of four rows (lane n the
+// 8 bytes of row n / 4, columns 4 (n mod 4) on) and lane n receives column n.
+template <int D, int TPW>
+__device__ __forceinline__ void weigh(uint32_t v, const bf16x8 (&P)[TPW][2], floatx4 (&O)[TPW][D / 16]) {
+  typedef short s4 __attribute__((ext_vector_type(4)));
+  typedef short s8 __attribute__((ext_vector_type(8)));
+  typedef __attribute__((address_space(3))) s4* lds_s4;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) p.v[i] = read_v<D>(v_first, i & 1, 2 * pair + i / 2);
-  return p;
-}
-
-// O += P' . V over one block; P'[ks] holds tokens 16 gq + 8 ks + j.  The next
-// two columns are read while two are multiplied; the barriers keep the compiler
-// from reading all of them at once, for which there are no registers.
-//
-// MASKED: of the tokens that not every row sees, NaN codes count as 0 (0 times
-// NaN would be NaN for rows that do not see them); mask has 0xff in the bytes
-// of those tokens.  Returns whether there were any: the finish kernel then
-// gives the rows that see them their NaN.
-template <int D, bool MASKED>
-__device__ __forceinline__ uint32_t weigh(uint32_t v_first, const bf16x8 (&P)[2], VPair cur,
-                                          const uint32_t (&mask)[4], floatx4 (&O)[D / 16]) {
-  uint32_t bad = 0;
+  for (int jd = 0; jd < D / 16; ++jd)
 #pragma unroll
-  for (int pair = 0; pair < D / 32; ++pair) {
-    VPair next;
-    if (pair + 1 < D / 32) next = read_pair<D>(v_first, pair + 1);
+    for (int h = 0; h < 2; ++h) {
+      const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)Lay<D>::v_at(v, jd, 32 * h));
+      const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)Lay<D>::v_at(v, jd, 32 * h + 16));
+      const bf16x8 b = __builtin_bit_cast(bf16x8, (s8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t v0 = cur.v[i][0], v1 = cur.v[i][1];
-      if constexpr (MASKED) {
-        const uint32_t b0 = nan_codes(v0) & mask[2 * (i & 1)], b1 = nan_codes(v1) & mask[2 * (i & 1) + 1];
-        bad |= b0 | b1;
-        v0 &= ~(b0 | (b0 - (b0 >> 7)));
-        v1 &= ~(b1 | (b1 - (b1 >> 7)));
-      }
-      const bf16x8 b = to_bf16(v0, v1, 1.f);
-      const int jd = 2 * pair + i / 2;
-      O[jd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[i & 1], b, O[jd], 0, 0, 0);
+      for (int x = 0; x < TPW; ++x) O[x][jd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][h], b, O[x][jd], 0, 0, 0);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    cur = next;
-  }
-  return bad;
 }
 
 // (maximum, sum) of two sets of scores.  A sum of 0 belongs to one of which the
@@ -364,8 +424,9 @@ template <int RT, int TPW>
 __device__ __forceinline__ void tile_lse(const QArgs& a, const Holders& h, int tile0, int tiles, const bool (&real)[TPW],
                                          int n, int gq, float (&lse)[TPW]) {
   constexpr int kU = TPW == 1 ? 8 : 4;  // records of every tile in flight
-  const int cnt = 2 * h.count;  // (of a tile that one wave has the first of every two)
-  const float2* st = a.stats + (size_t)h.rec * RT * 2 * 16 + n;
+  constexpr int TW = q8_waves(RT).tw;
+  const int cnt = TW * h.count;
+  const float2* st = a.stats + (size_t)h.rec * RT * TW * 16 + n;
   float M[TPW], Z[TPW];
 #pragma unroll
   for (int x = 0; x < TPW; ++x) M[x] = kNegInf, Z[x] = 0.f;
@@ -374,12 +435,9 @@ __device__ __forceinline__ void tile_lse(const QArgs& a, const Holders& h, int t
 #pragma unroll
     for (int j = 0; j < kU; ++j) {
       const int s = min(s0 + 4 * j, cnt - 1);
-      const float2* r = st + (size_t)(s / 2 * RT * 2 + s % 2) * 16;
+      const float2* r = st + (size_t)(s / TW * RT * TW + s % TW) * 16;
 #pragma unroll
-      for (int x = 0; x < TPW; ++x) {
-        const int tile = min(tile0 + x, tiles - 1);
-        v[j][x] = tile < q8_full_tiles(RT) && s % 2 ? make_float2(kNegInf, 0.f) : r[tile * 2 * 16];
-      }
+      for (int x = 0; x < TPW; ++x) v[j][x] = r[min(tile0 + x, tiles - 1) * TW * 16];
     }
 #pragma unroll
     for (int x = 0; x < TPW; ++x) {
@@ -403,8 +461,8 @@ __device__ __forceinline__ void tile_lse(const QArgs& a, const Holders& h, int t
   }
 }
 
-// Sum over the 16 rows (lanes n) of a block's values, of token `lane` of the
-// block: each step a lane keeps half of its values, chosen by one bit of n, and
+// Sum over the 16 rows (lanes n) of a block's values, of the value with
+// number n (lane & 15): each step a lane keeps half of its values, chosen by one bit of n, and
 // adds its partner's copy of that half.
 __device__ __forceinline__ float row_sums(const float (&p)[16], int lane) {
   const bool h8 = lane & 8, h4 = lane & 4, h2 = lane & 2, h1 = lane & 1;
@@ -418,273 +476,129 @@ __device__ __forceinline__ float row_sums(const float (&p)[16], int lane) {
   return (h1 ? a2[1] : a2[0]) + lane_xor1(h1 ? a2[0] : a2[1]);
 }
 
-// ------------------------------------------------------------------ ring --
-// A stage is 128 tokens' codes and exponents.  The loading waves copy stages
-// into an LDS ring by global->LDS loads of 1 KB (16 bytes a lane, in LDS order:
-// the lanes fetch permuted chunks), so loads stay in flight behind the other
-// waves' arithmetic.  One barrier a stage hands a landed slot over and an
-// emptied one back.
-template <int D>
-struct Ring {
-  static constexpr int ST = 128, KB = ST * D;          // tokens of a stage, bytes of its codes (K or V)
-  static constexpr int NI = KB / 1024;                 // load instructions for them
-  static constexpr int kSide = KB + 256;               // ... and exponents (ST bytes; a load writes 256)
-  static constexpr int RPI = 1024 / D, IPU = 32 / RPI; // rows of an instruction, instructions of a unit
-};
-
-// Loads as inline asm: the compiler neither counts them nor waits for them; the
-// loading wave, which issues no other vector memory operation (but to flag an
-// error, which only makes a wait longer), counts them itself.  An LDS load may
-// not directly follow the scalar write of M0 that gives its LDS address (one
-// wait state, hence the s_nop).
-__device__ __forceinline__ void lds_load16(int64_t base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "memory", "m0");
-}
-__device__ __forceinline__ void lds_load4(const void* p, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds), "v"(p) : "memory", "m0");
-}
-// Wait until at most `stages` later stages' loads (N each) are in flight.
-template <int N, int MOST>
-__device__ __forceinline__ void wait_stage(int stages) {
-  static_assert(MOST * N < 64, "vmcnt holds 6 bits");
-  if constexpr (MOST == 0) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  } else {
-    if (stages >= MOST) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N * MOST) : "memory");
-    else wait_stage<N, MOST - 1>(stages);
-  }
-}
-
-// The row index (in rows of codes) of the unit that token t opens.  A page entry
-// outside the pool is flagged and clamped into it.
-__device__ __forceinline__ int64_t unit_row(const QArgs& a, int b, int g, int t) {
-  if (!a.c.table) return ((int64_t)b * a.Hkv + g) * a.c.n_cap + t;
-  int pg = uniform_load(a.c.table, (int64_t)b * a.c.max_pages + (t >> a.c.shift));
-  if (pg < 0 || pg >= a.c.n_pages) {
-    dev_flag(a.status, PVLM_DEV_RANGE);
-    pg = pg < 0 ? 0 : (int)(a.c.n_pages - 1);
-  }
-  return (((int64_t)pg * a.Hkv + g) << a.c.shift) + (t & ((1 << a.c.shift) - 1));
-}
-
-// One side (K or V) of the stage at token t0 into LDS.  Rows past the piece repeat its last one;
-// exponents are read in groups of four rows, which never leave a unit.
-template <int D, bool IS_K>
-__device__ __forceinline__ void issue_stage(const QArgs& a, const Piece& p, int t0, const uint32_t (&off)[IS_K ? 2 : 1][Ring<D>::IPU],
-                                            uint32_t lds, int lane) {
-  typedef Ring<D> R_;
-  typedef Lay<D> L;
-  const uint8_t* codes = IS_K ? a.c.kc : a.c.vc;
-  const uint8_t* exps = IS_K ? a.c.ke : a.c.ve;
-  const int last = p.c1 - 1;
-  int64_t row[4];
-#pragma unroll
-  for (int u = 0; u < 4; ++u) row[u] = unit_row(a, p.b, p.g, min(t0 + 32 * u, last & ~31));
-  const bool whole = t0 + R_::ST <= p.c1;
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int64_t base = uniform64((int64_t)(uintptr_t)(codes + row[u] * D));
-#pragma unroll
-    for (int i = 0; i < R_::IPU; ++i) {
-      uint32_t o = off[IS_K ? u & 1 : 0][i];
-      if (!whole) {  // (offsets are row * D + 16 * chunk, rows counted from the unit)
-        const int most = max(0, last - (t0 + 32 * u));
-        const int at = t0 + 32 * u > last ? (last & 31) : min((int)(o / D), most);
-        o = at * D + o % D;
-      }
-      lds_load16(base, o, lds + (u * R_::IPU + i) * 1024);
-    }
-  }
-  // lane l: rows 4 l .. 4 l + 3 (lanes past the stage repeat)
-  const int l = lane & 31, u = l >> 3;
-  const int64_t r = u == 0 ? row[0] : u == 1 ? row[1] : u == 2 ? row[2] : row[3];
-  lds_load4(exps + r + 4 * (l & 7), lds + R_::KB);
-}
-
-// What a loading wave does: every stage of the workgroup's share, kSlots - 1
-// stages ahead, in STRIDE bytes a slot.
-template <int D, bool IS_K, int SLOTS, int STRIDE>
-__device__ __forceinline__ void load_share(const QArgs& a, Piece p, char* ring) {
-  typedef Ring<D> R_;
-  typedef Lay<D> L;
-  const int lane = threadIdx.x & 63;
-  // offsets of a lane's pieces in a unit; K's order repeats every two units, V's every one
-  uint32_t off[IS_K ? 2 : 1][R_::IPU];
-#pragma unroll
-  for (int u = 0; u < (IS_K ? 2 : 1); ++u)
-#pragma unroll
-    for (int i = 0; i < R_::IPU; ++i) {
-      const int line = (32 * u + i * R_::RPI) / L::LR + lane / 16;
-      const int at = (lane & 15) ^ (IS_K ? L::kkey(line) : L::vkey(line));
-      off[u][i] = (line * L::LR - 32 * u + at / L::CH) * D + 16 * (at % L::CH);
-    }
-  const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(ring));
-  __builtin_amdgcn_s_setprio(3);  // the loads go out before the other waves' arithmetic
-  __builtin_amdgcn_s_waitcnt(0);  // the counts start from zero
-  int issued = 0, t0 = p.c0;
-  bool more = true;
-  auto issue = [&]() {
-    issue_stage<D, IS_K>(a, p, t0, off, base + (issued % SLOTS) * STRIDE, lane);
-    ++issued;
-    t0 += R_::ST;
-    if (t0 >= p.c1) {
-      more = p.next(a);
-      t0 = p.c0;
-    }
-  };
-  for (int s = 0; s < SLOTS - 1 && more; ++s) issue();
-  for (int s = 0; s < issued; ++s) {
-    wait_stage<R_::NI + 1, SLOTS - 2>(issued - 1 - s);
-    lds_sync();  // stage s has landed; every wave is done with stage s - 1
-    if (more) issue();
-  }
-}
-
 // -------------------------------------------------------- partial kernel --
-template <int D>
-struct PartRing {
-  static constexpr int kSlots = D == 128 ? 4 : 8, kStride = 2 * Ring<D>::kSide, kLds = kSlots * kStride;
+template <int D, int RT>
+struct PartShape {
+  static constexpr int TPW = q8_waves(RT).tpw, RW = q8_waves(RT).rw, TW = q8_waves(RT).tw, CW = q8_waves(RT).cw;
+  static constexpr int kCompute = RW * TW, kThreads = (kCompute + 2 * CW) * 64;
+  // waves of a SIMD; two at least, so that a wave's registers are all of one kind
+  static constexpr int kPerEu = kThreads <= 512 ? 2 : 3;
+  static constexpr int kBlock = 2 * Lay<D>::kSide, kRound = TW * kBlock, kLds = 2 * kRound;
+  // blocks of 32 registers (D = 128) that a converting wave has on their way
+  static constexpr int kDepth = 3 * (128 / D);
 };
 
-// A computing wave's tile and blocks.  Wave w runs on SIMD w mod 4, the loading
-// waves on SIMDs 2 and 3 of three that hold ten others: waves of whole tiles
-// are placed first on those, then on 0 and 1 (RT = 6: 2 + 2 half tiles a SIMD).
-struct Role {
-  int tile, block, blocks;
-};
-template <int RT>
-__device__ __forceinline__ Role role(int w) {
-  constexpr int full = q8_full_tiles(RT);
-  constexpr int order[8] = {2, 3, 0, 1, 6, 7, 4, 5};
-  int ahead = 0;  // waves of whole tiles before w
-#pragma unroll
-  for (int k = 0; k < full; ++k) {
-    if (order[k] == w) return {k, 0, 2};
-    ahead += order[k] < w;
-  }
-  return {full + (w - ahead) / 2, (w - ahead) % 2, 1};
-}
-
-// A wave's state: a row tile against the tokens of its blocks.
-template <int D>
+// A computing wave's state: TPW row tiles against the tokens of its blocks.
+template <int D, int TPW>
 struct PartWave {
   static constexpr int DPL = D / 16;
-  Query<D> q[1];
-  int lim;  // last token that the lane's row sees
-  int ctx;  // last token that every row sees
-  float ref, z;
-  floatx4 O[DPL], zt;
-  uint32_t bad;  // a NaN value that not every row sees
-  uint32_t k_lane, v_lane;
+  Query<D> q[TPW];
+  int lim[TPW];  // last token that the lane's row sees
+  float ref[TPW], z[TPW];
+  floatx4 O[TPW][DPL], zt[TPW];
 
-  __device__ __forceinline__ void begin(const QArgs& a, const Piece& p, int tile, int n, int gq) {
-    ctx = p.ctx;
-    bad = 0;
-    k_lane = Lay<D>::k_lane(n, gq);
-    v_lane = Lay<D>::v_lane(n, gq);
-    const int row = tile * 16 + n;
-    load_query<D>(a, p.b, p.g, row, gq, q[0]);
-    lim = row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
-    ref = kNegInf;
-    z = 0.f;
-    zt = floatx4{0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void begin(const QArgs& a, const Piece& p, int tile0, int tiles, int n, int gq) {
 #pragma unroll
-    for (int jd = 0; jd < DPL; ++jd) O[jd] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int x = 0; x < TPW; ++x) {
+      const int row = (tile0 + x) * 16 + n;
+      load_query<D>(a, p.b, p.g, row, gq, q[x]);
+      lim[x] = x < tiles && row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
+      ref[x] = kNegInf;
+      z[x] = 0.f;
+      zt[x] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int jd = 0; jd < DPL; ++jd) O[x][jd] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
   }
 
-  // The block of tokens tb .. tb + 63, block x of the stage at LDS address `at`.  TAIL: some row does not see all of them.
+  // The block of tokens tb .. tb + 63, K and V at LDS addresses k and v (with the lane's offsets).  TAIL: some row
+  // does not see all of them.
   template <bool TAIL>
-  __device__ __forceinline__ void block(const QArgs& a, uint32_t at, int tb, int x, int n, int gq) {
-    typedef Ring<D> R_;
-    const uint32_t kb = at + x * 64 * D, vb = kb + R_::kSide, eb = at + R_::KB + x * 64;
-    const uint32_t ke = lds_read<uint32_t>(eb + 4 * n);
-    const uintx4 ve = lds_read<uintx4>(eb + R_::kSide + 16 * gq);
-    floatx4 S1[1][4];
-    scores<D, 1>(kb + k_lane, ke, q, S1);
-    floatx4(&S)[4] = S1[0];
-    if constexpr (TAIL) {  // the lane's token j is visible iff j <= lim - tb - 16 gq
-#pragma unroll
-      for (int j = 0; j < 16; ++j)
-        if (j > lim - tb - 16 * gq) S[j % 4][j / 4] = kNegInf;
-    }
-    float mx = kNegInf;  // (the maximum that passes NaN on: the other one has every operand canonicalised first)
-#pragma unroll
-    for (int j = 0; j < 16; ++j) mx = __builtin_elementwise_maximum(mx, S[j / 4][j % 4]);
-    mx = rows4_maximum(mx) * a.sl2;
-    if (__any(mx > ref + kRefSlack)) {  // the first block, and seldom after it
-      const float nm = fmaxf(ref, mx);
-      const float al = ref == kNegInf ? 0.f : fast_exp2(ref - nm);
-      z *= al;
-      ref = nm;
-      floatx4 f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = __shfl(al, 4 * gq + i, 64);
-      zt = zt * f;
-#pragma unroll
-      for (int jd = 0; jd < DPL; ++jd) O[jd] = O[jd] * f;
-    }
-    const VPair v0 = read_pair<D>(vb + v_lane, 0);
-    bf16x8 ones;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) ones[j] = static_cast<__bf16>(1.f);
-    const float r = ref == kNegInf ? 0.f : ref;  // no visible token yet: P = 0
-    bf16x8 pz[2], pv[2];
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const float e = fast_exp2(fmaf(S[j % 4][j / 4], a.sl2, -r));
-      z += e;
-      pz[j / 8][j % 8] = static_cast<__bf16>(e);
-      float y = e * q8_unit((ve[j / 4] >> (8 * (j % 4))) & 0xffu);
-      if constexpr (TAIL)
-        if (j > lim - tb - 16 * gq) y = 0.f;  // (an unwritten row's exponent may be anything)
-      pv[j / 8][j % 8] = static_cast<__bf16>(y);
-    }
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) zt = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pz[ks], ones, zt, 0, 0, 0);
-    uint32_t mask[4] = {0u, 0u, 0u, 0u};
+  __device__ __forceinline__ void block(const QArgs& a, uint32_t k, uint32_t v, int tb, int gq) {
+    floatx4 S[TPW][4];
+    scores<D, TPW>(k, q, S);
+    __builtin_amdgcn_sched_barrier(0);
     if constexpr (TAIL) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int o = ctx - tb - 16 * gq - 4 * k;  // tokens 4 k + j, j <= o, are seen by every row
-        mask[k] = o >= 3 ? 0u : o < 0 ? ~0u : ~0u << (8 * (o + 1));
+      for (int x = 0; x < TPW; ++x)
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (16 * tt + i > lim[x] - tb - 4 * gq) S[x][tt][i] = kNegInf;
+    }
+    float mx[TPW];
+    bool grow = false;
+#pragma unroll
+    for (int x = 0; x < TPW; ++x) {
+      float m = kNegInf;  // (the maximum that passes NaN on: the other one has every operand canonicalised first)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) m = __builtin_elementwise_maximum(m, S[x][j / 4][j % 4]);
+      mx[x] = rows4_maximum(m) * a.sl2;
+      grow |= mx[x] > ref[x] + kRefSlack;
+    }
+    if (__any(grow)) {  // the first block, and seldom after it
+#pragma unroll
+      for (int x = 0; x < TPW; ++x) {
+        const float nm = fmaxf(ref[x], mx[x]);
+        const float al = ref[x] == kNegInf ? 0.f : fast_exp2(ref[x] - nm);
+        z[x] *= al;
+        ref[x] = nm;
+        floatx4 f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = __shfl(al, 4 * gq + i, 64);
+        zt[x] = zt[x] * f;
+#pragma unroll
+        for (int jd = 0; jd < DPL; ++jd) O[x][jd] = O[x][jd] * f;
       }
     }
-    bad |= weigh<D, TAIL>(vb + v_lane, pv, v0, mask, O);
+    bf16x8 ones, P[TPW][2];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ones[j] = static_cast<__bf16>(1.f);
+#pragma unroll
+    for (int x = 0; x < TPW; ++x) {
+      const float r = ref[x] == kNegInf ? 0.f : ref[x];  // no visible token yet: P = 0
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = fast_exp2(fmaf(S[x][tt][i], a.sl2, -r));
+          z[x] += e;
+          P[x][tt / 2][4 * (tt % 2) + i] = static_cast<__bf16>(e);
+        }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) zt[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][h], ones, zt[x], 0, 0, 0);
+    }
+    weigh<D, TPW>(v, P, O);
   }
 
-  __device__ __forceinline__ void end(const QArgs& a, size_t rec, int tile, int n, int gq) {
-    const bool nan = __any(bad);
-    const float zz = rows4_sum(z);
-    rec *= 16;
-    if (gq == 0) a.stats[rec + n] = make_float2(ref, zz);
-    // (a negative sum: the rows' values hold a NaN that not every row sees)
-    if (n == 0) *reinterpret_cast<floatx4*>(a.zt + rec + 4 * gq) = nan ? -zt : zt;
-    // position DPL n + jd of a stored row holds column 16 jd + n
-    float* op = a.opart + rec * D;
+  __device__ __forceinline__ void end(const QArgs& a, size_t rec, int tw_count, int tile0, int tiles, int n, int gq) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (tile * 16 + 4 * gq + i < a.R)
+    for (int x = 0; x < TPW; ++x) {
+      if (x >= tiles) break;
+      const size_t at = (rec + x * tw_count) * 16;
+      const float zz = rows4_sum(z[x]);
+      if (gq == 0) a.stats[at + n] = make_float2(ref[x], zz);
+      if (n == 0) *reinterpret_cast<floatx4*>(a.zt + at + 4 * gq) = zt[x];
+      // position DPL n + jd of a stored row holds column 16 jd + n
+      float* op = a.opart + at * D;
 #pragma unroll
-        for (int h = 0; h < DPL / 4; ++h)
-          *reinterpret_cast<float4*>(op + (4 * gq + i) * D + DPL * n + 4 * h) =
-              make_float4(O[4 * h][i], O[4 * h + 1][i], O[4 * h + 2][i], O[4 * h + 3][i]);
+      for (int i = 0; i < 4; ++i)
+        if ((tile0 + x) * 16 + 4 * gq + i < a.R)
+#pragma unroll
+          for (int h = 0; h < DPL / 4; ++h)
+            *reinterpret_cast<float4*>(op + (4 * gq + i) * D + DPL * n + 4 * h) =
+                make_float4(O[x][4 * h][i], O[x][4 * h + 1][i], O[x][4 * h + 2][i], O[x][4 * h + 3][i]);
+    }
   }
-};
-
-template <int RT>
-struct PartShape {
-  static constexpr int kCompute = q8_part_waves(RT), kThreads = (kCompute + 2) * 64;
-  // waves of a SIMD; two at least, so that a wave's registers are all of one kind
-  static constexpr int kPerEu = kCompute <= 6 ? 2 : 3;
 };
 
 template <int D, int RT>
-__global__ void __launch_bounds__((PartShape<RT>::kThreads))
-__attribute__((amdgpu_waves_per_eu(PartShape<RT>::kPerEu, PartShape<RT>::kPerEu))) q8_part_kernel(QArgs a) {
-  typedef Ring<D> R_;
-  typedef PartRing<D> P_;
-  constexpr int kCompute = PartShape<RT>::kCompute;
-  extern __shared__ __align__(1024) char s_ring[];  // [slot][K, V][codes, exponents]
+__global__ void __launch_bounds__((PartShape<D, RT>::kThreads))
+__attribute__((amdgpu_waves_per_eu(PartShape<D, RT>::kPerEu, PartShape<D, RT>::kPerEu))) q8_part_kernel(QArgs a) {
+  typedef PartShape<D, RT> S_;
+  constexpr int TPW = S_::TPW, TW = S_::TW;
+  extern __shared__ __align__(1024) char s_ring[];  // [2][TW][K, V][64][D]
 
   Piece p;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -692,91 +606,78 @@ __attribute__((amdgpu_waves_per_eu(PartShape<RT>::kPerEu, PartShape<RT>::kPerEu)
     for (int b = threadIdx.x; b < a.B; b += 64)
       if (a.ctx_len[b] < 0 || a.ctx_len[b] > a.max_ctx) dev_flag(a.status, PVLM_DEV_RANGE);
   if (!p.first(a)) return;
-  if (w == kCompute) {
-    load_share<D, true, P_::kSlots, P_::kStride>(a, p, s_ring);
-    return;
-  }
-  if (w == kCompute + 1) {
-    load_share<D, false, P_::kSlots, P_::kStride>(a, p, s_ring + R_::kSide);
+  const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_addr(s_ring));
+  if (w >= S_::kCompute) {
+    const int x = w - S_::kCompute;
+    if (x < S_::CW) convert_share<D, TW, S_::CW, S_::kDepth, S_::kRound, S_::kBlock, false>(a, p, x, ring);
+    else convert_share<D, TW, S_::CW, S_::kDepth, S_::kRound, S_::kBlock, true>(a, p, x - S_::CW, ring + Lay<D>::kSide);
     return;
   }
   const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-  const Role my = role<RT>(w);
-  const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_addr(s_ring));
-  int slot = 0;
+  const int tw = w % TW, t_first = w / TW * TPW;  // its blocks, and its first tile
+  const uint32_t k0 = ring + tw * S_::kBlock + Lay<D>::k_lane(n, gq);
+  const uint32_t v0 = ring + tw * S_::kBlock + Lay<D>::kSide + Lay<D>::v_lane(n, gq);
+  uint32_t slot = 0;
   do {
-    const int tile = p.rg * RT + my.tile;  // of the KV head
-    const bool live = tile < a.RTT;
-    PartWave<D> v;
-    v.begin(a, p, tile, n, gq);
-    // the wave's stages whose blocks every row sees whole, then the others (two
+    const int tile0 = p.rg * RT + t_first, tiles = min(RT - t_first, a.RTT - tile0);  // of the wave; further ones are idle
+    PartWave<D, TPW> v;
+    v.begin(a, p, tile0, tiles, n, gq);
+    // the wave's rounds whose block every row sees whole, then the others (two
     // loops with their test at the end: joined, or with the test ahead, the
     // compiler copies all of O in every round)
-    const int nst = __builtin_amdgcn_readfirstlane((p.c1 - p.c0 + R_::ST - 1) / R_::ST);
-    const int last = 64 * (my.block + my.blocks) - 1;  // of the wave's tokens in a stage
-    const int whole = __builtin_amdgcn_readfirstlane(live ? (min(p.c1 - 1, p.ctx) - last - p.c0 + R_::ST) / R_::ST : 0);
-    auto stage = [&]() {
-      lds_sync();
-      const uint32_t at = ring + slot * P_::kStride;
-      slot = slot + 1 == P_::kSlots ? 0 : slot + 1;
-      return at;
-    };
+    const int rounds = __builtin_amdgcn_readfirstlane((p.c1 - p.c0 + 64 * TW - 1) / (64 * TW));
+    const int whole = __builtin_amdgcn_readfirstlane(
+        tiles > 0 ? (min(p.c1 - 1, p.ctx) - (64 * tw + 63) - p.c0 + 64 * TW) / (64 * TW) : 0);
     int s = 0;
     if (whole > 0) {
       do {
-        const uint32_t at = stage();
-        int x = 0;
-        do v.template block<false>(a, at, 0, my.block + x, n, gq);
-        while (++x < my.blocks);
+        lds_sync();
+        v.template block<false>(a, k0 + slot, v0 + slot, 0, gq);
+        slot = S_::kRound - slot;
       } while (++s < whole);
     }
-    if (s < nst) {
+    if (s < rounds) {
       do {
-        const uint32_t at = stage();
-        if (live) {
-          int x = 0;
-          do {
-            const int tb = p.c0 + s * R_::ST + 64 * (my.block + x);
-            if (tb < p.c1) v.template block<true>(a, at, tb, my.block + x, n, gq);
-          } while (++x < my.blocks);
-        }
-      } while (++s < nst);
+        lds_sync();
+        const int tb = p.c0 + 64 * (s * TW + tw);
+        if (tb < p.c1 && tiles > 0) v.template block<true>(a, k0 + slot, v0 + slot, tb, gq);
+        slot = S_::kRound - slot;
+      } while (++s < rounds);
     }
-    if (live) v.end(a, ((size_t)(p.group(a) + blockIdx.x) * RT + my.tile) * 2 + my.block, tile, n, gq);
+    v.end(a, ((size_t)(p.group(a) + blockIdx.x) * RT + t_first) * TW + tw, TW, tile0, tiles, n, gq);
   } while (p.next(a));
 }
 
 // ----------------------------------------------------------- mass kernel --
 // The partial kernel's shares again, every row's log-sum-exp known.
-template <int D>
-struct MassRing {
-  static constexpr int kSlots = D == 128 ? 4 : 8, kStride = Ring<D>::kSide, kLds = kSlots * kStride;
-};
-
-template <int RT>
+template <int D, int RT>
 struct MassShape {
-  static constexpr int TPW = q8_mass_tiles(RT), RW = q8_mass_rows(RT), kCompute = 2 * RW, kThreads = (kCompute + 1) * 64;
+  static constexpr int TPW = q8_mass_waves(RT).tpw, RW = q8_mass_waves(RT).rw, TW = q8_mass_waves(RT).tw;
+  static constexpr int CW = q8_mass_waves(RT).cw, kCompute = RW * TW, kThreads = (kCompute + CW) * 64;
+  static constexpr int kBlock = Lay<D>::kSide, kRound = TW * kBlock, kLds = 2 * kRound;
+  static constexpr int kDepth = 5 * (128 / D);
 };
 
 template <int D, int RT>
-__global__ void __launch_bounds__((MassShape<RT>::kThreads)) __attribute__((amdgpu_waves_per_eu(2, 2)))
+__global__ void __launch_bounds__((MassShape<D, RT>::kThreads)) __attribute__((amdgpu_waves_per_eu(2, 2)))
 q8_mass_kernel(QArgs a) {
-  typedef Ring<D> R_;
-  typedef MassRing<D> P_;
-  constexpr int TPW = MassShape<RT>::TPW, RW = MassShape<RT>::RW, kCompute = MassShape<RT>::kCompute;
-  extern __shared__ __align__(1024) char s_ring[];
+  typedef MassShape<D, RT> S_;
+  constexpr int TPW = S_::TPW, TW = S_::TW;
+  extern __shared__ __align__(1024) char s_ring[];  // [2][TW][64][D]
 
   Piece p;
   if (!p.first(a)) return;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (w == kCompute) {
-    load_share<D, true, P_::kSlots, P_::kStride>(a, p, s_ring);
+  const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_addr(s_ring));
+  if (w >= S_::kCompute) {
+    convert_share<D, TW, S_::CW, S_::kDepth, S_::kRound, S_::kBlock, false>(a, p, w - S_::kCompute, ring);
     return;
   }
   const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-  const int tw = w % 2, rw = w / 2, t_first = rw * TPW;
-  const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_addr(s_ring)), k_lane = Lay<D>::k_lane(n, gq);
-  int slot = 0;
+  const int tw = w % TW, rw = w / TW, t_first = rw * TPW;
+  const uint32_t k0 = ring + tw * S_::kBlock + Lay<D>::k_lane(n, gq);
+  const int token = 16 * (n / 4) + 4 * gq + n % 4;  // of a block, whose sum the lane gets
+  uint32_t slot = 0;
   do {
     const int tiles = min(RT, a.RTT - p.rg * RT);
     const Holders h = holders(a, p.per, p.before, p.b, p.g * a.RG + p.rg, p.ctx);
@@ -793,22 +694,21 @@ q8_mass_kernel(QArgs a) {
     }
     tile_lse<RT, TPW>(a, h, t_first, tiles, real, n, gq, lse);
     const int vis_all = min(p.c1 - 1, p.ctx);
-    float* mp = a.mpart + ((size_t)p.group(a) * RW + rw) * a.c.n_cap;
-    for (int t0 = p.c0; t0 < p.c1; t0 += R_::ST) {
+    float* mp = a.mpart + ((size_t)p.group(a) * S_::RW + rw) * a.c.n_cap;
+    for (int t0 = p.c0; t0 < p.c1; t0 += 64 * TW) {
       lds_sync();
-      const uint32_t at = ring + slot * P_::kStride;
-      slot = slot + 1 == P_::kSlots ? 0 : slot + 1;
+      const uint32_t k = k0 + slot;
+      slot = S_::kRound - slot;
       const int tb = t0 + 64 * tw;
       if (__builtin_amdgcn_readfirstlane(tb - p.c1) >= 0) continue;
-      const uint32_t ke = lds_read<uint32_t>(at + R_::KB + 64 * tw + 4 * n);
       floatx4 S[TPW][4];
-      scores<D, TPW>(at + tw * 64 * D + k_lane, ke, q, S);
+      scores<D, TPW>(k, q, S);
       if (__builtin_amdgcn_readfirstlane(tb + 63 - vis_all) > 0) {
 #pragma unroll
         for (int x = 0; x < TPW; ++x)
 #pragma unroll
           for (int j = 0; j < 16; ++j)
-            if (j > lim[x] - tb - 16 * gq) S[x][j % 4][j / 4] = kNegInf;
+            if (16 * (j / 4) + j % 4 > lim[x] - tb - 4 * gq) S[x][j / 4][j % 4] = kNegInf;
       }
       // (NaN scores of padding rows, whose q is a real row's, make a token's sum NaN that the real row makes so)
       float sum[16];
@@ -816,11 +716,11 @@ q8_mass_kernel(QArgs a) {
       for (int x = 0; x < TPW; ++x)
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const float e = fast_exp2(fmaf(S[x][j % 4][j / 4], a.sl2, -lse[x]));
+          const float e = fast_exp2(fmaf(S[x][j / 4][j % 4], a.sl2, -lse[x]));
           sum[j] = x ? sum[j] + e : e;
         }
       const float m = row_sums(sum, lane);
-      if (tb + lane < p.c1) mp[tb + lane] = m;
+      if (tb + token < p.c1) mp[tb + token] = m;
     }
   } while (p.next(a));
 }
@@ -852,7 +752,7 @@ __device__ __forceinline__ void join(RowSum& a, float m, float z, float zt, floa
 
 template <int D, int RT, int WPR>
 __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_row)[D / 4]) {
-  constexpr int LPR = D / 4, SG = 64 / LPR, kU = 8;
+  constexpr int LPR = D / 4, SG = 64 / LPR, TW = q8_waves(RT).tw, CW = q8_waves(RT).cw, kU = 8;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane % LPR;
   const int id = wg * (kFinWaves / WPR) + w / WPR;  // (fewer than 2^22 rows)
   const bool row_here = id < a.B * a.Hkv * a.R;
@@ -867,17 +767,22 @@ __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_
     ctx = s_.ctx;
     const int rg = row / (16 * RT), tile = row / 16 - rg * RT;
     const Holders h = holders(a, s_.per, s_.before, b, g * a.RG + rg, s_.ctx);
-    const int tw = tile < q8_full_tiles(RT) ? 1 : 2;  // records of a tile in each of the group's
-    const size_t rec = ((size_t)h.rec * RT + tile) * 2 * 16 + row % 16;
-    const int cnt = h.count * tw, sets = SG * WPR;
+    const size_t rec = ((size_t)h.rec * RT + tile) * TW * 16 + row % 16;
+    const int cnt = h.count * TW, sets = SG * WPR;
     for (int s0 = lane / LPR + SG * (w % WPR); s0 < cnt; s0 += kU * sets) {
       float2 v[kU];
       float zt[kU];
+      uint32_t nan[kU];
       floatx4 o[kU];
 #pragma unroll
       for (int j = 0; j < kU; ++j) {
         const int s = min(s0 + j * sets, cnt - 1);
-        const size_t i = rec + (size_t)(tw == 1 ? 2 * RT * s : s / 2 * RT * 2 + s % 2) * 16;
+        const size_t i = rec + (size_t)(s / TW * RT * TW + s % TW) * 16;
+#pragma unroll
+        for (int c = 0; c < CW; ++c) {
+          const uint32_t x = a.nan[(h.rec + s / TW) * CW + c];
+          nan[j] = c ? nan[j] | x : x;
+        }
         v[j] = a.stats[i];
         zt[j] = a.zt[i];
         o[j] = *reinterpret_cast<const floatx4*>(a.opart + i * D + 4 * col);
@@ -895,8 +800,8 @@ __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_
         if (s0 + j * sets < cnt && v[j].y != 0.f) {  // (0: nothing that the row sees)
           const float e = fast_exp2(v[j].x - r);
           t.z = fmaf(v[j].y, e, t.z);
-          t.zt = fmaf(fabsf(zt[j]), e, t.zt);
-          t.nan |= zt[j] < 0.f;
+          t.zt = fmaf(zt[j], e, t.zt);
+          t.nan |= nan[j] != 0;
           t.o = t.o + o[j] * e;
         }
     }
@@ -922,7 +827,8 @@ __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_
   constexpr int DPL = D / 16;
   if (t.nan) {  // the values past the context that the row sees, whose NaN codes counted as 0
     for (int j = ctx + 1; j <= ctx + tt; ++j) {
-      const int64_t r = unit_row(a, b, g, j & ~31) + (j & 31);
+      bool flagged_before;  // by the partial kernel
+      const int64_t r = unit_row(a, b, g, j & ~31, flagged_before) + (j & 31);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int c = 4 * col + k;
@@ -944,7 +850,7 @@ __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_
 // order (0 past the sequence).
 template <int RT>
 __device__ __forceinline__ void sum_mass(const QArgs& a, int id) {
-  const int P = a.HR * q8_mass_rows(RT);
+  const int P = a.HR * q8_mass_waves(RT).rw;
   const int b = id / a.mass_per;
   const int64_t t0 = (int64_t)(id - b * a.mass_per) * a.mass_rows;
   const int N = clamp_ctx(a, a.ctx_len[b]) + a.T;
@@ -983,8 +889,8 @@ struct QKernels {
 
 template <int D, int RT>
 QKernels kernels() {
-  return {q8_part_kernel<D, RT>, q8_mass_kernel<D, RT>, {q8_finish_kernel<D, RT, 1>, q8_finish_kernel<D, RT, kFinWaves>}, PartShape<RT>::kThreads,
-          MassShape<RT>::kThreads, PartRing<D>::kLds, MassRing<D>::kLds};
+  return {q8_part_kernel<D, RT>, q8_mass_kernel<D, RT>, {q8_finish_kernel<D, RT, 1>, q8_finish_kernel<D, RT, kFinWaves>}, PartShape<D, RT>::kThreads,
+          MassShape<D, RT>::kThreads, PartShape<D, RT>::kLds, MassShape<D, RT>::kLds};
 }
 template <int D>
 QKernels pick(int RT) {
@@ -997,7 +903,8 @@ QKernels pick(int RT) {
     case 6: return kernels<D, 6>();
     case 7: return kernels<D, 7>();
     case 8: return kernels<D, 8>();
-    default: return kernels<D, 9>();
+    case 9: return kernels<D, 9>();
+    default: return kernels<D, 10>();
   }
 }
 
@@ -1038,6 +945,7 @@ pvlm_status verify_q8_run(int B, int T, int Hq, int Hkv, int D, int64_t max_ctx,
   a.mpart = reinterpret_cast<float*>(wsb + p.off_mpart);
   a.stats = reinterpret_cast<float2*>(wsb + p.off_stats);
   a.zt = reinterpret_cast<float*>(wsb + p.off_zt);
+  a.nan = reinterpret_cast<uint32_t*>(wsb + p.off_nan);
   a.opart = reinterpret_cast<float*>(wsb + p.off_opart);
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
@@ -1056,7 +964,7 @@ pvlm_status verify_q8_run(int B, int T, int Hq, int Hkv, int D, int64_t max_ctx,
     PVLM_LAUNCHED();
   }
   // a wave joins 16 records (8 at D = 64: 32) in one round of loads
-  const bool wide = p.recs * 2 > (size_t)B * a.HR * 2 * 16;
+  const bool wide = p.recs * q8_waves(p.RT).tw > (size_t)B * a.HR * 2 * 16;
   const int per_wg = wide ? 1 : kFinWaves, row_count = B * Hkv * p.R;
   hipLaunchKernelGGL(k.finish[wide], dim3(a.mass_wgs + (row_count + per_wg - 1) / per_wg), dim3(kFinThreads), 0, stream,
                      a);

@@ -14,26 +14,34 @@ namespace pvlm {
 // group and begin the next.  The shares follow from the lengths on the device.
 constexpr int kQUnit = 32;
 constexpr int kQMinUnits = 2;  // least share: one 64-token block
-constexpr int kQMaxRT = 9;     // 16-row tiles of a workgroup
+constexpr int kQMaxRT = 10;    // 16-row tiles of a workgroup
 
-// The partial kernel's computing waves: one for each row tile and stage (two
-// blocks of 64 tokens), and one for each block where there are waves left: three
-// waves a SIMD with the two that load.  Tiles 0 .. full - 1 have one wave, the
-// others two, each with records of its own.
-constexpr int kQWaves = 10;
-constexpr int q8_full_tiles(int RT) { return RT <= kQWaves / 2 ? 0 : 2 * RT - kQWaves; }
-constexpr int q8_part_waves(int RT) { return 2 * RT - q8_full_tiles(RT); }
-// The mass kernel's: up to three tiles a wave, which convert a block's keys and
-// sum their rows together, and one wave for each block.
-constexpr int q8_mass_rows(int RT) { return (RT + 2) / 3; }
-constexpr int q8_mass_tiles(int RT) { return (RT + q8_mass_rows(RT) - 1) / q8_mass_rows(RT); }
+// How a workgroup's computing waves share its row tiles and the blocks of 64
+// tokens: TPW tiles a wave, RW waves for the tiles, TW of each for TW blocks at a
+// time.  Up to five tiles a wave each; from six on two tiles a wave, which read a
+// block once for both (LDS would bound it, 9 tiles: 32 KB a tile and block).
+// CW more waves convert the blocks of K and CW those of V, one each of a round's
+// TW blocks or all; twelve waves, three a SIMD, at most.
+struct QWaves {
+  int tpw, rw, tw, cw;
+};
+constexpr QWaves q8_waves(int RT) {
+  const int tpw = RT <= 5 ? 1 : 2, rw = (RT + tpw - 1) / tpw;
+  return {tpw, rw, 2, rw <= 4 ? 2 : 1};
+}
+// The mass kernel's, with K alone: up to three tiles a wave, which sum their rows
+// together, and two waves a SIMD.
+constexpr QWaves q8_mass_waves(int RT) {
+  const int rw = (RT + 2) / 3, tw = rw <= 3 ? 2 : 1;
+  return {(RT + rw - 1) / rw, rw, tw, tw};
+}
 
 struct QSplit {
   int G, R;         // query heads of a KV head, and its query rows G * T
   int RTT, RG, RT;  // their 16-row tiles, the workgroups that share them, and the tiles of one
   int wgs;          // workgroups of the partial and mass kernels
   size_t recs;      // partial results of RT tiles: group x of workgroup w is number x + w
-  size_t off_mpart, off_stats, off_zt, off_opart, bytes;
+  size_t off_mpart, off_stats, off_zt, off_nan, off_opart, bytes;
 };
 
 inline pvlm_status check_verify_q8(int B, int T, int Hq, int Hkv, int D, int64_t n_cap, int64_t max_ctx) {
@@ -42,9 +50,9 @@ inline pvlm_status check_verify_q8(int B, int T, int Hq, int Hkv, int D, int64_t
   if (n_cap % 32 != 0) return PVLM_ERR_SHAPE;
   // the finish kernel has 64 work-items for each row, in one launch of fewer than 2^32
   if ((int64_t)B * Hq * T > ((int64_t)1 << 22)) return PVLM_ERR_SHAPE;
-  // units are counted in 32 bits (at most 5 workgroups share 40 tiles)
+  // units are counted in 32 bits (at most 4 workgroups share 40 tiles)
   const int64_t units = (max_ctx + T + kQUnit - 1) / kQUnit;
-  return (int64_t)B * Hkv * 5 * units > INT32_MAX - 65536 ? PVLM_ERR_SHAPE : PVLM_OK;
+  return (int64_t)B * Hkv * 4 * units > INT32_MAX - 65536 ? PVLM_ERR_SHAPE : PVLM_OK;
 }
 
 // The plan for arguments that check_verify_q8 takes, on `cus` compute units (a
@@ -62,11 +70,12 @@ inline void split_verify_q8(int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
   const int64_t shares = (units + kQMinUnits - 1) / kQMinUnits;
   p->wgs = (int)(shares < cus ? shares : cus);
   p->recs = (size_t)(groups + p->wgs);
-  const size_t rows = p->recs * p->RT * 2 * 16;
+  const size_t rows = p->recs * p->RT * q8_waves(p->RT).tw * 16;
   p->off_mpart = kSyncRegion;  // (the region at the start is other calls')
-  p->off_stats = align_up(p->off_mpart + 4 * (size_t)groups * q8_mass_rows(p->RT) * n_cap, 256);
+  p->off_stats = align_up(p->off_mpart + 4 * (size_t)groups * q8_mass_waves(p->RT).rw * n_cap, 256);
   p->off_zt = align_up(p->off_stats + 8 * rows, 256);
-  p->off_opart = align_up(p->off_zt + 4 * rows, 256);
+  p->off_nan = align_up(p->off_zt + 4 * rows, 256);
+  p->off_opart = align_up(p->off_nan + 4 * p->recs * q8_waves(p->RT).cw, 256);
   p->bytes = align_up(p->off_opart + 4 * rows * D, 256);
 }
 

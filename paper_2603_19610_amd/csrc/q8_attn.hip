@@ -201,10 +201,10 @@ __device__ __forceinline__ int64_t unit_row(const QArgs& a, int b, int g, int t,
 }
 
 // LDS holds a block of 64 tokens as bf16 rows, of K and of V: 16-byte chunk c
-// of row r lies at chunk c ^ swz(r) of the row.  swz permutes the bits of r mod 16
-// so that over the 64 banks (256 bytes: one row, or two of D = 64) 16 rows' same
-// chunk, and 8 rows' same two chunks, are apart: what the reads of K and V take
-// at a time.  (r mod CH in its place: a third of all LDS cycles were conflicts.)
+// of row r lies at chunk c ^ swz(r) of the row.  128 bytes are read or written at
+// a time: of K eight rows' same chunk, of V four rows' same two chunks, and two
+// rows' even chunks when they are filled.  swz places the bits of r so that each
+// of these falls on distinct banks.
 template <int D>
 struct Lay {
   static constexpr int CH = D / 8, kSide = 64 * D * 2;  // chunks of a row, bytes of a block's K or V
@@ -212,10 +212,7 @@ struct Lay {
   // 4 ks chunks and 16 tt rows on), and V's 8 bytes of row 4 gq + n / 4 (32 jd
   // bytes, and 16 and 32 rows on).  Chunks differ by an exclusive or of the
   // address: blocks start at multiples of 256 bytes.
-  static constexpr __host__ __device__ int swz(int r) {
-    const int m = D == 64 ? (r & 15) >> 1 : r & 15;
-    return ((m << 1) | (m >> (D == 64 ? 2 : 3))) & (CH - 1);
-  }
+  static constexpr __host__ __device__ int swz(int r) { return (((r << 1) & 6) | ((r >> 2) & 1) | (r & 8)) & (CH - 1); }
   static __device__ __forceinline__ uint32_t k_lane(int n, int gq) { return n * D * 2 + ((gq ^ swz(n)) << 4); }
   static __device__ __forceinline__ uint32_t k_at(uint32_t lane, int ks, int tt) { return (lane ^ (ks << 6)) + tt * 32 * D; }
   static __device__ __forceinline__ uint32_t v_lane(int n, int gq) {
@@ -256,12 +253,17 @@ __device__ __forceinline__ bf16x8 to_bf16(uint32_t lo, uint32_t hi, float unit) 
 template <int D, int TW, int CW, int DEPTH, int ROUND, int BLOCK, bool IS_V>
 __device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first, uint32_t ring) {
   constexpr int PER = TW / CW;  // blocks of a round
-  constexpr int NI = D / 16;  // lanes of a row, and rows of a lane: consecutive ones, whose exponents it reads at once
+  // lanes of a row, and rows of a lane: consecutive ones, whose exponents it reads
+  // at once.  With eight lanes a row, the upper four take the rows in the order
+  // i ^ 4: what eight lanes write at a time is then two rows' (see Lay).
+  constexpr int NI = D / 16;
   typedef uint32_t Exps __attribute__((ext_vector_type(NI / 4)));
   const uint8_t* codes = IS_V ? a.c.vc : a.c.kc;
   const uint8_t* exps = IS_V ? a.c.ve : a.c.ke;
   const int lane = threadIdx.x & 63, c = lane % NI, row0 = NI * (lane / NI);
-  const uint32_t lds0 = row0 * D * 2 + (((2 * c) ^ Lay<D>::swz(row0)) << 4);
+  const int flip = c & 4;  // (of four lanes a row: 0)
+  const uint32_t lds0 = (row0 + flip) * D * 2 + (((2 * c) ^ Lay<D>::swz(row0 + flip)) << 4);
+  const int lds_step = -2 * flip * D * 2;  // to the rows of i >= 4, past the 4 rows of i
 
   uintx4 v[DEPTH][NI];
   Exps e[DEPTH];
@@ -279,7 +281,7 @@ __device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first
     const int64_t r = row0 < 32 ? u0 + row0 : u1 + (row0 - 32);
     const uint8_t* src = codes + r * D + 16 * c;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) v[k][i] = *reinterpret_cast<const uintx4*>(src + i * D);
+    for (int i = 0; i < NI; ++i) v[k][i] = *reinterpret_cast<const uintx4*>(src + (i < 4 ? flip : -flip) * D + i * D);
     e[k] = *reinterpret_cast<const Exps*>(exps + r);
     if (!more) return;
     tb[k] = t0;
@@ -304,10 +306,15 @@ __device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first
   uint32_t bad = 0;
   auto convert = [&](int k, uint32_t at) {
     const int whole = IS_V ? min(c1[k] - 1, ctx[k]) : c1[k] - 1;
+    if constexpr (NI == 8) {
+      const uint32_t x = e[k][0];
+      e[k][0] = flip ? e[k][1] : x;
+      e[k][1] = flip ? x : e[k][1];
+    }
     if (__builtin_amdgcn_readfirstlane(tb[k] + 63 - whole) > 0) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int t = tb[k] + row0 + i;
+        const int t = tb[k] + row0 + (i ^ flip);
         if (t >= c1[k]) {
           v[k][i] = uintx4{0, 0, 0, 0};
           e[k][i / 4] = (e[k][i / 4] & ~(0xffu << 8 * (i % 4))) | 127u << 8 * (i % 4);
@@ -324,8 +331,9 @@ __device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const float unit = q8_unit((e[k][i / 4] >> (8 * (i % 4))) & 0xffu);
-      lds_write((at ^ (Lay<D>::swz(i) << 4)) + i * D * 2, to_bf16(v[k][i][0], v[k][i][1], unit));
-      lds_write((at ^ ((Lay<D>::swz(i) ^ 1) << 4)) + i * D * 2, to_bf16(v[k][i][2], v[k][i][3], unit));
+      const uint32_t row = at + (i < 4 ? 0 : lds_step);  // (swz(i ^ 4) = swz(i) ^ swz(4))
+      lds_write((row ^ (Lay<D>::swz(i) << 4)) + i * D * 2, to_bf16(v[k][i][0], v[k][i][1], unit));
+      lds_write((row ^ ((Lay<D>::swz(i) ^ 1) << 4)) + i * D * 2, to_bf16(v[k][i][2], v[k][i][3], unit));
     }
     if (IS_V && last_of[k] >= 0) {
       const bool any = __any(bad);
@@ -373,41 +381,55 @@ __device__ __forceinline__ float rows4_maximum(float x) {
   return __builtin_elementwise_maximum(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+// AHEAD operand reads of LDS are under way while the matrix instructions of
+// earlier ones run (the compiler, left to itself, waits for each read alone).
 // Scores of a block (its K at LDS address k plus the lane's offset) against a wave's row tiles.
-template <int D, int TPW>
+template <int D, int TPW, int AHEAD>
 __device__ __forceinline__ void scores(uint32_t k, const Query<D> (&q)[TPW], floatx4 (&S)[TPW][4]) {
+  constexpr int N = D / 8;  // operands: chunk 4 ks + gq of the rows of tile tt, number 4 ks + tt
+  bf16x8 kr[AHEAD];
+#pragma unroll
+  for (int j = 0; j < AHEAD - 1; ++j) kr[j] = lds_read<bf16x8>(Lay<D>::k_at(k, j / 4, j % 4));
 #pragma unroll
   for (int x = 0; x < TPW; ++x)
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) S[x][tt] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int ks = 0; ks < D / 32; ++ks)
+  for (int j = 0; j < N; ++j) {
+    const int m = j + AHEAD - 1;
+    if (m < N) kr[m % AHEAD] = lds_read<bf16x8>(Lay<D>::k_at(k, m / 4, m % 4));
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int tt = 0; tt < 4; ++tt) {
-      const bf16x8 kr = lds_read<bf16x8>(Lay<D>::k_at(k, ks, tt));
-#pragma unroll
-      for (int x = 0; x < TPW; ++x) S[x][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr, q[x].s[ks], S[x][tt], 0, 0, 0);
-    }
+    for (int x = 0; x < TPW; ++x)
+      S[x][j % 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr[j % AHEAD], q[x].s[j / 4], S[x][j % 4], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
 
-// O += P . V over a block; P[x][h] holds tokens 32 h + 4 gq + {0..3, 16..19}.
+// O += P . V over a block; P[h] holds tokens 32 h + 4 gq + {0..3, 16..19}.
 // Transposed LDS reads: each 16 lanes fetch 16 columns of four rows (lane n the
 // 8 bytes of row n / 4, columns 4 (n mod 4) on) and lane n receives column n.
-template <int D, int TPW>
-__device__ __forceinline__ void weigh(uint32_t v, const bf16x8 (&P)[TPW][2], floatx4 (&O)[TPW][D / 16]) {
+template <int D, int AHEAD>
+__device__ __forceinline__ void weigh(uint32_t v, const bf16x8 (&P)[2], floatx4 (&O)[D / 16]) {
   typedef short s4 __attribute__((ext_vector_type(4)));
   typedef short s8 __attribute__((ext_vector_type(8)));
   typedef __attribute__((address_space(3))) s4* lds_s4;
+  constexpr int N = D / 8;  // operands: columns 16 jd + n of tokens 32 h on, number 2 jd + h
+  s4 lo[AHEAD], hi[AHEAD];
+  auto read = [&](int j) {
+    lo[j % AHEAD] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)Lay<D>::v_at(v, j / 2, j % 2 * 32));
+    hi[j % AHEAD] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)Lay<D>::v_at(v, j / 2, j % 2 * 32 + 16));
+  };
 #pragma unroll
-  for (int jd = 0; jd < D / 16; ++jd)
+  for (int j = 0; j < AHEAD - 1; ++j) read(j);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)Lay<D>::v_at(v, jd, 32 * h));
-      const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)Lay<D>::v_at(v, jd, 32 * h + 16));
-      const bf16x8 b = __builtin_bit_cast(bf16x8, (s8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-      for (int x = 0; x < TPW; ++x) O[x][jd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][h], b, O[x][jd], 0, 0, 0);
-    }
+  for (int j = 0; j < N; ++j) {
+    if (j + AHEAD - 1 < N) read(j + AHEAD - 1);
+    __builtin_amdgcn_sched_barrier(0);
+    const bf16x8 b = __builtin_bit_cast(bf16x8, (s8)__builtin_shufflevector(lo[j % AHEAD], hi[j % AHEAD], 0, 1, 2, 3, 4, 5, 6, 7));
+    O[j / 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[j % 2], b, O[j / 2], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
 
 // (maximum, sum) of two sets of scores.  A sum of 0 belongs to one of which the
@@ -479,8 +501,8 @@ __device__ __forceinline__ float row_sums(const float (&p)[16], int lane) {
 // -------------------------------------------------------- partial kernel --
 template <int D, int RT>
 struct PartShape {
-  static constexpr int TPW = q8_waves(RT).tpw, RW = q8_waves(RT).rw, TW = q8_waves(RT).tw, CW = q8_waves(RT).cw;
-  static constexpr int kCompute = RW * TW, kThreads = (kCompute + 2 * CW) * 64;
+  static constexpr int TW = q8_waves(RT).tw, CW = q8_waves(RT).cw;
+  static constexpr int kCompute = RT * TW, kThreads = (kCompute + 2 * CW) * 64;
   // waves of a SIMD; two at least, so that a wave's registers are all of one kind
   static constexpr int kPerEu = kThreads <= 512 ? 2 : 3;
   static constexpr int kBlock = 2 * Lay<D>::kSide, kRound = TW * kBlock, kLds = 2 * kRound;
@@ -488,108 +510,81 @@ struct PartShape {
   static constexpr int kDepth = 3 * (128 / D);
 };
 
-// A computing wave's state: TPW row tiles against the tokens of its blocks.
-template <int D, int TPW>
+// A computing wave's state: a row tile against the tokens of its blocks.
+template <int D>
 struct PartWave {
-  static constexpr int DPL = D / 16;
-  Query<D> q[TPW];
-  int lim[TPW];  // last token that the lane's row sees
-  float ref[TPW], z[TPW];
-  floatx4 O[TPW][DPL], zt[TPW];
+  static constexpr int DPL = D / 16, AHEAD = 8;
+  Query<D> q[1];
+  int lim;  // last token that the lane's row sees
+  float ref, z;
+  floatx4 O[DPL], zt;
 
-  __device__ __forceinline__ void begin(const QArgs& a, const Piece& p, int tile0, int tiles, int n, int gq) {
+  __device__ __forceinline__ void begin(const QArgs& a, const Piece& p, int tile, bool here, int n, int gq) {
+    const int row = tile * 16 + n;
+    load_query<D>(a, p.b, p.g, row, gq, q[0]);
+    lim = here && row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
+    ref = kNegInf;
+    z = 0.f;
+    zt = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int x = 0; x < TPW; ++x) {
-      const int row = (tile0 + x) * 16 + n;
-      load_query<D>(a, p.b, p.g, row, gq, q[x]);
-      lim[x] = x < tiles && row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
-      ref[x] = kNegInf;
-      z[x] = 0.f;
-      zt[x] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int jd = 0; jd < DPL; ++jd) O[x][jd] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int jd = 0; jd < DPL; ++jd) O[jd] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
 
   // The block of tokens tb .. tb + 63, K and V at LDS addresses k and v (with the lane's offsets).  TAIL: some row
   // does not see all of them.
   template <bool TAIL>
   __device__ __forceinline__ void block(const QArgs& a, uint32_t k, uint32_t v, int tb, int gq) {
-    floatx4 S[TPW][4];
-    scores<D, TPW>(k, q, S);
-    __builtin_amdgcn_sched_barrier(0);
+    floatx4 S[1][4];
+    scores<D, 1, AHEAD>(k, q, S);
     if constexpr (TAIL) {
 #pragma unroll
-      for (int x = 0; x < TPW; ++x)
-#pragma unroll
-        for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (16 * tt + i > lim[x] - tb - 4 * gq) S[x][tt][i] = kNegInf;
+      for (int j = 0; j < 16; ++j)
+        if (16 * (j / 4) + j % 4 > lim - tb - 4 * gq) S[0][j / 4][j % 4] = kNegInf;
     }
-    float mx[TPW];
-    bool grow = false;
+    float m = kNegInf;  // (the maximum that passes NaN on: the other one has every operand canonicalised first)
 #pragma unroll
-    for (int x = 0; x < TPW; ++x) {
-      float m = kNegInf;  // (the maximum that passes NaN on: the other one has every operand canonicalised first)
+    for (int j = 0; j < 16; ++j) m = __builtin_elementwise_maximum(m, S[0][j / 4][j % 4]);
+    m = rows4_maximum(m) * a.sl2;
+    if (__any(m > ref + kRefSlack)) {  // the first block, and seldom after it
+      const float nm = fmaxf(ref, m);
+      const float al = ref == kNegInf ? 0.f : fast_exp2(ref - nm);
+      z *= al;
+      ref = nm;
+      floatx4 f;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) m = __builtin_elementwise_maximum(m, S[x][j / 4][j % 4]);
-      mx[x] = rows4_maximum(m) * a.sl2;
-      grow |= mx[x] > ref[x] + kRefSlack;
+      for (int i = 0; i < 4; ++i) f[i] = __shfl(al, 4 * gq + i, 64);
+      zt = zt * f;
+#pragma unroll
+      for (int jd = 0; jd < DPL; ++jd) O[jd] = O[jd] * f;
     }
-    if (__any(grow)) {  // the first block, and seldom after it
-#pragma unroll
-      for (int x = 0; x < TPW; ++x) {
-        const float nm = fmaxf(ref[x], mx[x]);
-        const float al = ref[x] == kNegInf ? 0.f : fast_exp2(ref[x] - nm);
-        z[x] *= al;
-        ref[x] = nm;
-        floatx4 f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = __shfl(al, 4 * gq + i, 64);
-        zt[x] = zt[x] * f;
-#pragma unroll
-        for (int jd = 0; jd < DPL; ++jd) O[x][jd] = O[x][jd] * f;
-      }
-    }
-    bf16x8 ones, P[TPW][2];
+    bf16x8 ones, P[2];
 #pragma unroll
     for (int j = 0; j < 8; ++j) ones[j] = static_cast<__bf16>(1.f);
+    const float r = ref == kNegInf ? 0.f : ref;  // no visible token yet: P = 0
 #pragma unroll
-    for (int x = 0; x < TPW; ++x) {
-      const float r = ref[x] == kNegInf ? 0.f : ref[x];  // no visible token yet: P = 0
-#pragma unroll
-      for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e = fast_exp2(fmaf(S[x][tt][i], a.sl2, -r));
-          z[x] += e;
-          P[x][tt / 2][4 * (tt % 2) + i] = static_cast<__bf16>(e);
-        }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) zt[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][h], ones, zt[x], 0, 0, 0);
+    for (int j = 0; j < 16; ++j) {
+      const float e = fast_exp2(fmaf(S[0][j / 4][j % 4], a.sl2, -r));
+      z += e;
+      P[j / 8][j % 8] = static_cast<__bf16>(e);
     }
-    weigh<D, TPW>(v, P, O);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) zt = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[h], ones, zt, 0, 0, 0);
+    weigh<D, AHEAD>(v, P, O);
   }
 
-  __device__ __forceinline__ void end(const QArgs& a, size_t rec, int tw_count, int tile0, int tiles, int n, int gq) {
+  __device__ __forceinline__ void end(const QArgs& a, size_t rec, int tile, int n, int gq) {
+    const float zz = rows4_sum(z);
+    if (gq == 0) a.stats[rec * 16 + n] = make_float2(ref, zz);
+    if (n == 0) *reinterpret_cast<floatx4*>(a.zt + rec * 16 + 4 * gq) = zt;
+    // position DPL n + jd of a stored row holds column 16 jd + n
+    float* op = a.opart + rec * 16 * D;
 #pragma unroll
-    for (int x = 0; x < TPW; ++x) {
-      if (x >= tiles) break;
-      const size_t at = (rec + x * tw_count) * 16;
-      const float zz = rows4_sum(z[x]);
-      if (gq == 0) a.stats[at + n] = make_float2(ref[x], zz);
-      if (n == 0) *reinterpret_cast<floatx4*>(a.zt + at + 4 * gq) = zt[x];
-      // position DPL n + jd of a stored row holds column 16 jd + n
-      float* op = a.opart + at * D;
+    for (int i = 0; i < 4; ++i)
+      if (tile * 16 + 4 * gq + i < a.R)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if ((tile0 + x) * 16 + 4 * gq + i < a.R)
-#pragma unroll
-          for (int h = 0; h < DPL / 4; ++h)
-            *reinterpret_cast<float4*>(op + (4 * gq + i) * D + DPL * n + 4 * h) =
-                make_float4(O[x][4 * h][i], O[x][4 * h + 1][i], O[x][4 * h + 2][i], O[x][4 * h + 3][i]);
-    }
+        for (int h = 0; h < DPL / 4; ++h)
+          *reinterpret_cast<float4*>(op + (4 * gq + i) * D + DPL * n + 4 * h) =
+              make_float4(O[4 * h][i], O[4 * h + 1][i], O[4 * h + 2][i], O[4 * h + 3][i]);
   }
 };
 
@@ -597,7 +592,7 @@ template <int D, int RT>
 __global__ void __launch_bounds__((PartShape<D, RT>::kThreads))
 __attribute__((amdgpu_waves_per_eu(PartShape<D, RT>::kPerEu, PartShape<D, RT>::kPerEu))) q8_part_kernel(QArgs a) {
   typedef PartShape<D, RT> S_;
-  constexpr int TPW = S_::TPW, TW = S_::TW;
+  constexpr int TW = S_::TW;
   extern __shared__ __align__(1024) char s_ring[];  // [2][TW][K, V][64][D]
 
   Piece p;
@@ -614,20 +609,21 @@ __attribute__((amdgpu_waves_per_eu(PartShape<D, RT>::kPerEu, PartShape<D, RT>::k
     return;
   }
   const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-  const int tw = w % TW, t_first = w / TW * TPW;  // its blocks, and its first tile
+  const int tw = w % TW, tile = w / TW;  // its blocks, and its tile
   const uint32_t k0 = ring + tw * S_::kBlock + Lay<D>::k_lane(n, gq);
   const uint32_t v0 = ring + tw * S_::kBlock + Lay<D>::kSide + Lay<D>::v_lane(n, gq);
   uint32_t slot = 0;
   do {
-    const int tile0 = p.rg * RT + t_first, tiles = min(RT - t_first, a.RTT - tile0);  // of the wave; further ones are idle
-    PartWave<D, TPW> v;
-    v.begin(a, p, tile0, tiles, n, gq);
+    const int tile_g = p.rg * RT + tile;  // of the KV head's; one past its rows is idle
+    const bool here = tile_g < a.RTT;
+    PartWave<D> v;
+    v.begin(a, p, tile_g, here, n, gq);
     // the wave's rounds whose block every row sees whole, then the others (two
     // loops with their test at the end: joined, or with the test ahead, the
     // compiler copies all of O in every round)
     const int rounds = __builtin_amdgcn_readfirstlane((p.c1 - p.c0 + 64 * TW - 1) / (64 * TW));
     const int whole = __builtin_amdgcn_readfirstlane(
-        tiles > 0 ? (min(p.c1 - 1, p.ctx) - (64 * tw + 63) - p.c0 + 64 * TW) / (64 * TW) : 0);
+        here ? (min(p.c1 - 1, p.ctx) - (64 * tw + 63) - p.c0 + 64 * TW) / (64 * TW) : 0);
     int s = 0;
     if (whole > 0) {
       do {
@@ -640,11 +636,11 @@ __attribute__((amdgpu_waves_per_eu(PartShape<D, RT>::kPerEu, PartShape<D, RT>::k
       do {
         lds_sync();
         const int tb = p.c0 + 64 * (s * TW + tw);
-        if (tb < p.c1 && tiles > 0) v.template block<true>(a, k0 + slot, v0 + slot, tb, gq);
+        if (tb < p.c1 && here) v.template block<true>(a, k0 + slot, v0 + slot, tb, gq);
         slot = S_::kRound - slot;
       } while (++s < rounds);
     }
-    v.end(a, ((size_t)(p.group(a) + blockIdx.x) * RT + t_first) * TW + tw, TW, tile0, tiles, n, gq);
+    if (here) v.end(a, ((size_t)(p.group(a) + blockIdx.x) * RT + tile) * TW + tw, tile_g, n, gq);
   } while (p.next(a));
 }
 
@@ -702,7 +698,7 @@ q8_mass_kernel(QArgs a) {
       const int tb = t0 + 64 * tw;
       if (__builtin_amdgcn_readfirstlane(tb - p.c1) >= 0) continue;
       floatx4 S[TPW][4];
-      scores<D, TPW>(k, q, S);
+      scores<D, TPW, 8>(k, q, S);
       if (__builtin_amdgcn_readfirstlane(tb + 63 - vis_all) > 0) {
 #pragma unroll
         for (int x = 0; x < TPW; ++x)

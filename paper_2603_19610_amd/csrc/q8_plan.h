@@ -16,21 +16,18 @@ constexpr int kQUnit = 32;
 constexpr int kQMinUnits = 2;  // least share: one 64-token block
 constexpr int kQMaxRT = 10;    // 16-row tiles of a workgroup
 
-// How a workgroup's computing waves share its row tiles and the blocks of 64
-// tokens: TPW tiles a wave, RW waves for the tiles, TW of each for TW blocks at a
-// time.  Up to five tiles a wave each; from six on two tiles a wave, which read a
-// block once for both (LDS would bound it, 9 tiles: 32 KB a tile and block).
-// CW more waves convert the blocks of K and CW those of V, one each of a round's
-// TW blocks or all; twelve waves, three a SIMD, at most.
+// The waves of a workgroup: RW for its row tiles, with TPW tiles each, times TW
+// for as many blocks of 64 tokens at a time, and CW that convert K's blocks and CW
+// for V's, each all of them or its own of a round's TW.
 struct QWaves {
   int tpw, rw, tw, cw;
 };
-constexpr QWaves q8_waves(int RT) {
-  const int tpw = RT <= 5 ? 1 : 2, rw = (RT + tpw - 1) / tpw;
-  return {tpw, rw, 2, rw <= 4 ? 2 : 1};
-}
-// The mass kernel's, with K alone: up to three tiles a wave, which sum their rows
-// together, and two waves a SIMD.
+// The partial kernel's: twelve waves, three a SIMD, at most.  (Two tiles a wave,
+// which read a block once for both: they are two a SIMD or spill, and 9 tiles
+// over 132K tokens took 126 to 146 us in place of 124 to 128.)
+constexpr QWaves q8_waves(int RT) { return {1, RT, RT <= 5 ? 2 : 1, RT <= 4 ? 2 : 1}; }
+// The mass kernel's, with K alone and no results to hold: up to three tiles a
+// wave, which sum their rows together, and two waves a SIMD.
 constexpr QWaves q8_mass_waves(int RT) {
   const int rw = (RT + 2) / 3, tw = rw <= 3 ? 2 : 1;
   return {(RT + rw - 1) / rw, rw, tw, tw};

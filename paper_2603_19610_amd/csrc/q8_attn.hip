@@ -4,25 +4,40 @@
 // decode step) to 32 rows.
 //
 // Mathematics.  With K_i = ck_i 2^(ek_i - 127) and V_i likewise:
-//   s_i = scale <q, ck_i> 2^(ek_i - 127)     P_i = softmax(s)_i over visible i
-//   out = sum_i (P_i 2^(ev_i - 127)) cv_i    mass_i = sum over rows of P_i
-//  * Both products run on bf16 with fp32 sums: codes become bf16 exactly, a
-//    key's with its row's power of two taken in by the conversion.  (The 8-bit
-//    matrix instructions align an instruction's products to the largest of them
-//    and lose up to 2^-14 of it, measured against float64; bf16 ones 2^-21.)
-//  * P is rounded to bf16 after its row's unit 2^(ev - 127) is taken in: half a
-//    step, 2^-8 of each term, of a result that is rounded to bf16 itself.
+//   s_i = scale <q, K_i>     P_i = softmax(s)_i over visible i
+//   out = sum_i P_i V_i      mass_i = sum over rows of P_i
+//  * Both products run on bf16 with fp32 sums: K_i and V_i are bf16 values (four
+//    significant bits and a power of two), so their conversion rounds nothing.
+//    (The 8-bit matrix instructions align an instruction's products to the
+//    largest of them and lose up to 2^-14 of it, measured against float64; bf16
+//    ones 2^-21.)
+//  * P is rounded to bf16 for the second product, half a step being 2^-9 to 2^-8
+//    of a term of a result that is rounded to bf16 itself; the row is divided by
+//    the sum of what was rounded.  lse and mass use the unrounded sum.
 //  * One pass over a chunk with a running maximum and sum in fp32; the chunks'
 //    (maximum, sum) and fp32 O partials are joined by the finish kernel.  The
-//    mass needs every row's log-sum-exp first, so K is read a second time.
+//    mass needs every row's sum first, so K is read a second time.
 //    Every order of summation is fixed.  No workgroup waits for another.
+//
+// Three launches (two without the mass), all on the caller's stream:
+//   partial  waves that convert a block of 64 tokens from memory to bf16 in LDS,
+//            once for all row tiles, beside waves that hold a tile of 16 rows
+//   mass     the same shares of the tokens, K alone, up to three tiles a wave
+//   finish   a wave or a workgroup joins a row's records; others sum the mass
+// What bounds them, and what they measured (one MI355X, D = 128, kernel times):
+//   memory: 32 sequences of one token, 85 MB of each of K and V: partial 37 us,
+//     4.5 TB/s.  9 tokens x 4 sequences, 117 MB each: partial 62 us, 3.8 TB/s.
+//   issue and matrix rate with many rows: 136 rows a head over 132K tokens, 135 MB
+//     each: partial 124 us (0.6 PFLOP/s), mass 75 us.  Of a SIMD's cycles then a
+//     third are matrix instructions, two fifths vector ones.
+//   latency in small calls: a launch that waits for lengths, then for the first
+//     block (all compute units ask at once), then for its stores takes 5 to 8 us.
 #include "q8.h"
 #include "q8_plan.h"
 
 namespace pvlm {
 namespace {
 
-typedef int intx2 __attribute__((ext_vector_type(2)));
 typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -35,11 +50,6 @@ constexpr float kNegInf = -__builtin_huge_valf();
 // in three of 72).  Probabilities then reach 2^24 in a type of bf16's range.
 constexpr float kRefSlack = 24.f;
 constexpr int kFinWaves = kFinThreads / 64;
-
-__device__ __forceinline__ int64_t uniform64(int64_t x) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
-  return (int64_t)((uint64_t)hi << 32 | lo);
-}
 
 struct QArgs {
   const uint16_t* q;
@@ -257,7 +267,7 @@ __device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first
   // at once.  With eight lanes a row, the upper four take the rows in the order
   // i ^ 4: what eight lanes write at a time is then two rows' (see Lay).
   constexpr int NI = D / 16;
-  typedef uint32_t Exps __attribute__((ext_vector_type(NI / 4)));
+  typedef uint32_t Exps __attribute__((ext_vector_type(NI / 4), aligned(4)));
   const uint8_t* codes = IS_V ? a.c.vc : a.c.kc;
   const uint8_t* exps = IS_V ? a.c.ve : a.c.ke;
   const int lane = threadIdx.x & 63, c = lane % NI, row0 = NI * (lane / NI);
@@ -270,7 +280,7 @@ __device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first
   int tb[DEPTH], c1[DEPTH], ctx[DEPTH], last_of[DEPTH];  // its tokens; its record if it is its piece's last block, else -1
   int t0 = p.c0 + 64 * first, x = 0, total = 0;
   bool more = true, bad_page = false;
-  // nothing of another path is under way (the compiler would wait for it at every block)
+  // vmcnt(0): nothing of another path is under way (the compiler would wait for it at every block)
   __builtin_amdgcn_s_waitcnt(0x0f70);
   // (always loads, so that the compiler knows how many loads are under way: past
   // the share, the rows of its last block again)
@@ -381,9 +391,10 @@ __device__ __forceinline__ float rows4_maximum(float x) {
   return __builtin_elementwise_maximum(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// AHEAD operand reads of LDS are under way while the matrix instructions of
-// earlier ones run (the compiler, left to itself, waits for each read alone).
-// Scores of a block (its K at LDS address k plus the lane's offset) against a wave's row tiles.
+// Scores of a block (its K at LDS address k plus the lane's offset) against a
+// wave's row tiles.  AHEAD operand reads of LDS are under way while the matrix
+// instructions of earlier ones run (the compiler, left to itself, waits for each
+// read alone).
 template <int D, int TPW, int AHEAD>
 __device__ __forceinline__ void scores(uint32_t k, const Query<D> (&q)[TPW], floatx4 (&S)[TPW][4]) {
   constexpr int N = D / 8;  // operands: chunk 4 ks + gq of the rows of tile tt, number 4 ks + tt
@@ -426,8 +437,8 @@ __device__ __forceinline__ void weigh(uint32_t v, const bf16x8 (&P)[2], floatx4 
   for (int j = 0; j < N; ++j) {
     if (j + AHEAD - 1 < N) read(j + AHEAD - 1);
     __builtin_amdgcn_sched_barrier(0);
-    const bf16x8 b = __builtin_bit_cast(bf16x8, (s8)__builtin_shufflevector(lo[j % AHEAD], hi[j % AHEAD], 0, 1, 2, 3, 4, 5, 6, 7));
-    O[j / 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[j % 2], b, O[j / 2], 0, 0, 0);
+    const s8 b = __builtin_shufflevector(lo[j % AHEAD], hi[j % AHEAD], 0, 1, 2, 3, 4, 5, 6, 7);
+    O[j / 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[j % 2], __builtin_bit_cast(bf16x8, b), O[j / 2], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   }
 }
@@ -439,12 +450,14 @@ __device__ __forceinline__ void join(float& m, float& z, float m2, float z2) {
   z = (z != 0.f ? z * fast_exp2(m - r) : 0.f) + (z2 != 0.f ? z2 * fast_exp2(m2 - r) : 0.f);
   m = M;
 }
-// log2-sum-exp of row n of a wave's tiles over a group's records, the lane
-// groups taking them in turn, with many loads in flight (+inf for padding rows:
-// their probabilities are 0).
+// Maximum of row n of a wave's tiles over a group's records, and the inverse of its
+// sum, the lane groups taking the records in turn, with many loads in flight
+// (padding rows: +inf, their probabilities are 0).  The two apart, and not their
+// log-sum-exp: a probability's exponent is then rounded at its distance from the
+// maximum, which is nothing where the mass is.
 template <int RT, int TPW>
-__device__ __forceinline__ void tile_lse(const QArgs& a, const Holders& h, int tile0, int tiles, const bool (&real)[TPW],
-                                         int n, int gq, float (&lse)[TPW]) {
+__device__ __forceinline__ void tile_sums(const QArgs& a, const Holders& h, int tile0, int tiles, const bool (&real)[TPW],
+                                         int n, int gq, float (&top)[TPW], float (&inv)[TPW]) {
   constexpr int kU = TPW == 1 ? 8 : 4;  // records of every tile in flight
   constexpr int TW = q8_waves(RT).tw;
   const int cnt = TW * h.count;
@@ -479,13 +492,14 @@ __device__ __forceinline__ void tile_lse(const QArgs& a, const Holders& h, int t
   for (int x = 0; x < TPW; ++x) {
     join(M[x], Z[x], lane_xor16(M[x]), lane_xor16(Z[x]));
     join(M[x], Z[x], lane_xor32(M[x]), lane_xor32(Z[x]));
-    lse[x] = real[x] ? M[x] + __log2f(Z[x]) : __builtin_huge_valf();
+    top[x] = real[x] ? M[x] : __builtin_huge_valf();
+    inv[x] = real[x] ? 1.f / Z[x] : 0.f;
   }
 }
 
-// Sum over the 16 rows (lanes n) of a block's values, of the value with
-// number n (lane & 15): each step a lane keeps half of its values, chosen by one bit of n, and
-// adds its partner's copy of that half.
+// Sum over the 16 rows (lanes n) of the value with number n (lane & 15): each
+// step a lane keeps half of its values, chosen by one bit of n, and adds its
+// partner's copy of that half.
 __device__ __forceinline__ float row_sums(const float (&p)[16], int lane) {
   const bool h8 = lane & 8, h4 = lane & 4, h2 = lane & 2, h1 = lane & 1;
   float a8[8], a4[4], a2[2];
@@ -516,7 +530,8 @@ struct PartWave {
   static constexpr int DPL = D / 16, AHEAD = 8;
   Query<D> q[1];
   int lim;  // last token that the lane's row sees
-  float ref, z;
+  float ref;
+  float z, over;  // the sum of the row's probabilities, and what its rounding added to that
   floatx4 O[DPL], zt;
 
   __device__ __forceinline__ void begin(const QArgs& a, const Piece& p, int tile, bool here, int n, int gq) {
@@ -524,7 +539,7 @@ struct PartWave {
     load_query<D>(a, p.b, p.g, row, gq, q[0]);
     lim = here && row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
     ref = kNegInf;
-    z = 0.f;
+    z = over = 0.f;
     zt = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int jd = 0; jd < DPL; ++jd) O[jd] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -549,6 +564,7 @@ struct PartWave {
       const float nm = fmaxf(ref, m);
       const float al = ref == kNegInf ? 0.f : fast_exp2(ref - nm);
       z *= al;
+      over *= al;
       ref = nm;
       floatx4 f;
 #pragma unroll
@@ -561,19 +577,26 @@ struct PartWave {
 #pragma unroll
     for (int j = 0; j < 8; ++j) ones[j] = static_cast<__bf16>(1.f);
     const float r = ref == kNegInf ? 0.f : ref;  // no visible token yet: P = 0
+    float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       const float e = fast_exp2(fmaf(S[0][j / 4][j % 4], a.sl2, -r));
-      z += e;
+      sum += e;
       P[j / 8][j % 8] = static_cast<__bf16>(e);
     }
+    // Kahan's sum over the blocks: beside one large term, thousands of small ones
+    // would each be rounded away (a log-sum-exp 6e-6 off over 132K tokens)
+    sum -= over;
+    const float old = z;
+    z += sum;
+    over = (z - old) - sum;
 #pragma unroll
     for (int h = 0; h < 2; ++h) zt = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[h], ones, zt, 0, 0, 0);
     weigh<D, AHEAD>(v, P, O);
   }
 
   __device__ __forceinline__ void end(const QArgs& a, size_t rec, int tile, int n, int gq) {
-    const float zz = rows4_sum(z);
+    const float zz = rows4_sum(z - over);
     if (gq == 0) a.stats[rec * 16 + n] = make_float2(ref, zz);
     if (n == 0) *reinterpret_cast<floatx4*>(a.zt + rec * 16 + 4 * gq) = zt;
     // position DPL n + jd of a stored row holds column 16 jd + n
@@ -645,7 +668,7 @@ __attribute__((amdgpu_waves_per_eu(PartShape<D, RT>::kPerEu, PartShape<D, RT>::k
 }
 
 // ----------------------------------------------------------- mass kernel --
-// The partial kernel's shares again, every row's log-sum-exp known.
+// The partial kernel's shares again, every row's maximum and sum known.
 template <int D, int RT>
 struct MassShape {
   static constexpr int TPW = q8_mass_waves(RT).tpw, RW = q8_mass_waves(RT).rw, TW = q8_mass_waves(RT).tw;
@@ -679,7 +702,7 @@ q8_mass_kernel(QArgs a) {
     const Holders h = holders(a, p.per, p.before, p.b, p.g * a.RG + p.rg, p.ctx);
     Query<D> q[TPW];
     int lim[TPW];
-    float lse[TPW];
+    float top[TPW], inv[TPW];
     bool real[TPW];
 #pragma unroll
     for (int x = 0; x < TPW; ++x) {
@@ -688,7 +711,7 @@ q8_mass_kernel(QArgs a) {
       load_query<D>(a, p.b, p.g, row, gq, q[x]);
       lim[x] = real[x] ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
     }
-    tile_lse<RT, TPW>(a, h, t_first, tiles, real, n, gq, lse);
+    tile_sums<RT, TPW>(a, h, t_first, tiles, real, n, gq, top, inv);
     const int vis_all = min(p.c1 - 1, p.ctx);
     float* mp = a.mpart + ((size_t)p.group(a) * S_::RW + rw) * a.c.n_cap;
     for (int t0 = p.c0; t0 < p.c1; t0 += 64 * TW) {
@@ -712,8 +735,8 @@ q8_mass_kernel(QArgs a) {
       for (int x = 0; x < TPW; ++x)
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const float e = fast_exp2(fmaf(S[x][j / 4][j % 4], a.sl2, -lse[x]));
-          sum[j] = x ? sum[j] + e : e;
+          const float e = fast_exp2(fmaf(S[x][j / 4][j % 4], a.sl2, -top[x]));
+          sum[j] = x ? fmaf(e, inv[x], sum[j]) : e * inv[x];
         }
       const float m = row_sums(sum, lane);
       if (tb + token < p.c1) mp[tb + token] = m;
@@ -885,8 +908,13 @@ struct QKernels {
 
 template <int D, int RT>
 QKernels kernels() {
-  return {q8_part_kernel<D, RT>, q8_mass_kernel<D, RT>, {q8_finish_kernel<D, RT, 1>, q8_finish_kernel<D, RT, kFinWaves>}, PartShape<D, RT>::kThreads,
-          MassShape<D, RT>::kThreads, PartShape<D, RT>::kLds, MassShape<D, RT>::kLds};
+  return {q8_part_kernel<D, RT>,
+          q8_mass_kernel<D, RT>,
+          {q8_finish_kernel<D, RT, 1>, q8_finish_kernel<D, RT, kFinWaves>},
+          PartShape<D, RT>::kThreads,
+          MassShape<D, RT>::kThreads,
+          PartShape<D, RT>::kLds,
+          MassShape<D, RT>::kLds};
 }
 template <int D>
 QKernels pick(int RT) {

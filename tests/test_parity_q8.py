@@ -628,6 +628,94 @@ def test_workspace_is_checked_and_shared_with_other_calls():
         assert all(torch.equal(a, b) for a, b in zip(mine, q8))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T,G", [(3, 4), (4, 7), (9, 5), (9, 7), (10, 8), (12, 8), (16, 7), (32, 4), (17, 8), (32, 5),
+                                 (32, 6)])
+def test_verify_every_number_of_row_tiles(T, G, D):
+    """1 to 10 tiles of 16 rows in a workgroup, and 12 over two; pages of one unit."""
+    rng = np.random.default_rng(T * G + D)
+    ctx = [261, 1337]
+    q, cache = queries(rng, 2, T, 2 * G, D), random_cache(rng, 2, 2, max(ctx) + T, D)
+    note(f"verify q8 tiles T={T} G={G} D={D}")
+    out, mass, lse = run_verify(q, cache, ctx, P=32, seed=T)
+    (ro, rl, rm), (bo, bl, bm) = reference(q, values(*cache[:2]), values(*cache[2:]), ctx, D ** -0.5)
+    check(out, ro, bo, "out")
+    check(lse, rl, bl, "lse")
+    check(mass[:, :rm.shape[1]], rm, bm, "mass")
+
+
+@pytest.mark.parametrize("B", [64, 65, 200])
+def test_verify_many_sequences(B):
+    """More sequences than a wave has lanes; lengths from 0 on, some workgroups with pieces of several sequences."""
+    rng = np.random.default_rng(B)
+    T, Hq, Hkv, D = 2, 6, 2, 64
+    ctx = [int(x) for x in rng.integers(0, 400, B)]
+    ctx[0], ctx[B // 2], ctx[B - 1] = 0, 30, 1
+    q, cache = queries(rng, B, T, Hq, D), random_cache(rng, B, Hkv, max(ctx) + T, D)
+    note(f"verify q8 {B} sequences")
+    out, mass, lse = run_verify(q, cache, ctx, P=32, seed=B)
+    (ro, rl, rm), (bo, bl, bm) = reference(q, values(*cache[:2]), values(*cache[2:]), ctx, D ** -0.5)
+    check(out, ro, bo, "out")
+    check(lse, rl, bl, "lse")
+    check(mass[:, :rm.shape[1]], rm, bm, "mass")
+
+
+def test_verify_small_probabilities_beside_a_large_one():
+    """One key of score 18 (17.5 as its row holds it), 40000 of score 0: each small term is a quarter of the last place of
+    the large one, and their sum is 6e-4.  Scores are exact (one channel), so the log-sum-exp is off by five roundings of
+    its size (the scale's factor log2(e), two products, two sums) and the logarithm's 2^-20: 6.2e-6.  Rounded away, the
+    small terms that share a lane with the large one (600, of 5000 tokens a workgroup) are 9e-6."""
+    B, Hkv, D, n = 4, 8, 64, 40000
+    x = np.zeros((B, Hkv, cap32(n + 1), D))
+    x[:, :, 37, 0] = 17.5
+    cache = [*to_cache(x), *to_cache(np.ones_like(x))]
+    q = torch.zeros((B, 1, Hkv, D), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0
+    note("verify q8 one large probability among small ones")
+    out, mass, lse = run_verify(q, cache, [n] * B, scale=1.0, garbage=False)
+    want = np.logaddexp(values(*cache[:2])[0, 0, 37, 0].item(), np.log(n))
+    assert (lse.double() - want).abs().max().item() <= 5 * 17.5 * 2.0 ** -24 + 2.0 ** -20
+    assert torch.equal(out, torch.ones_like(out))
+    p = np.exp(-want)
+    assert (mass[:, 1000:n].double() / (Hkv * p) - 1).abs().max().item() <= 2.0 ** -16
+
+
+def test_verify_calls_of_several_streams_in_one_graph():
+    """Two calls with workspaces of their own on two branches of a captured graph, replayed among eager calls."""
+    rng = np.random.default_rng(21)
+    shapes = [([700, 90], 5, 8, 2, 128), ([3000], 17, 16, 2, 64)]
+    work = []
+    for ctx, T, Hq, Hkv, D in shapes:
+        cache = random_cache(rng, len(ctx), Hkv, max(ctx) + T, D)
+        work.append((queries(rng, len(ctx), T, Hq, D), cache, torch.tensor(ctx, dtype=torch.int32, device="cuda"),
+                     pv.Workspace()))
+    want = [pv.verify_attn_q8(q, *c, n, ws=ws) for q, c, n, ws in work]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    note("verify q8 on two branches of a graph")
+    with torch.cuda.graph(g):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        q, c, n, ws = work[0]
+        got = [pv.verify_attn_q8(q, *c, n, ws=ws)]
+        with torch.cuda.stream(side):
+            q, c, n, ws = work[1]
+            got.append(pv.verify_attn_q8(q, *c, n, ws=ws))
+        main.wait_stream(side)
+    for _ in range(3):
+        for o in got:
+            for t in o:
+                t.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        for o, w in zip(got, want):
+            assert all(torch.equal(a, b) for a, b in zip(o, w))
+        for (q, c, n, ws), w in zip(work, want):
+            assert all(torch.equal(a, b) for a, b in zip(pv.verify_attn_q8(q, *c, n, ws=ws), w))
+        torch.cuda.synchronize()
+
+
 # ----------------------------------------------------------------- gather --
 @pytest.mark.parametrize("dtype", [torch.float8_e4m3fn, torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("P,D", [(0, 128), (64, 64), (32, 128)])

@@ -526,7 +526,9 @@ pvlm_status pvlm_quantize_kv_paged(pvlm_dtype dt, int n_layers, int B, int Hkv, 
  * the same definition with k_i and v_i the values that the rows stand for; T = 1
  * with mass = NULL is a decode step.  q and out are bf16 (dt PVLM_BF16;
  * PVLM_ERR_UNSUPPORTED otherwise) and q is not rounded further; scores, softmax
- * statistics and sums are fp32, P is rounded to bf16 before P . V.
+ * statistics and sums are fp32, P is rounded to bf16 before P . V.  Values are at
+ * most 2^80 in magnitude (partial sums of P . V may be up to 2^24 times their
+ * result).
  * A value of NaN reaches the rows that see it and no other; cache rows at and
  * past ctx_len[b] + T are not used, whatever they hold.
  *   ws    >= pvlm_verify_attn_q8_workspace_size() bytes (under every compute-unit

@@ -211,10 +211,14 @@ __device__ __forceinline__ int64_t unit_row(const QArgs& a, int b, int g, int t,
 }
 
 // LDS holds a block of 64 tokens as bf16 rows, of K and of V: 16-byte chunk c
-// of row r lies at chunk c ^ swz(r) of the row.  128 bytes are read or written at
-// a time: of K eight rows' same chunk, of V four rows' same two chunks, and two
-// rows' even chunks when they are filled.  swz places the bits of r so that each
-// of these falls on distinct banks.
+// of row r lies at chunk c ^ swz(r) of the row.  swz is linear in the bits of r
+// mod 16, and these are placed so that what LDS serves at a time falls on distinct
+// banks (its conflict counter is then 0; r mod 16 in place of swz: a third of the
+// LDS cycles were conflicts):
+//   a read of K, 256 bytes: chunk 4 ks of rows 0-3 and 12-15, chunk 4 ks + 1 of
+//     rows 4-11, or the other way round;
+//   a read of V, 256 bytes: eight rows' same two chunks;
+//   a write, 128 bytes: four even chunks of two rows that differ in bit 2.
 template <int D>
 struct Lay {
   static constexpr int CH = D / 8, kSide = 64 * D * 2;  // chunks of a row, bytes of a block's K or V
@@ -222,7 +226,10 @@ struct Lay {
   // 4 ks chunks and 16 tt rows on), and V's 8 bytes of row 4 gq + n / 4 (32 jd
   // bytes, and 16 and 32 rows on).  Chunks differ by an exclusive or of the
   // address: blocks start at multiples of 256 bytes.
-  static constexpr __host__ __device__ int swz(int r) { return (((r << 1) & 6) | ((r >> 2) & 1) | (r & 8)) & (CH - 1); }
+  static constexpr __host__ __device__ int swz(int r) {
+    const int m = D == 128 ? r : r >> 1 & 7;  // (two rows of D = 64 fill the banks)
+    return (m << 1 & 6) ^ (D == 128 ? (r & 4 ? 9 : 0) ^ (r & 8) : (r & 4 ? 1 : 0) ^ (r & 8 ? 4 : 0));
+  }
   static __device__ __forceinline__ uint32_t k_lane(int n, int gq) { return n * D * 2 + ((gq ^ swz(n)) << 4); }
   static __device__ __forceinline__ uint32_t k_at(uint32_t lane, int ks, int tt) { return (lane ^ (ks << 6)) + tt * 32 * D; }
   static __device__ __forceinline__ uint32_t v_lane(int n, int gq) {

@@ -25,13 +25,16 @@
 //   mass     the same shares of the tokens, K alone, up to three tiles a wave
 //   finish   a wave or a workgroup joins a row's records; others sum the mass
 // What bounds them, and what they measured (one MI355X, D = 128, kernel times):
-//   memory: 32 sequences of one token, 85 MB of each of K and V: partial 37 us,
-//     4.5 TB/s.  9 tokens x 4 sequences, 117 MB each: partial 62 us, 3.8 TB/s.
-//   issue and matrix rate with many rows: 136 rows a head over 132K tokens, 135 MB
-//     each: partial 124 us (0.6 PFLOP/s), mass 75 us.  Of a SIMD's cycles then a
-//     third are matrix instructions, two fifths vector ones.
-//   latency in small calls: a launch that waits for lengths, then for the first
-//     block (all compute units ask at once), then for its stores takes 5 to 8 us.
+//   memory: 16 sequences of one token, 84 MB of each of K and V: partial 38 us,
+//     4.5 TB/s.  4 sequences of 9 tokens, 117 MB each: partial 61 us, 3.9 TB/s;
+//     mass (K again) 40 us, 2.9 TB/s.
+//   instructions, with many rows: 136 rows a head over 132K tokens, 136 MB each:
+//     partial 117 us (0.63 PFLOP/s), mass 70 to 78 us (0.5 PFLOP/s).  Of a SIMD's
+//     cycles 37 % are matrix instructions, 47 % vector ones, of LDS's 42 % reads
+//     and writes; barriers keep the waves too close in step for more of each.
+//   latency in small calls: a launch that waits for the lengths, then for its
+//     first blocks (all compute units ask at once), then for its stores takes
+//     4 to 8 us.
 #include "q8.h"
 #include "q8_plan.h"
 

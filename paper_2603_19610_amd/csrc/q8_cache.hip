@@ -5,7 +5,13 @@
 //
 // All three are streams: every row is read once and written once by a few
 // neighbouring lanes (8 values each; 16 codes each in the gather), whose
-// maximum is a reduction over at most 16 lanes that stays in the vector unit.
+// maximum is a reduction over at most 16 lanes that stays in the vector unit.  They
+// are bound by HBM where there are rows enough, by a launch's latency else (one
+// MI355X, kernel times):
+//   append    80 heads of 12800 prompt rows, 0.5 GB: 97 us, 5.1 TB/s; 6 rows: 3.6 us
+//   quantise  28 layers of 6432 rows, 4 heads, 0.55 GB: 96 us, 5.7 TB/s; one of 787: 3 us
+//   gather    80 layers, 1510 rows kept, to bf16, 0.74 GB: 146 to 162 us, 4.6 to
+//             5.1 TB/s; 28 layers, 0.045 GB, copied: 10 us, 4.5 TB/s
 #include "q8.h"
 
 namespace pvlm {

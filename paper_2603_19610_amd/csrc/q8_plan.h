@@ -24,7 +24,7 @@ struct QWaves {
 };
 // The partial kernel's: twelve waves, three a SIMD, at most.  (Two tiles a wave,
 // which read a block once for both: they are two a SIMD or spill, and 9 tiles
-// over 132K tokens took 126 to 146 us in place of 124 to 128.)
+// over 132K tokens took 126 to 146 us where one took 124 to 128.)
 constexpr QWaves q8_waves(int RT) { return {1, RT, RT <= 5 ? 2 : 1, RT <= 4 ? 2 : 1}; }
 // The mass kernel's, with K alone and no results to hold: up to three tiles a
 // wave, which sum their rows together, and two waves a SIMD.

@@ -26,10 +26,10 @@
 //   finish   a wave or a workgroup joins a row's records; others sum the mass
 // What bounds them, and what they measured (one MI355X, D = 128, kernel times):
 //   memory: 16 sequences of one token, 84 MB of each of K and V: partial 38 us,
-//     4.5 TB/s.  4 sequences of 9 tokens, 117 MB each: partial 61 us, 3.9 TB/s;
-//     mass (K again) 40 us, 2.9 TB/s.
+//     4.5 TB/s.  4 sequences of 9 tokens, 117 MB each: partial 55 us, 4.3 TB/s;
+//     mass (K again) 39 us, 3.0 TB/s.
 //   instructions, with many rows: 136 rows a head over 132K tokens, 136 MB each:
-//     partial 117 us (0.63 PFLOP/s), mass 70 to 78 us (0.5 PFLOP/s).  Of a SIMD's
+//     partial 114 us (0.65 PFLOP/s), mass 70 to 75 us (0.5 PFLOP/s).  Of a SIMD's
 //     cycles 37 % are matrix instructions, 47 % vector ones, of LDS's 42 % reads
 //     and writes; barriers keep the waves too close in step for more of each.
 //   latency in small calls: a launch that waits for the lengths, then for its
@@ -257,14 +257,13 @@ __device__ __forceinline__ bf16x8 to_bf16(uint32_t lo, uint32_t hi, float unit) 
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// What a converting wave does: one side (K or V) of the workgroup's blocks (of
-// a round's blocks those from number `first` on, CW apart), from memory through
-// registers into LDS as bf16, a row's power of two taken in.  Each conversion
-// happens once for all row tiles.
-// DEPTH blocks are on their way at any time, by ordinary loads that the
-// compiler waits for one block at a time.  TW blocks make a round, for which
-// LDS has two slots of ROUND bytes: one barrier a round hands a filled one over
-// and an emptied one back.
+// What a converting wave does: one side (K or V) of the workgroup's blocks, from
+// memory through registers into LDS as bf16, a row's power of two taken in.  Each
+// conversion happens once for all row tiles.  A wave takes half a block (one
+// unit) at a time: of a round's 2 TW halves those from number `first` on, CW apart.
+// DEPTH halves are on their way at any time, by ordinary loads that the compiler
+// waits for one half at a time.  For a round, LDS has two slots of ROUND bytes: one
+// barrier a round hands a filled one over and an emptied one back.
 //
 // Rows past the piece become zeros (their tokens' probabilities are 0, and 0
 // times what an unwritten row holds may be NaN).  So do NaN values of rows that
@@ -272,53 +271,49 @@ __device__ __forceinline__ bf16x8 to_bf16(uint32_t lo, uint32_t hi, float unit) 
 // them.
 template <int D, int TW, int CW, int DEPTH, int ROUND, int BLOCK, bool IS_V>
 __device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first, uint32_t ring) {
-  constexpr int PER = TW / CW;  // blocks of a round
-  // lanes of a row, and rows of a lane: consecutive ones, whose exponents it reads
-  // at once.  With eight lanes a row, the upper four take the rows in the order
-  // i ^ 4: what eight lanes write at a time is then two rows' (see Lay).
-  constexpr int NI = D / 16;
-  typedef uint32_t Exps __attribute__((ext_vector_type(NI / 4), aligned(4)));
+  constexpr int PER = 2 * TW / CW;  // halves of a round
+  // Lanes of a row, and rows of a lane: consecutive ones, whose exponents it reads
+  // at once.  Eight neighbouring lanes write rows that differ in bit 2 (see Lay).
+  constexpr int LPR = D / 16, NI = D / 32;
+  const int lane = threadIdx.x & 63, c = lane % LPR, q = lane / LPR;
+  const int row0 = NI * (D == 128 ? q ^ (c >> 2) : (q & ~3) | (q & 1) << 1 | (q >> 1 & 1));
   const uint8_t* codes = IS_V ? a.c.vc : a.c.kc;
   const uint8_t* exps = IS_V ? a.c.ve : a.c.ke;
-  const int lane = threadIdx.x & 63, c = lane % NI, row0 = NI * (lane / NI);
-  const int flip = c & 4;  // (of four lanes a row: 0)
-  const uint32_t lds0 = (row0 + flip) * D * 2 + (((2 * c) ^ Lay<D>::swz(row0 + flip)) << 4);
-  const int lds_step = -2 * flip * D * 2;  // to the rows of i >= 4, past the 4 rows of i
+  const uint32_t lds0 = row0 * D * 2 + (((2 * c) ^ Lay<D>::swz(row0)) << 4);
 
   uintx4 v[DEPTH][NI];
-  Exps e[DEPTH];
-  int tb[DEPTH], c1[DEPTH], ctx[DEPTH], last_of[DEPTH];  // its tokens; its record if it is its piece's last block, else -1
-  int t0 = p.c0 + 64 * first, x = 0, total = 0;
+  uint32_t e[DEPTH];
+  int tb[DEPTH], c1[DEPTH], ctx[DEPTH], last_of[DEPTH];  // its tokens; its record if it is its piece's last, else -1
+  int t0 = p.c0 + 32 * first, x = 0, total = 0;
   bool more = true, bad_page = false;
-  // vmcnt(0): nothing of another path is under way (the compiler would wait for it at every block)
+  // vmcnt(0): nothing of another path is under way (the compiler would wait for it at every half)
   __builtin_amdgcn_s_waitcnt(0x0f70);
   // (always loads, so that the compiler knows how many loads are under way: past
-  // the share, the rows of its last block again)
+  // the share, rows of its last piece again)
   auto issue = [&](int k) {
-    const int last = (p.c1 - 1) & ~31;  // the piece's last unit; of a whole unit every row may be read
-    const int64_t u0 = unit_row(a, p.b, p.g, min(t0, last), bad_page);
-    const int64_t u1 = unit_row(a, p.b, p.g, min(t0 + 32, last), bad_page);
-    const int64_t r = row0 < 32 ? u0 + row0 : u1 + (row0 - 32);
+    // past the piece, the piece's last unit; of a whole unit every row may be read
+    const int64_t r = unit_row(a, p.b, p.g, min(t0, (p.c1 - 1) & ~31), bad_page) + row0;
     const uint8_t* src = codes + r * D + 16 * c;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) v[k][i] = *reinterpret_cast<const uintx4*>(src + (i < 4 ? flip : -flip) * D + i * D);
-    e[k] = *reinterpret_cast<const Exps*>(exps + r);
+    for (int i = 0; i < NI; ++i) v[k][i] = *reinterpret_cast<const uintx4*>(src + i * D);
+    if constexpr (NI == 4) e[k] = *reinterpret_cast<const uint32_t*>(exps + r);
+    else e[k] = *reinterpret_cast<const uint16_t*>(exps + r);
     if (!more) return;
     tb[k] = t0;
     c1[k] = p.c1;
     ctx[k] = p.ctx;
     last_of[k] = -1;
     ++total;
-    t0 += 64 * CW;
+    t0 += 32 * CW;
     if (++x == PER) {
       x = 0;
-      if (t0 - 64 * first >= p.c1) {
+      if (t0 - 32 * first >= p.c1) {
         last_of[k] = (p.group(a) + blockIdx.x) * CW + first;
         Piece next = p;
         more = next.next(a);
         if (more) {
           p = next;
-          t0 = p.c0 + 64 * first;
+          t0 = p.c0 + 32 * first;
         }
       }
     }
@@ -326,18 +321,13 @@ __device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first
   uint32_t bad = 0;
   auto convert = [&](int k, uint32_t at) {
     const int whole = IS_V ? min(c1[k] - 1, ctx[k]) : c1[k] - 1;
-    if constexpr (NI == 8) {
-      const uint32_t x = e[k][0];
-      e[k][0] = flip ? e[k][1] : x;
-      e[k][1] = flip ? x : e[k][1];
-    }
-    if (__builtin_amdgcn_readfirstlane(tb[k] + 63 - whole) > 0) {
+    if (__builtin_amdgcn_readfirstlane(tb[k] + 31 - whole) > 0) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int t = tb[k] + row0 + (i ^ flip);
+        const int t = tb[k] + row0 + i;
         if (t >= c1[k]) {
           v[k][i] = uintx4{0, 0, 0, 0};
-          e[k][i / 4] = (e[k][i / 4] & ~(0xffu << 8 * (i % 4))) | 127u << 8 * (i % 4);
+          e[k] = (e[k] & ~(0xffu << 8 * i)) | 127u << 8 * i;
         }
         if (IS_V && t > ctx[k])
 #pragma unroll
@@ -350,10 +340,9 @@ __device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first
     }
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const float unit = q8_unit((e[k][i / 4] >> (8 * (i % 4))) & 0xffu);
-      const uint32_t row = at + (i < 4 ? 0 : lds_step);  // (swz(i ^ 4) = swz(i) ^ swz(4))
-      lds_write((row ^ (Lay<D>::swz(i) << 4)) + i * D * 2, to_bf16(v[k][i][0], v[k][i][1], unit));
-      lds_write((row ^ ((Lay<D>::swz(i) ^ 1) << 4)) + i * D * 2, to_bf16(v[k][i][2], v[k][i][3], unit));
+      const float unit = q8_unit((e[k] >> (8 * i)) & 0xffu);
+      lds_write((at ^ (Lay<D>::swz(i) << 4)) + i * D * 2, to_bf16(v[k][i][0], v[k][i][1], unit));
+      lds_write((at ^ ((Lay<D>::swz(i) ^ 1) << 4)) + i * D * 2, to_bf16(v[k][i][2], v[k][i][3], unit));
     }
     if (IS_V && last_of[k] >= 0) {
       const bool any = __any(bad);
@@ -367,7 +356,8 @@ __device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first
 #pragma unroll
     for (int k = 0; k < DEPTH; ++k) {
       const bool now = done >= 0 && done < total;
-      if (now) convert(k, ring + lds0 + (done / PER % 2) * ROUND + (done % PER * CW + first) * BLOCK);
+      const int half = done % PER * CW + first;
+      if (now) convert(k, ring + lds0 + (done / PER % 2) * ROUND + half / 2 * BLOCK + half % 2 * 32 * D * 2);
       issue(k);
       ++done;
       if (now && done % PER == 0) lds_sync();  // the round is there; every wave is done with the one before
@@ -528,16 +518,17 @@ struct PartShape {
   static constexpr int TW = q8_waves(RT).tw, CW = q8_waves(RT).cw;
   static constexpr int kCompute = RT * TW, kThreads = (kCompute + 2 * CW) * 64;
   // waves of a SIMD; two at least, so that a wave's registers are all of one kind
-  static constexpr int kPerEu = kThreads <= 512 ? 2 : 3;
+  static constexpr int kPerEu = kThreads <= 512 ? 2 : (kThreads + 255) / 256;
   static constexpr int kBlock = 2 * Lay<D>::kSide, kRound = TW * kBlock, kLds = 2 * kRound;
-  // blocks of 32 registers (D = 128) that a converting wave has on their way
-  static constexpr int kDepth = 3 * (128 / D);
+  // halves of blocks, of 16 registers (D = 128), that a converting wave has on their way
+  static constexpr int kDepth = 4 * (128 / D);
 };
 
-// A computing wave's state: a row tile against the tokens of its blocks.
-template <int D>
+// A computing wave's state: a row tile against the tokens of its blocks, with AHEAD
+// operands read ahead.
+template <int D, int AHEAD>
 struct PartWave {
-  static constexpr int DPL = D / 16, AHEAD = 8;
+  static constexpr int DPL = D / 16;
   Query<D> q[1];
   int lim;  // last token that the lane's row sees
   float ref;
@@ -649,7 +640,7 @@ __attribute__((amdgpu_waves_per_eu(PartShape<D, RT>::kPerEu, PartShape<D, RT>::k
   do {
     const int tile_g = p.rg * RT + tile;  // of the KV head's; one past its rows is idle
     const bool here = tile_g < a.RTT;
-    PartWave<D> v;
+    PartWave<D, S_::kPerEu == 4 ? 4 : 8> v;  // (by a wave's registers: 128 or 168)
     v.begin(a, p, tile_g, here, n, gq);
     // the wave's rounds whose block every row sees whole, then the others (two
     // loops with their test at the end: joined, or with the test ahead, the
@@ -684,7 +675,7 @@ struct MassShape {
   static constexpr int TPW = q8_mass_waves(RT).tpw, RW = q8_mass_waves(RT).rw, TW = q8_mass_waves(RT).tw;
   static constexpr int CW = q8_mass_waves(RT).cw, kCompute = RW * TW, kThreads = (kCompute + CW) * 64;
   static constexpr int kBlock = Lay<D>::kSide, kRound = TW * kBlock, kLds = 2 * kRound;
-  static constexpr int kDepth = 5 * (128 / D);
+  static constexpr int kDepth = 8 * (128 / D);
 };
 
 template <int D, int RT>

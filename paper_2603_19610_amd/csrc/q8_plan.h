@@ -17,20 +17,22 @@ constexpr int kQMinUnits = 2;  // least share: one 64-token block
 constexpr int kQMaxRT = 10;    // 16-row tiles of a workgroup
 
 // The waves of a workgroup: RW for its row tiles, with TPW tiles each, times TW
-// for as many blocks of 64 tokens at a time, and CW that convert K's blocks and CW
-// for V's, each all of them or its own of a round's TW.
+// for as many blocks of 64 tokens at a time (a round), and CW that convert K's
+// halves of these blocks and CW for V's.
 struct QWaves {
   int tpw, rw, tw, cw;
 };
-// The partial kernel's: twelve waves, three a SIMD, at most.  (Two tiles a wave,
-// which read a block once for both: they are two a SIMD or spill, and 9 tiles
-// over 132K tokens took 126 to 146 us where one took 124 to 128.)
-constexpr QWaves q8_waves(int RT) { return {1, RT, RT <= 5 ? 2 : 1, RT <= 4 ? 2 : 1}; }
+// The partial kernel's: sixteen waves, four a SIMD, at most.  With few tiles the
+// conversion bounds a round, and every half has a wave of its own (3 tiles, 117 MB
+// of each of K and V: 55 us, with two halves a wave 60).  Two tiles a wave, which
+// read a block once for both, are two a SIMD or spill: 9 tiles over 132K tokens
+// took 126 to 146 us where one took 124 to 128.
+constexpr QWaves q8_waves(int RT) { return {1, RT, RT <= 6 ? 2 : 1, RT <= 4 ? 4 : 2}; }
 // The mass kernel's, with K alone and no results to hold: up to three tiles a
 // wave, which sum their rows together, and two waves a SIMD.
 constexpr QWaves q8_mass_waves(int RT) {
-  const int rw = (RT + 2) / 3, tw = rw <= 3 ? 2 : 1;
-  return {(RT + rw - 1) / rw, rw, tw, tw};
+  const int rw = (RT + 2) / 3;
+  return {(RT + rw - 1) / rw, rw, rw <= 3 ? 2 : 1, 2};
 }
 
 struct QSplit {

@@ -122,8 +122,8 @@ static bool bad_shares(const Call& c, int cus, const QSplit& p) {
 static bool bad_waves(const Call&, int, const QSplit& p) {
   if (p.RT < 1 || p.RT > kQMaxRT || p.RT * p.RG < p.RTT) return true;
   const QWaves w = q8_waves(p.RT), m = q8_mass_waves(p.RT);
-  if (w.tpw != 1 || w.rw != p.RT || w.tw % w.cw || w.rw * w.tw + 2 * w.cw > 12) return true;
-  return m.tpw > 3 || m.rw * m.tpw < p.RT || (m.rw - 1) * m.tpw >= p.RT || m.tw % m.cw || m.rw * m.tw + m.cw > 8;
+  if (w.tpw != 1 || w.rw != p.RT || 2 * w.tw % w.cw || w.rw * w.tw + 2 * w.cw > 16) return true;
+  return m.tpw > 3 || m.rw * m.tpw < p.RT || (m.rw - 1) * m.tpw >= p.RT || 2 * m.tw % m.cw || m.rw * m.tw + m.cw > 8;
 }
 
 int main(int argc, char** argv) {

@@ -66,7 +66,8 @@
  *     budget of C compute units, long-row top-k calls and the launches of
  *     verify calls that stream the cache take at most C workgroups, one per
  *     compute unit (verify calls with more than C groups of a sequence's, a KV
- *     head's query rows take more, and never wait).  Streams whose budgets sum
+ *     head's query rows take more, and never wait; those over an 8-bit cache
+ *     never take more).  Streams whose budgets sum
  *     to at most the device's compute units may therefore replay waiting
  *     graphs at the same time: every workgroup of all of them fits at once.
  *     Other launches (accept, gather, rope, the sums that end a verify call)

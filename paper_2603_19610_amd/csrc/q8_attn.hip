@@ -201,16 +201,19 @@ __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_ex
 __device__ __forceinline__ int row_t(const QArgs& a, int row) { return (int)((unsigned)row * a.g_magic >> 20); }
 
 // ------------------------------------------------------------- the blocks --
-// The row index (in rows of codes) of the unit that token t opens.  A page entry
-// outside the pool sets bad and is clamped into it.
-__device__ __forceinline__ int64_t unit_row(const QArgs& a, int b, int g, int t, bool& bad) {
+// The page-table entry of token t (0 in a padded cache), and the row index (in
+// rows of codes) of the unit that t opens.  An entry outside the pool sets bad
+// and is clamped into it.
+__device__ __forceinline__ int page_entry(const QArgs& a, int b, int t) {
+  return a.c.table ? uniform_load(a.c.table, (int64_t)b * a.c.max_pages + (t >> a.c.shift)) : 0;
+}
+__device__ __forceinline__ int64_t unit_row(const QArgs& a, int b, int g, int t, int page, bool& bad) {
   if (!a.c.table) return ((int64_t)b * a.Hkv + g) * a.c.n_cap + t;
-  int pg = uniform_load(a.c.table, (int64_t)b * a.c.max_pages + (t >> a.c.shift));
-  if (pg < 0 || pg >= a.c.n_pages) {
+  if (page < 0 || page >= a.c.n_pages) {
     bad = true;
-    pg = pg < 0 ? 0 : (int)(a.c.n_pages - 1);
+    page = page < 0 ? 0 : (int)(a.c.n_pages - 1);
   }
-  return (((int64_t)pg * a.Hkv + g) << a.c.shift) + (t & ((1 << a.c.shift) - 1));
+  return (((int64_t)page * a.Hkv + g) << a.c.shift) + (t & ((1 << a.c.shift) - 1));
 }
 
 // LDS holds a block of 64 tokens as bf16 rows, of K and of V: 16-byte chunk c
@@ -276,7 +279,8 @@ __device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first
   // at once.  Eight neighbouring lanes write rows that differ in bit 2 (see Lay).
   constexpr int LPR = D / 16, NI = D / 32;
   const int lane = threadIdx.x & 63, c = lane % LPR, q = lane / LPR;
-  const int row0 = NI * (D == 128 ? q ^ (c >> 2) : (q & ~3) | (q & 1) << 1 | (q >> 1 & 1));
+  const uint32_t row0 = NI * (D == 128 ? q ^ (c >> 2) : (q & ~3) | (q & 1) << 1 | (q >> 1 & 1));
+  const uint32_t at_codes = row0 * D + 16 * c;
   const uint8_t* codes = IS_V ? a.c.vc : a.c.kc;
   const uint8_t* exps = IS_V ? a.c.ve : a.c.ke;
   const uint32_t lds0 = row0 * D * 2 + (((2 * c) ^ Lay<D>::swz(row0)) << 4);
@@ -288,16 +292,22 @@ __device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first
   bool more = true, bad_page = false;
   // vmcnt(0): nothing of another path is under way (the compiler would wait for it at every half)
   __builtin_amdgcn_s_waitcnt(0x0f70);
+  // The next half's unit (past the piece, the piece's last; of a whole unit every
+  // row may be read), and its page entry, which is then there when it is wanted.
+  int unit, page;
+  auto find_unit = [&] {
+    unit = min(t0, (p.c1 - 1) & ~31);
+    page = page_entry(a, p.b, unit);
+  };
   // (always loads, so that the compiler knows how many loads are under way: past
   // the share, rows of its last piece again)
   auto issue = [&](int k) {
-    // past the piece, the piece's last unit; of a whole unit every row may be read
-    const int64_t r = unit_row(a, p.b, p.g, min(t0, (p.c1 - 1) & ~31), bad_page) + row0;
-    const uint8_t* src = codes + r * D + 16 * c;
+    const int64_t r = unit_row(a, p.b, p.g, unit, page, bad_page);
+    const uint8_t *src = codes + r * D, *src_e = exps + r;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) v[k][i] = *reinterpret_cast<const uintx4*>(src + i * D);
-    if constexpr (NI == 4) e[k] = *reinterpret_cast<const uint32_t*>(exps + r);
-    else e[k] = *reinterpret_cast<const uint16_t*>(exps + r);
+    for (int i = 0; i < NI; ++i) v[k][i] = *reinterpret_cast<const uintx4*>(src + at_codes + i * D);
+    if constexpr (NI == 4) e[k] = *reinterpret_cast<const uint32_t*>(src_e + row0);
+    else e[k] = *reinterpret_cast<const uint16_t*>(src_e + row0);
     if (!more) return;
     tb[k] = t0;
     c1[k] = p.c1;
@@ -317,14 +327,16 @@ __device__ __forceinline__ void convert_share(const QArgs& a, Piece p, int first
         }
       }
     }
+    find_unit();
   };
+  find_unit();
   uint32_t bad = 0;
   auto convert = [&](int k, uint32_t at) {
     const int whole = IS_V ? min(c1[k] - 1, ctx[k]) : c1[k] - 1;
     if (__builtin_amdgcn_readfirstlane(tb[k] + 31 - whole) > 0) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int t = tb[k] + row0 + i;
+        const int t = tb[k] + (int)row0 + i;
         if (t >= c1[k]) {
           v[k][i] = uintx4{0, 0, 0, 0};
           e[k] = (e[k] & ~(0xffu << 8 * i)) | 127u << 8 * i;
@@ -458,7 +470,9 @@ __device__ __forceinline__ void join(float& m, float& z, float m2, float z2) {
 template <int RT, int TPW>
 __device__ __forceinline__ void tile_sums(const QArgs& a, const Holders& h, int tile0, int tiles, const bool (&real)[TPW],
                                          int n, int gq, float (&top)[TPW], float (&inv)[TPW]) {
-  constexpr int kU = TPW == 1 ? 8 : 4;  // records of every tile in flight
+  // records of every tile in flight: a group has dozens, and a round trip takes a
+  // microsecond (42 rows over 6432 tokens, 102 records: 14.4 us, with four 17.5)
+  constexpr int kU = 16;
   constexpr int TW = q8_waves(RT).tw;
   const int cnt = TW * h.count;
   const float2* st = a.stats + (size_t)h.rec * RT * TW * 16 + n;
@@ -848,7 +862,7 @@ __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_
   if (t.nan) {  // the values past the context that the row sees, whose NaN codes counted as 0
     for (int j = ctx + 1; j <= ctx + tt; ++j) {
       bool flagged_before;  // by the partial kernel
-      const int64_t r = unit_row(a, b, g, j & ~31, flagged_before) + (j & 31);
+      const int64_t r = unit_row(a, b, g, j & ~31, page_entry(a, b, j), flagged_before) + (j & 31);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int c = 4 * col + k;

@@ -11,7 +11,8 @@ namespace pvlm {
 // counted in units of 32 (a page holds whole ones), all groups in a row, and
 // every workgroup takes an equal share of that row, whatever the lengths are:
 // a ragged batch keeps no compute unit idle, and a workgroup may end one
-// group and begin the next.  The shares follow from the lengths on the device.
+// group and begin the next (unless the shares are enough for every group to begin
+// its own).  The shares follow from the lengths on the device.
 constexpr int kQUnit = 32;
 constexpr int kQMinUnits = 2;  // least share: one 64-token block
 constexpr int kQMaxRT = 10;    // 16-row tiles of a workgroup

@@ -74,6 +74,13 @@ static bool bad_shares(const Call& c, int cus, const QSplit& p) {
   }
   long per = (total * HR + p.wgs - 1) / p.wgs;
   if (per < kQMinUnits) per = kQMinUnits;
+  // groups begin shares of their own where these are enough
+  std::vector<int> real = units;
+  long rounded = 0;
+  for (int u : units) rounded += (u + per - 1) / per * per;
+  const bool aligned = c.B * HR <= p.wgs && rounded * HR <= p.wgs * per;
+  if (aligned)
+    for (int& u : units) u = (int)((u + per - 1) / per * per);
   std::set<long> records;
   std::vector<long> first(c.B * HR, -1), count(c.B * HR, 0);
   long done = 0;
@@ -87,9 +94,12 @@ static bool bad_shares(const Call& c, int cus, const QSplit& p) {
     long off = at - before * HR, left = per;
     int hr = (int)(off / units[b]);
     off -= (long)hr * units[b];
+    if (aligned && real[b] - off < left) left = real[b] - off;
+    if (left <= 0) return true;
+    const long share = left;
     while (left > 0) {
       const long here = left < units[b] - off ? left : units[b] - off, group = (long)b * HR + hr;
-      if (at + per - left != before * HR + (long)hr * units[b] + off) return true;
+      if (at + share - left != before * HR + (long)hr * units[b] + off) return true;
       const long rec = group + w;
       if (rec >= (long)p.recs || !records.insert(rec).second) return true;
       if (first[group] < 0) first[group] = w;

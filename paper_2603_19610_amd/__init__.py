@@ -913,6 +913,16 @@ def _need_q8(k_codes, k_exps, v_codes, v_exps, dev, paged, stacked=None):
     return shape
 
 
+def _ws_buffer(kind, ws, nbytes, dev):
+    """The buffer of a call whose launches rely on nothing that a workspace held
+    before.  A captured call without a workspace of its own takes one of its
+    graph's memory, as its temporaries are: graphs captured on one stream may
+    be replayed on different ones at once, beside that stream's eager calls."""
+    if ws is None and torch.cuda.is_current_stream_capturing():
+        return torch.empty(max(nbytes, 1), dtype=torch.uint8, device=dev)
+    return (ws or _default_ws(kind)).get(nbytes)
+
+
 def _need_table(page_table, dev, B):
     _need(page_table, "page_table", torch.int32, dev)
     if page_table.dim() != 2 or page_table.shape[0] != B:
@@ -1053,8 +1063,7 @@ def _verify_q8(q, cache, page_table, ctx_len, scale, max_ctx, out, mass, lse, wa
     elif _need(lse, "lse", torch.float32, dev).shape != (B, Hq, T):
         raise ValueError("lse must be [B][Hq][T]")
     L = lib()
-    wsb = (ws or _default_ws("verify_q8")).get(
-        L.pvlm_verify_attn_q8_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx))
+    wsb = _ws_buffer("verify_q8", ws, L.pvlm_verify_attn_q8_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx), dev)
     name = "pvlm_verify_attn_q8" if page_table is None else "pvlm_verify_attn_q8_paged"
     st = getattr(L, name)(PVLM_BF16, B, T, Hq, Hkv, D, *geom, max_ctx,
                           float(D ** -0.5 if scale is None else scale), q.data_ptr(),

@@ -54,14 +54,13 @@ constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kRefSlack = 24.f;
 constexpr int kFinWaves = kFinThreads / 64;
 
-struct QArgs {
+struct QArgs : QShape {
   const uint16_t* q;
   Q8Cache c;
   const int32_t* ctx_len;
-  int B, T, Hq, Hkv, G, R;
+  int Hq, G, R;
   unsigned g_magic;  // row / G == row * g_magic >> 20 for row < 640 (2^20 / G + 1; G <= 640)
-  int RTT, RG, HR;   // HR = Hkv * RG, the groups of a sequence
-  int max_ctx, wgs;
+  int RTT;
   float sl2;         // scale * log2(e)
   float* mpart;      // [B][HR][waves][n_cap] mass of one wave's rows
   float2* stats;     // [record][tile][token wave][16] (log2-domain maximum, sum) of rows
@@ -78,22 +77,6 @@ struct QArgs {
 typedef const __attribute__((address_space(4))) int32_t* ConstInts;  // (uniform loads go through the scalar cache)
 __device__ __forceinline__ int uniform_load(const int32_t* p, int64_t i) { return ((ConstInts)(uintptr_t)p)[i]; }
 
-__device__ __forceinline__ int clamp_ctx(const QArgs& a, int ctx) { return ctx < 0 ? 0 : min(ctx, a.max_ctx); }
-__device__ __forceinline__ int units_of(const QArgs& a, int ctx) { return (ctx + a.T + kQUnit - 1) / kQUnit; }
-
-// Where the groups lie in the row of units.  Every wave finds its place from
-// the lengths: sequence b's first group begins at HR * before.  Where the shares
-// are enough for it, every group begins a share of its own (align = per; its units
-// count as a multiple of that): a share that ends one group and begins another
-// takes a round and the statistics of both (72 rows over 12800 tokens, 8 groups:
-// mass kernel 15.8 us, aligned 13.0).
-struct Shares {
-  int per;     // units of a workgroup
-  int align;   // what a group's units are rounded up to a multiple of
-  int before;  // units (of one group each) of the sequences ahead of b
-  int b, ctx;
-};
-__device__ __forceinline__ int aligned(int units, int align) { return align == 1 ? units : (units + align - 1) / align * align; }
 // Inclusive sum over the wave's lanes.
 __device__ __forceinline__ int wave_scan(int x) {
 #define PVLM_SCAN(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, false)
@@ -107,118 +90,39 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
-// The sequence that holds the first unit of share wg (b = B: none), or sequence `seq`.
-template <bool FIND_UNIT>
-__device__ __forceinline__ Shares find(const QArgs& a, int wg, int seq) {
-  const int lane = threadIdx.x & 63;
-  Shares s;
-  int total = 0, ctx = 0, raw = 0, u = 0, upto = 0;
-  auto load = [&](int b0) {
+// The lengths of 64 sequences, one a lane, for q8_find.
+struct Wave {
+  const int32_t* ctx_len;
+  int lane, ctx, raw, u, upto;
+  __device__ __forceinline__ explicit Wave(const QArgs& a) : ctx_len(a.ctx_len), lane(threadIdx.x & 63) {}
+  __device__ __forceinline__ void load(const QShape& a, int b0) {
     const bool here = b0 + lane < a.B;
-    ctx = here ? clamp_ctx(a, a.ctx_len[b0 + lane]) : 0;
+    ctx = here ? clamp_ctx(a, ctx_len[b0 + lane]) : 0;
     raw = here ? units_of(a, ctx) : 0;
-  };
-  auto add_up = [&](int b0, int align) {
-    if (b0 > 0 || a.B > 64) load(b0);
+  }
+  __device__ __forceinline__ void sum(int align) {
     u = aligned(raw, align);
     upto = wave_scan(u);
-  };
-  load(0);
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    add_up(b0, 1);
-    total += __builtin_amdgcn_readlane(upto, 63);
   }
-  s.per = max((total * a.HR + a.wgs - 1) / a.wgs, kQMinUnits);
-  s.align = 1;
-  if (a.B * a.HR <= a.wgs) {  // (so the sums below stay under wgs shares and as many units of rounding)
-    int sum = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-      add_up(b0, s.per);
-      sum += __builtin_amdgcn_readlane(upto, 63);
-    }
-    if ((int64_t)sum * a.HR <= (int64_t)a.wgs * s.per) s.align = s.per;
+  __device__ __forceinline__ int last() const { return __builtin_amdgcn_readlane(upto, 63); }
+  __device__ __forceinline__ int ahead(int x) const { return __builtin_amdgcn_readlane(upto - u, x); }
+  __device__ __forceinline__ int ctx_of(int x) const { return __builtin_amdgcn_readlane(ctx, x); }
+  __device__ __forceinline__ int reaching(const QShape& a, int b0, int before, int at) const {
+    const uint64_t m = __ballot(b0 + lane < a.B && (before + upto) * a.HR > at);
+    return m ? __builtin_ctzll(m) : -1;
   }
-  s.before = 0;
-  s.b = a.B;
-  s.ctx = 0;
-  // (wg * per stays within 32 bits: per exceeds total / wgs by less than one, or is the least share of few units)
-  const int at = wg * s.per;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    add_up(b0, s.align);
-    int hit = seq - b0;
-    if constexpr (FIND_UNIT) {
-      const uint64_t m = __ballot(b0 + lane < a.B && (s.before + upto) * a.HR > at);
-      hit = m ? __builtin_ctzll(m) : -1;
-    }
-    if (hit >= 0 && hit < 64) {
-      s.before += __builtin_amdgcn_readlane(upto - u, hit);
-      s.b = b0 + hit;
-      s.ctx = __builtin_amdgcn_readlane(ctx, hit);
-      break;
-    }
-    s.before += __builtin_amdgcn_readlane(upto, 63);
-  }
-  return s;
-}
+};
 
-// A workgroup's share as pieces of groups, one after the other.
-struct Piece {
-  int b, g, rg, ctx;     // group: sequence, KV head, share of its row tiles
-  int c0, c1;            // its tokens (c0 opens a unit)
-  int left;              // units of the share from c0 on
-  int before, per, align;  // units of the sequences ahead of b; of a share; see Shares
-  __device__ __forceinline__ void set(const QArgs& a) {
-    const int N = ctx + a.T, u = c0 / kQUnit + left;
-    c1 = __builtin_amdgcn_readfirstlane(u > N / kQUnit ? N : u * kQUnit);
-  }
+struct Piece : QPiece {
   // false where the share is empty
   __device__ __forceinline__ bool first(const QArgs& a) {
-    const Shares s = find<true>(a, blockIdx.x, 0);
-    if (s.b >= a.B) return false;
-    b = s.b;
-    ctx = s.ctx;
-    before = s.before;
-    per = s.per;
-    align = s.align;
-    const int units = units_of(a, ctx), u = aligned(units, align), off = (int)blockIdx.x * per - before * a.HR;
-    const int hr = __builtin_amdgcn_readfirstlane(off / u);
-    g = __builtin_amdgcn_readfirstlane(hr / a.RG);
-    rg = hr - g * a.RG;
-    const int from = __builtin_amdgcn_readfirstlane(off - hr * u);
-    left = min(per, align == 1 ? per : units - from);
-    c0 = from * kQUnit;
-    set(a);
-    return true;
+    return begin(a, q8_find<true>(a, Wave(a), blockIdx.x, 0), blockIdx.x);
   }
   // false where the share ends
   __device__ __forceinline__ bool next(const QArgs& a) {
-    left -= (c1 - c0 + kQUnit - 1) / kQUnit;
-    if (left <= 0) return false;
-    if (++rg == a.RG) {
-      rg = 0;
-      if (++g == a.Hkv) {
-        g = 0;
-        before += units_of(a, ctx);
-        if (++b == a.B) return false;
-        ctx = __builtin_amdgcn_readfirstlane(clamp_ctx(a, uniform_load(a.ctx_len, b)));
-      }
-    }
-    c0 = 0;
-    set(a);
-    return true;
+    return advance(a, [&](int x) { return __builtin_amdgcn_readfirstlane(clamp_ctx(a, uniform_load(a.ctx_len, x))); });
   }
-  __device__ __forceinline__ int group(const QArgs& a) const { return (b * a.Hkv + g) * a.RG + rg; }
 };
-
-// The workgroups that hold pieces of a group (hr = g * RG + rg), and its first record.
-struct Holders {
-  int rec, count;
-};
-__device__ __forceinline__ Holders holders(const QArgs& a, int per, int align, int before, int b, int hr, int ctx) {
-  const int u = aligned(units_of(a, ctx), align), start = before * a.HR + hr * u;
-  const int w0 = start / per, w1 = (start + u - 1) / per;
-  return {b * a.HR + hr + w0, w1 - w0 + 1};
-}
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ int row_t(const QArgs& a, int row) { return (int)((unsigned)row * a.g_magic >> 20); }
@@ -820,7 +724,7 @@ __device__ __forceinline__ void combine_rows(const QArgs& a, int wg, RowSum (*s_
     row = id - bg * a.R;
     b = bg / a.Hkv;
     g = bg - b * a.Hkv;
-    const Shares s_ = find<false>(a, 0, b);
+    const Shares s_ = q8_find<false>(a, Wave(a), 0, b);
     ctx = s_.ctx;
     const int rg = row / (16 * RT), tile = row / 16 - rg * RT;
     const Holders h = holders(a, s_.per, s_.align, s_.before, b, g * a.RG + rg, s_.ctx);

@@ -1,6 +1,7 @@
 // Launch plan of verify attention over an 8-bit cache: how its row tiles and
 // tokens are spread over workgroups, and where the workspace's areas lie.  Plain
-// C++, so that the plan can be run over all sizes without a GPU.
+// C++, so that the plan can be run over all sizes without a GPU, and with it the
+// arithmetic by which the kernels find their shares.
 #pragma once
 
 #include "verify_plan.h"
@@ -43,6 +44,154 @@ struct QSplit {
   size_t recs;      // partial results of RT tiles: group x of workgroup w is number x + w
   size_t off_mpart, off_stats, off_zt, off_nan, off_opart, bytes;
 };
+
+// What the shares follow from, beside the lengths.
+struct QShape {
+  int B, T, Hkv, RG;  // RG: workgroups that share a KV head's row tiles
+  int HR;             // Hkv * RG, the groups of a sequence
+  int wgs, max_ctx;
+};
+
+#if defined(__HIPCC__)
+#define PVLM_Q8_FN __host__ __device__ __forceinline__
+#else
+#define PVLM_Q8_FN inline
+#endif
+
+// A value that a wave's lanes have in common, held once for the wave.
+PVLM_Q8_FN int q8_uniform(int x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_readfirstlane(x);
+#else
+  return x;
+#endif
+}
+
+PVLM_Q8_FN int clamp_ctx(const QShape& a, int ctx) { return ctx < 0 ? 0 : ctx < a.max_ctx ? ctx : a.max_ctx; }
+PVLM_Q8_FN int units_of(const QShape& a, int ctx) { return (ctx + a.T + kQUnit - 1) / kQUnit; }
+PVLM_Q8_FN int aligned(int units, int align) { return align == 1 ? units : (units + align - 1) / align * align; }
+
+// Where the groups lie in the row of units.  Every wave finds its place from
+// the lengths: sequence b's first group begins at HR * before.  Where the shares
+// are enough for it, every group begins a share of its own (align = per; its units
+// count as a multiple of that): a share that ends one group and begins another
+// takes a round and the statistics of both (72 rows over 12800 tokens, 8 groups:
+// mass kernel 15.8 us, aligned 13.0).
+struct Shares {
+  int per;     // units of a workgroup
+  int align;   // what a group's units are rounded up to a multiple of
+  int before;  // units (of one group each) of the sequences ahead of b
+  int b, ctx;
+};
+
+// The sequence that holds the first unit of share wg (b = B: none), or sequence
+// `seq`.  Wave holds 64 sequences at a time, one a lane: load(a, b0) those from
+// b0 on; sum(align) adds their units up, to last() in all, ahead(lane) before a
+// lane's; reaching(a, b0, before, at) is the first lane whose groups end past
+// unit `at` of the row (-1: none); ctx_of(lane) its length.
+template <bool FIND_UNIT, typename Wave>
+PVLM_Q8_FN Shares q8_find(const QShape& a, Wave w, int wg, int seq) {
+  Shares s;
+  int total = 0;
+  auto add_up = [&](int b0, int align) {
+    if (b0 > 0 || a.B > 64) w.load(a, b0);
+    w.sum(align);
+  };
+  w.load(a, 0);
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    add_up(b0, 1);
+    total += w.last();
+  }
+  s.per = (total * a.HR + a.wgs - 1) / a.wgs;
+  if (s.per < kQMinUnits) s.per = kQMinUnits;
+  s.align = 1;
+  if (a.B * a.HR <= a.wgs) {  // (so the sums below stay under wgs shares and as many units of rounding)
+    int sum = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+      add_up(b0, s.per);
+      sum += w.last();
+    }
+    if ((int64_t)sum * a.HR <= (int64_t)a.wgs * s.per) s.align = s.per;
+  }
+  s.before = 0;
+  s.b = a.B;
+  s.ctx = 0;
+  // (wg * per stays within 32 bits: per exceeds total / wgs by less than one, or is the least share of few units)
+  const int at = wg * s.per;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    add_up(b0, s.align);
+    int hit = seq - b0;
+    if constexpr (FIND_UNIT) hit = w.reaching(a, b0, s.before, at);
+    if (hit >= 0 && hit < 64) {
+      s.before += w.ahead(hit);
+      s.b = b0 + hit;
+      s.ctx = w.ctx_of(hit);
+      break;
+    }
+    s.before += w.last();
+  }
+  return s;
+}
+
+// A workgroup's share as pieces of groups, one after the other.
+struct QPiece {
+  int b, g, rg, ctx;     // group: sequence, KV head, share of its row tiles
+  int c0, c1;            // its tokens (c0 opens a unit)
+  int left;              // units of the share from c0 on
+  int before, per, align;  // units of the sequences ahead of b; of a share; see Shares
+  PVLM_Q8_FN void set(const QShape& a) {
+    const int N = ctx + a.T, u = c0 / kQUnit + left;
+    c1 = q8_uniform(u > N / kQUnit ? N : u * kQUnit);
+  }
+  // The first piece of share wg, with that share's Shares; false where it is empty.
+  PVLM_Q8_FN bool begin(const QShape& a, const Shares& s, int wg) {
+    if (s.b >= a.B) return false;
+    b = s.b;
+    ctx = s.ctx;
+    before = s.before;
+    per = s.per;
+    align = s.align;
+    const int units = units_of(a, ctx), u = aligned(units, align), off = wg * per - before * a.HR;
+    const int hr = q8_uniform(off / u);
+    g = q8_uniform(hr / a.RG);
+    rg = hr - g * a.RG;
+    const int from = q8_uniform(off - hr * u);
+    left = align == 1 || per < units - from ? per : units - from;
+    c0 = from * kQUnit;
+    set(a);
+    return true;
+  }
+  // The next piece, `ctx_of(b)` giving a sequence's length; false where the share
+  // ends.  (A share that is aligned holds one piece.)
+  template <typename F>
+  PVLM_Q8_FN bool advance(const QShape& a, F ctx_of) {
+    left -= (c1 - c0 + kQUnit - 1) / kQUnit;
+    if (left <= 0) return false;
+    if (++rg == a.RG) {
+      rg = 0;
+      if (++g == a.Hkv) {
+        g = 0;
+        before += units_of(a, ctx);
+        if (++b == a.B) return false;
+        ctx = ctx_of(b);
+      }
+    }
+    c0 = 0;
+    set(a);
+    return true;
+  }
+  PVLM_Q8_FN int group(const QShape& a) const { return (b * a.Hkv + g) * a.RG + rg; }
+};
+
+// The workgroups that hold pieces of a group (hr = g * RG + rg), and its first record.
+struct Holders {
+  int rec, count;
+};
+PVLM_Q8_FN Holders holders(const QShape& a, int per, int align, int before, int b, int hr, int ctx) {
+  const int u = aligned(units_of(a, ctx), align), start = before * a.HR + hr * u;
+  const int w0 = start / per, w1 = (start + u - 1) / per;
+  return {b * a.HR + hr + w0, w1 - w0 + 1};
+}
 
 inline pvlm_status check_verify_q8(int B, int T, int Hq, int Hkv, int D, int64_t n_cap, int64_t max_ctx) {
   const pvlm_status st = check_verify(PVLM_BF16, B, T, Hq, Hkv, D, n_cap, max_ctx);

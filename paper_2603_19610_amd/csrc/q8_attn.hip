@@ -62,7 +62,8 @@ struct QArgs : QShape {
   unsigned g_magic;  // row / G == row * g_magic >> 20 for row < 640 (2^20 / G + 1; G <= 640)
   int RTT;
   float sl2;         // scale * log2(e)
-  float* mpart;      // [B][HR][waves][n_cap] mass of one wave's rows
+  float* mpart;      // [B][HR][waves][mrows] mass of one wave's rows
+  int64_t mrows;     // max_ctx + T in whole units
   float2* stats;     // [record][tile][token wave][16] (log2-domain maximum, sum) of rows
   float* zt;         // the same sums of the probabilities as P . V takes them, rounded to bf16
   uint32_t* nan;     // [record][CW] the values hold a NaN that not every row sees
@@ -655,7 +656,7 @@ q8_mass_kernel(QArgs a) {
     }
     tile_sums<RT, TPW>(a, h, t_first, tiles, real, n, gq, top, inv);
     const int vis_all = min(p.c1 - 1, p.ctx);
-    float* mp = a.mpart + ((size_t)p.group(a) * S_::RW + rw) * a.c.n_cap;
+    float* mp = a.mpart + ((size_t)p.group(a) * S_::RW + rw) * a.mrows;
     for (int t0 = p.c0; t0 < p.c1; t0 += 64 * TW) {
       lds_sync();
       const uint32_t k = k0 + slot;
@@ -815,7 +816,7 @@ __device__ __forceinline__ void sum_mass(const QArgs& a, int id) {
   const int b = id / a.mass_per;
   const int64_t t0 = (int64_t)(id - b * a.mass_per) * a.mass_rows;
   const int N = clamp_ctx(a, a.ctx_len[b]) + a.T;
-  const float* mp = a.mpart + (size_t)b * P * a.c.n_cap;
+  const float* mp = a.mpart + (size_t)b * P * a.mrows;
   float* mass = a.mass + (size_t)b * a.c.n_cap;
   for (int64_t t = t0 + threadIdx.x; t < min(t0 + a.mass_rows, a.c.n_cap); t += kFinThreads) {
     constexpr int kU = 8;  // partials in flight
@@ -824,7 +825,7 @@ __device__ __forceinline__ void sum_mass(const QArgs& a, int id) {
       for (int p0 = 0; p0 < P; p0 += kU) {
         float v[kU];
 #pragma unroll
-        for (int j = 0; j < kU; ++j) v[j] = mp[(size_t)min(p0 + j, P - 1) * a.c.n_cap + t];
+        for (int j = 0; j < kU; ++j) v[j] = mp[(size_t)min(p0 + j, P - 1) * a.mrows + t];
 #pragma unroll
         for (int j = 0; j < kU; ++j)
           if (p0 + j < P) sum += v[j];
@@ -909,6 +910,7 @@ pvlm_status verify_q8_run(int B, int T, int Hq, int Hkv, int D, int64_t max_ctx,
   a.wgs = p.wgs;
   a.sl2 = (float)((double)scale * kLog2e);
   a.mpart = reinterpret_cast<float*>(wsb + p.off_mpart);
+  a.mrows = p.mrows;
   a.stats = reinterpret_cast<float2*>(wsb + p.off_stats);
   a.zt = reinterpret_cast<float*>(wsb + p.off_zt);
   a.nan = reinterpret_cast<uint32_t*>(wsb + p.off_nan);

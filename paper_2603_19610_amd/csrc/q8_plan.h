@@ -42,6 +42,7 @@ struct QSplit {
   int RTT, RG, RT;  // their 16-row tiles, the workgroups that share them, and the tiles of one
   int wgs;          // workgroups of the partial and mass kernels
   size_t recs;      // partial results of RT tiles: group x of workgroup w is number x + w
+  int64_t mrows;    // tokens of a row of mass partials: no sequence has more
   size_t off_mpart, off_stats, off_zt, off_nan, off_opart, bytes;
 };
 
@@ -207,8 +208,7 @@ inline pvlm_status check_verify_q8(int B, int T, int Hq, int Hkv, int D, int64_t
 // The plan for arguments that check_verify_q8 takes, on `cus` compute units (a
 // workgroup's ring takes most of a unit's LDS).  It grows with `cus`, so the
 // bytes planned for the whole device are enough under every budget.
-inline void split_verify_q8(int B, int T, int Hq, int Hkv, int D, int64_t n_cap, int64_t max_ctx, int cus,
-                            QSplit* p) {
+inline void split_verify_q8(int B, int T, int Hq, int Hkv, int D, int64_t, int64_t max_ctx, int cus, QSplit* p) {
   p->G = Hq / Hkv;
   p->R = p->G * T;
   p->RTT = (p->R + 15) / 16;
@@ -220,8 +220,9 @@ inline void split_verify_q8(int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
   p->wgs = (int)(shares < cus ? shares : cus);
   p->recs = (size_t)(groups + p->wgs);
   const size_t rows = p->recs * p->RT * q8_waves(p->RT).tw * 16;
+  p->mrows = (max_ctx + T + 31) / 32 * 32;
   p->off_mpart = kSyncRegion;  // (the region at the start is other calls')
-  p->off_stats = align_up(p->off_mpart + 4 * (size_t)groups * q8_mass_waves(p->RT).rw * n_cap, 256);
+  p->off_stats = align_up(p->off_mpart + 4 * (size_t)groups * q8_mass_waves(p->RT).rw * p->mrows, 256);
   p->off_zt = align_up(p->off_stats + 8 * rows, 256);
   p->off_nan = align_up(p->off_zt + 4 * rows, 256);
   p->off_opart = align_up(p->off_nan + 4 * p->recs * q8_waves(p->RT).cw, 256);

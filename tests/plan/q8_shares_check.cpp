@@ -8,6 +8,7 @@
 //   are the workgroups that hold it, and its first record the first of them.
 //   q8_shares_check ragged    sizes of all kinds, random lengths
 //   q8_shares_check extremes  the largest unit counts that a call is taken for
+//   q8_shares_check workspace a workspace goes by the longest context, not by the cache's capacity
 //   q8_shares_check planted   one length counted a token long: has to fail
 // Built with a check of signed overflow: an index past 32 bits ends the run.
 #include <cstdint>
@@ -166,6 +167,17 @@ int main(int argc, char** argv) {
               }
             }
         }
+  } else if (!std::strcmp(what, "workspace")) {
+    for (int B : {1, 4, 64})
+      for (int T : {1, 9, 32})
+        for (int64_t ctx : {0, 31, 787, 16384})
+          for (int64_t n_cap : {32768, 131072, 1 << 30}) {
+            QSplit tight, wide;
+            split_verify_q8(B, T, 64, 8, 128, (ctx + T + 31) / 32 * 32, ctx, 256, &tight);
+            split_verify_q8(B, T, 64, 8, 128, n_cap, ctx, 256, &wide);
+            ++g_runs;
+            g_fail += tight.bytes != wide.bytes;
+          }
   } else {
     return 2;
   }

@@ -46,3 +46,31 @@ def test_graphs_of_one_capture_stream_replay_together():
             for o, w in zip(got, want):
                 assert all(torch.equal(a, b) for a, b in zip(o, w))
     assert pv.synchronize() == 0
+
+
+@pytest.mark.parametrize("B,T,Hq,Hkv,D,ctx,spare", [(2, 9, 20, 4, 128, [800, 31], 3000), (1, 32, 20, 1, 64, [333], 9000),
+                                                    (1, 1, 8, 8, 64, [0], 64)])
+def test_a_cache_with_much_room_takes_the_workspace_of_its_contexts(B, T, Hq, Hkv, D, ctx, spare):
+    """A capacity beyond the longest context changes neither the workspace nor the results, and nothing is written past
+    the workspace's end."""
+    rng = np.random.default_rng(spare)
+    tight = -(-(max(ctx) + T) // 32) * 32
+    cache = random_cache(rng, B, Hkv, tight + spare, D)
+    q = queries(rng, B, T, Hq, D)
+    n = torch.tensor(ctx, dtype=torch.int32, device="cuda")
+    n_cap = cache[0].shape[2]
+    need = pv.verify_attn_q8_workspace_size(B, T, Hq, Hkv, D, n_cap, max(ctx))
+    assert need == pv.verify_attn_q8_workspace_size(B, T, Hq, Hkv, D, tight, max(ctx))
+    buf = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+
+    class Exact:
+        def get(self, nbytes):
+            assert nbytes == need
+            return buf[:need]
+    note(f"verify q8 with {spare} spare rows")
+    got = pv.verify_attn_q8(q, *cache, n, max_ctx=max(ctx), ws=Exact())
+    want = pv.verify_attn_q8(q, *[c[:, :, :tight].contiguous() for c in cache], n, max_ctx=max(ctx))
+    torch.cuda.synchronize()
+    assert bool((buf[need:] == 0xA5).all())
+    assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+    assert torch.equal(got[1][:, :tight], want[1]) and not got[1][:, tight:].any()

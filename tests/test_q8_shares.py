@@ -27,6 +27,12 @@ def test_the_kernels_shares_hold_every_token_once(check, what):
     assert r.returncode == 0, r.stdout + r.stderr
 
 
+def test_a_workspace_does_not_grow_with_the_capacity(check):
+    """64 decoding sequences of 16384 tokens with room for 131072 once reserved 282 MB, 268 of them never touched."""
+    r = check("workspace")
+    assert r.returncode == 0, r.stdout + r.stderr
+
+
 def test_a_planted_slip_is_seen(check):
     r = check("planted")
     assert r.returncode == 1 and "plans" in r.stdout, r.stdout + r.stderr

@@ -509,7 +509,9 @@ pvlm_status pvlm_rope_append_q8_paged(pvlm_dtype dt, int B, int T, int Hq, int H
  *                 serves every layer.
  * A len[b] outside [0, min(src_cap, n_cap)] is clamped into it and flagged
  * PVLM_DEV_RANGE; a row whose page entry lies outside the pool is skipped and
- * flagged.  n_layers * B <= 65535, Hkv <= 65535, src_cap <= 2^30.
+ * flagged.  PVLM_ERR_SHAPE for n_layers * B > 65535, Hkv > 65535, src_cap > 2^30,
+ * and for min(src_cap, n_cap) * D / 8 > 2^32 - 256 (one launch, a work-item for
+ * eight values of a row).
  * ---------------------------------------------------------------------- */
 pvlm_status pvlm_quantize_kv(pvlm_dtype dt, int n_layers, int B, int Hkv, int D, int64_t src_cap,
                              const void* k_src, const void* v_src, const int32_t* len,
@@ -535,7 +537,8 @@ pvlm_status pvlm_quantize_kv_paged(pvlm_dtype dt, int n_layers, int B, int Hkv, 
  *   ws    >= pvlm_verify_attn_q8_workspace_size() bytes (under every compute-unit
  *         budget).
  * Other arguments, flags and errors are those of pvlm_verify_attn(_paged);
- * PVLM_ERR_SHAPE for B * Hq * T > 2^22.
+ * PVLM_ERR_SHAPE for B * Hq * T > 2^22, and for 4 * B * Hkv blocks of 32 rows up to
+ * max_ctx + T of more than 2^31 - 65537 in all (they are counted in 32 bits).
  * ---------------------------------------------------------------------- */
 size_t pvlm_verify_attn_q8_workspace_size(int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
                                           int64_t max_ctx);
@@ -560,13 +563,16 @@ pvlm_status pvlm_verify_attn_q8_paged(pvlm_dtype dt, int B, int T, int Hq, int H
  *   dst_dt PVLM_E4M3            an 8-bit cache again (codes and exponents copied;
  *                               dst_cap a multiple of 32), or
  *   dst_dt PVLM_BF16, PVLM_F32  the values that the rows stand for (exact, but
- *                               that a bf16 value under 2^-126 is rounded);
+ *                               that a bf16 value under 2^-126 is rounded, and
+ *                               one of 2^128 or more, which a magnitude from
+ *                               1.9375 * 2^127 on rounds to, is infinite);
  *                               k_dst_exps and v_dst_exps are then not used.
  *   fill                        0: destination rows past k[b] + tail_len[b], and
  *                               skipped ones, are left as they were; else they
  *                               are written 0 (for a destination that is new).
  * Source rows, order, clamps, flags and limits are those of
- * pvlm_gather_kv(_paged).
+ * pvlm_gather_kv(_paged); PVLM_ERR_SHAPE also for Hkv > 65535, dst_cap > 2^30, and for
+ * dst_cap * D / 16 > 2^32 - 256 (one launch, a work-item for 16 codes of a row).
  * ---------------------------------------------------------------------- */
 pvlm_status pvlm_gather_kv_q8(pvlm_dtype dst_dt, int n_layers, int B, int Hkv, int D, int64_t n_cap,
                               const uint8_t* k_codes, const uint8_t* k_exps,

@@ -144,3 +144,24 @@ def test_verify_without_mass_or_lse_gives_the_same_outputs(T, D, ctx, P):
     got = pv.verify_attn_q8(q, *cache, n, max_ctx=mc, out=given[0], mass=given[1], lse=given[2])
     for a, b, w in zip(got, given, (out, mass, lse)):
         assert a is b and torch.equal(a, w)
+
+
+@pytest.mark.parametrize("B,T,Hq,Hkv,D,ctx,P", [(1, 8, 4, 1, 64, [63], 32), (2, 32, 20, 1, 64, [90, 33], 0),
+                                                (2, 9, 64, 8, 128, [2000, 31], 64), (1, 17, 32, 2, 128, [4095], 0)])
+def test_nan_in_every_draft_row_reaches_the_rows_that_see_it(B, T, Hq, Hkv, D, ctx, P):
+    """One KV head's values: row ctx + j has a NaN in column j (mod D); a query row t has the columns 0 .. t of it."""
+    rng = np.random.default_rng(T + D)
+    cache = random_cache(rng, B, Hkv, max(ctx) + T, D)
+    q = queries(rng, B, T, Hq, D)
+    clean = run_verify(q, cache, ctx, P=P, seed=3)
+    g, G = Hkv - 1, Hq // Hkv
+    want = torch.zeros((B, T, Hq, D), dtype=torch.bool, device="cuda")
+    for b, c in enumerate(ctx):
+        for j in range(T):
+            cache[2][b, g, c + j, j % D] = 0xff if j % 2 else 0x7f
+            want[b, j:, g * G:, j % D] = True
+    note(f"verify q8 NaN in every draft row, T={T} D={D} P={P}")
+    out, mass, lse = run_verify(q, cache, ctx, P=P, seed=3)
+    assert torch.equal(torch.isnan(out), want)
+    assert torch.equal(out[~want], clean[0][~want])
+    assert torch.equal(mass, clean[1]) and torch.equal(lse, clean[2])

@@ -24,14 +24,18 @@
 //            once for all row tiles, beside waves that hold a tile of 16 rows
 //   mass     the same shares of the tokens, K alone, up to three tiles a wave
 //   finish   a wave or a workgroup joins a row's records; others sum the mass
-// What bounds them, and what they measured (one MI355X, D = 128, kernel times):
-//   memory: 16 sequences of one token, 84 MB of each of K and V: partial 38 us,
-//     4.5 TB/s.  4 sequences of 9 tokens, 117 MB each: partial 55 us, 4.3 TB/s;
-//     mass (K again) 39 us, 3.0 TB/s.
+// What bounds them, and what they measured (one MI355X, D = 128, kernel times
+// under the profiler, which slows the longer ones by up to a tenth):
+//   memory: 16 sequences of one token, 84 MB of each of K and V: partial 37.5 us,
+//     4.5 TB/s.  4 sequences of 9 tokens, 117 MB each: partial 54 to 59 us, 4.0 to
+//     4.3 TB/s; mass (K again) 41 to 43 us, 2.8 TB/s.
 //   instructions, with many rows: 136 rows a head over 132K tokens, 136 MB each:
-//     partial 114 us (0.65 PFLOP/s), mass 70 to 75 us (0.5 PFLOP/s).  Of a SIMD's
-//     cycles 37 % are matrix instructions, 47 % vector ones, of LDS's 42 % reads
-//     and writes; barriers keep the waves too close in step for more of each.
+//     partial 112 to 121 us (0.6 PFLOP/s), mass 69 to 75 us (0.5 PFLOP/s).  Of a
+//     SIMD's cycles 37 % are matrix instructions, 48 % vector ones, of LDS's 43 %
+//     reads and writes; barriers keep the waves too close in step for more of each.
+//   partial results, with few rows over few tokens: 72 rows a head over 12800 tokens
+//     write and read 18 MB of them beside 26 MB of cache (partial 19 us, mass 13,
+//     finish 7).
 //   latency in small calls: a launch that waits for the lengths, then for its
 //     first blocks (all compute units ask at once), then for its stores takes
 //     4 to 8 us.

@@ -8,10 +8,12 @@
 // maximum is a reduction over at most 16 lanes that stays in the vector unit.  They
 // are bound by HBM where there are rows enough, by a launch's latency else (one
 // MI355X, kernel times):
-//   append    80 heads of 12800 prompt rows, 0.5 GB: 97 us, 5.1 TB/s; 6 rows: 3.6 us
-//   quantise  28 layers of 6432 rows, 4 heads, 0.55 GB: 96 us, 5.7 TB/s; one of 787: 3 us
-//   gather    80 layers, 1510 rows kept, to bf16, 0.74 GB: 146 to 162 us, 4.6 to
-//             5.1 TB/s; 28 layers, 0.045 GB, copied: 10 us, 4.5 TB/s
+//   append    80 heads of 12800 prompt rows, 0.5 GB: 97 us, 5.1 TB/s; 6 rows: 3.5 us
+//   quantise  28 layers of 6432 rows, 4 heads, 0.55 GB: 95 us, 5.8 TB/s; from fp32,
+//             0.92 GB: 163 us, 5.7 TB/s; one layer of 787 rows: 3 us
+//   gather    80 layers, 1510 rows kept, to bf16, 0.74 GB: 148 to 164 us, 4.5 to
+//             5.0 TB/s; to fp32, 1.24 GB: 396 us, 3.1 TB/s (stores of 8 and 16 bytes
+//             a lane, 32 and 64 apart); 28 layers, 0.045 GB, copied: 10 us, 4.5 TB/s
 #include "q8.h"
 
 namespace pvlm {

@@ -28,7 +28,7 @@ struct QWaves {
 // conversion bounds a round, and every half has a wave of its own (3 tiles, 117 MB
 // of each of K and V: 55 us, with two halves a wave 60).  Two tiles a wave, which
 // read a block once for both, are two a SIMD or spill: 9 tiles over 132K tokens
-// took 126 to 146 us where one took 124 to 128.
+// took 126 to 146 us where one, at that step, took 124 to 128 (now 112 to 121).
 constexpr QWaves q8_waves(int RT) { return {1, RT, RT <= 6 ? 2 : 1, RT <= 4 ? 4 : 2}; }
 // The mass kernel's, with K alone and no results to hold: up to three tiles a
 // wave, which sum their rows together, and two waves a SIMD.

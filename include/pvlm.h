@@ -23,6 +23,13 @@
  *   pvlm_gather_kv_q8   append, verify and gather over a cache of 8-bit rows,
  *                       padded or paged, and the rows of a 16- or 32-bit cache
  *                       into one
+ *   pvlm_rotary_append_q4, pvlm_quantize_kv_q4, pvlm_verify_attn_q4,
+ *   pvlm_gather_kv_q4   the same over a cache of 4-bit rows
+ *   pvlm_rotary_append  rotary embedding in every layout (interleaved pairs, part
+ *                       of a head, scaled frequencies) and the append of rows by
+ *                       cache slot, for padded, paged and ragged batches
+ *   pvlm_pages_resize, pvlm_slot_map  a batch's page tables from its lengths, and
+ *                       the cache slots of its new rows
  *   pvlm_spec_accept    speculative-sampling accept/reject (Sec. 2.2) with the
  *                       bonus token of Suppl. B
  *   pvlm_set_stream_cu_budget  compute-unit budgets, so the draft's and the
@@ -99,9 +106,9 @@ typedef enum {
   PVLM_ERR_HIP = 5           /* a HIP call failed; see pvlm_last_hip_error()   */
 } pvlm_status;
 
-/* PVLM_E4M3: 8-bit cache rows (see pvlm_rope_append_q8), taken only where a call
- * says so. */
-typedef enum { PVLM_F32 = 0, PVLM_BF16 = 1, PVLM_E4M3 = 2 } pvlm_dtype;
+/* PVLM_E4M3, PVLM_E2M1: 8-bit and 4-bit cache rows (see pvlm_rope_append_q8 and
+ * pvlm_rotary_append_q4), taken only where a call says so. */
+typedef enum { PVLM_F32 = 0, PVLM_BF16 = 1, PVLM_E4M3 = 2, PVLM_E2M1 = 3 } pvlm_dtype;
 
 /* Criterion fed to UV-Prune's variation operator. */
 typedef enum {
@@ -117,6 +124,7 @@ typedef enum {
                                zero-fill the workspace again before reusing it) */
 #define PVLM_DEV_PLACEMENT 4 /* reserved: a workgroup ran on another XCD than
                                the launch planned for (no call raises it)    */
+#define PVLM_DEV_NO_PAGES 8 /* pvlm_pages_resize: too few free pages for the batch  */
 
 /* Compute-unit budget of `stream` on the current device: cus = 0 removes it
  * (calls then plan for the whole device), otherwise a multiple of the
@@ -582,6 +590,240 @@ pvlm_status pvlm_gather_kv_q8(pvlm_dtype dst_dt, int n_layers, int B, int Hkv, i
                               void* k_dst, uint8_t* k_dst_exps, void* v_dst,
                               uint8_t* v_dst_exps, int32_t* status, hipStream_t stream);
 pvlm_status pvlm_gather_kv_q8_paged(pvlm_dtype dst_dt, int n_layers, int B, int Hkv, int D,
+                                    int page_size, int max_pages, int64_t n_pages,
+                                    const uint8_t* k_codes, const uint8_t* k_exps,
+                                    const uint8_t* v_codes, const uint8_t* v_exps,
+                                    const int32_t* page_table, const int32_t* idx,
+                                    const int32_t* k, int32_t k_cap, const int32_t* tail_begin,
+                                    const int32_t* tail_len, int64_t dst_cap, int fill,
+                                    void* k_dst, uint8_t* k_dst_exps, void* v_dst,
+                                    uint8_t* v_dst_exps, int32_t* status, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Page tables and slots.  The paged calls read a page table and lengths from
+ * device memory; these two calls make them there, so that a verify step that
+ * grows its sequences, appends, verifies and rolls back (Suppl. B) needs no host
+ * between, and can be captured into a graph.
+ *
+ * pvlm_pages_resize -- the pages of every sequence for len[b] rows:
+ *   page_size, max_pages, n_pages  as pvlm_verify_attn_paged
+ *                (max_pages * page_size <= 2^30);
+ *   len         [B] rows that sequence b is to have room for;
+ *   n_held      [B] pages that it has: entries 0 .. n_held[b] - 1 of its row of the
+ *               table; updated;
+ *   page_table  [B][max_pages]; updated;
+ *   free_pages, n_free  a stack of the pages that no sequence holds:
+ *               free_pages[0 .. n_free[0]), room for n_pages; updated;
+ *   granted     [B] or NULL: 1 where the sequence has the pages that it needs, else 0.
+ * With need[b] = ceil(len[b] / page_size): first, entries need[b] .. n_held[b] - 1 go
+ * on the stack in ascending order (b, then entry) and become -1.  Then sequences
+ * take their need[b] - n_held[b] missing pages off the top in ascending order (b,
+ * then entry), so long as enough are left for all that a sequence lacks; the first
+ * for which there are not, and every later one that lacks any, gets none, keeps
+ * what it has, and PVLM_DEV_NO_PAGES is set.  Entries of the table past n_held[b],
+ * and of free_pages past n_free, that no page was moved from or to are left as
+ * they were.  The caller begins with n_held 0 and every page on the stack once.
+ * PVLM_DEV_RANGE: a length, n_held or n_free outside its range (clamped into it),
+ * an entry given back that names no page or has no room on the stack (dropped).
+ * One launch of one workgroup.  PVLM_ERR_SHAPE for sizes outside their ranges,
+ * PVLM_ERR_UNSUPPORTED for B > 4096.
+ *
+ * pvlm_slot_map -- the cache rows (slots) of a batch's new rows, for
+ * pvlm_rotary_append(_q4): row j < n_new[b] of sequence b is its row ctx_len[b] + j
+ * and lies in slot page * page_size + (ctx_len[b] + j) % page_size, page =
+ * page_table[b][(ctx_len[b] + j) / page_size].
+ *   rows_per_seq  0: packed, the rows of all sequences one after the other; else
+ *                 row j of sequence b is number b * rows_per_seq + j (as the rows of
+ *                 a [B][T] tensor), n_new[b] <= rows_per_seq, n_rows =
+ *                 B * rows_per_seq.
+ *   page_table    [B][max_pages], or NULL for a padded cache: page_size then is its
+ *                 n_cap (any from 1 to 2^30), max_pages 1, and sequence b's rows lie
+ *                 in page b (n_pages >= B).
+ *   slots         [n_rows] int64; pos [n_rows] int32 or NULL: the row's position in
+ *                 its sequence; seq [n_rows] int32 or NULL: its sequence;
+ *                 row_start [B + 1] int32 or NULL: sums of n_new, the packed rows of
+ *                 sequence b being row_start[b] .. row_start[b + 1] - 1.
+ * Entries of no row are -1 in slots and seq, 0 in pos.  A row past the table or whose
+ * page entry lies outside the pool has slot -1 and pos 0, and PVLM_DEV_RANGE is set,
+ * as for an n_new that is out of range (clamped) and packed rows past n_rows (dropped).
+ * PVLM_ERR_SHAPE for sizes outside their ranges or n_rows > 2^30,
+ * PVLM_ERR_UNSUPPORTED for B > 4096 or slots that is not 8-byte aligned.
+ * ---------------------------------------------------------------------- */
+pvlm_status pvlm_pages_resize(int B, int page_size, int max_pages, int64_t n_pages,
+                              const int32_t* len, int32_t* n_held, int32_t* page_table,
+                              int32_t* free_pages, int32_t* n_free, int32_t* granted,
+                              int32_t* status, hipStream_t stream);
+pvlm_status pvlm_slot_map(int B, int64_t n_rows, int rows_per_seq, int page_size, int max_pages,
+                          int64_t n_pages, const int32_t* page_table, const int32_t* ctx_len,
+                          const int32_t* n_new, int64_t* slots, int32_t* pos, int32_t* seq,
+                          int32_t* row_start, int32_t* status, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * pvlm_rotary_append -- pvlm_rope_append for models that pair, place or scale
+ * their rotation otherwise, and for rows that are not [B][T]: for row n < N with
+ * slot s = slots[n] >= 0, row s % block_rows of block s / block_rows of the cache,
+ *   q_out[n,h]           = rot(q_in[n,h], pos of n)
+ *   k_cache[blk,g,row]   = rot(k_in[n,g], pos of n)
+ *   v_cache[blk,g,row]   = v_in[n,g]       (bit copy)
+ * and nothing of row n for s < 0 (padding: it is neither read nor written).  Slots
+ * >= 0 are distinct (of two rows with one slot, the cache row is a mixture).  A slot
+ * past the cache is flagged PVLM_DEV_RANGE and treated as padding.
+ *   q_in, k_in, v_in  rows of [Hq][D], [Hkv][D], [Hkv][D], one every q_stride,
+ *               k_stride and v_stride elements: slices of one projection's rows, say;
+ *   k_cache, v_cache  [n_blocks][Hkv][block_rows][D]: a page pool, or a padded cache
+ *               [B][Hkv][n_cap][D] with block_rows = n_cap (slots: pvlm_slot_map);
+ *   pos         [N] int32, or [3][N] with M-RoPE sections; q_out [N][Hq][D].
+ * rot turns the first rot_dim values of a head and leaves the rest (a bit copy): pair
+ * i < rot_dim / 2 by the angle p * f_i, both results times mscale,
+ *   layout   PVLM_ROPE_HALF: elements (i, i + rot_dim / 2); PVLM_ROPE_INTERLEAVED:
+ *            (2 i, 2 i + 1);
+ *   scaling  with w_i = base^(-2 i / rot_dim),
+ *            PVLM_ROPE_UNSCALED  f_i = w_i;
+ *            PVLM_ROPE_LINEAR    f_i = w_i / factor (position interpolation);
+ *            PVLM_ROPE_PARTS     f_i = w_i (c + (1 - c) / factor), c =
+ *                                clamp((r_i - alpha) / (beta - alpha), 0, 1), r_i =
+ *                                orig_ctx w_i / (2 pi): pairs that turn beta times or
+ *                                more over the original context stay, those that turn
+ *                                alpha times or less are interpolated ("NTK by parts",
+ *                                YaRN Sec. 3.2; also the form by wavelengths, with its
+ *                                low and high frequency factors alpha and beta);
+ *            PVLM_ROPE_YARN      the same with c linear in the pair's number: c = 1 -
+ *                                clamp((i - lo) / max(hi - lo, 0.001), 0, 1), lo =
+ *                                max(floor(d(beta)), 0), hi = min(ceil(d(alpha)),
+ *                                rot_dim - 1), d(x) = rot_dim / 2 *
+ *                                ln(orig_ctx / (2 pi x)) / ln(base), where pairs turn x
+ *                                times;
+ *   mscale   1, or the attention factor of a scaled model (YaRN: 0.1 ln factor + 1);
+ *   sections all 0: 1-D positions; else three widths that sum to rot_dim / 2, as
+ *            pvlm_rope_append's.
+ * Angles, sines, cosines and the rotation are float64; results are rounded to fp32,
+ * then to dt.  dt PVLM_BF16 or PVLM_F32.  q_out may be q_in where q_stride = Hq * D;
+ * no other output may alias an input.
+ * Errors: PVLM_ERR_NULL for a NULL pointer; PVLM_ERR_SHAPE for a size < 1, Hq not a
+ * multiple of Hkv, D not a multiple of 8 or > 256, rot_dim not a multiple of 8 or
+ * outside [8, D], a stride shorter than its row, block_rows > 2^30, n_blocks >= 2^31, N >
+ * 2^24 - 1, Hq + 2 * Hkv > 65536, base not finite and > 1, or parameters that the scaling
+ * uses not finite and > 0 (beta > alpha); PVLM_ERR_UNSUPPORTED for another dtype, strides
+ * that are not multiples of 8, tensors that are not 16-byte aligned (slots: 8).
+ *
+ * pvlm_rotary_freqs (host only): the rot_dim / 2 frequencies f_i of a pvlm_rotary.
+ * ---------------------------------------------------------------------- */
+typedef enum { PVLM_ROPE_HALF = 0, PVLM_ROPE_INTERLEAVED = 1 } pvlm_rope_layout;
+typedef enum {
+  PVLM_ROPE_UNSCALED = 0,
+  PVLM_ROPE_LINEAR = 1,
+  PVLM_ROPE_PARTS = 2,
+  PVLM_ROPE_YARN = 3
+} pvlm_rope_scaling;
+
+typedef struct {
+  double base, factor, orig_ctx, alpha, beta, mscale;
+  int32_t rot_dim, layout, scaling;
+  int32_t sections[3];
+} pvlm_rotary;
+
+pvlm_status pvlm_rotary_freqs(const pvlm_rotary* rot, double* freqs);
+pvlm_status pvlm_rotary_append(pvlm_dtype dt, int64_t N, int Hq, int Hkv, int D,
+                               const pvlm_rotary* rot, const int32_t* pos, const void* q_in,
+                               int64_t q_stride, const void* k_in, int64_t k_stride,
+                               const void* v_in, int64_t v_stride, const int64_t* slots,
+                               int64_t n_blocks, int64_t block_rows, void* q_out, void* k_cache,
+                               void* v_cache, int32_t* status, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * 4-bit caches.  A quarter of a bf16 cache's bytes (and 1/16 for the exponents).
+ *
+ * A row x of D values (one position, one KV head, K or V) is D / 32 blocks of 32
+ * consecutive values.  A block is 32 e2m1 codes (sign, 2 exponent bits, 1 mantissa
+ * bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), two in a byte with the first in its low half,
+ * and one exponent byte e, and stands for code_i * 2^(e - 127):
+ *   e      = the smallest integer in [1, 254] with max |x_i| <= 7 * 2^(e - 127) over
+ *            the block, or 255, all 32 values NaN, where an x_i is infinite or NaN;
+ *   code_i = x_i * 2^(127 - e) rounded to nearest, ties to the even code, at most 6
+ *            (0 where e = 255).
+ * The scaling is exact, so a value is off by at most half a step: a quarter of the
+ * power of two below it, 2^(e - 129) under 2^(e - 127), 2^(e - 127) over 6.
+ *   padded  codes [B][Hkv][n_cap][D / 2], exponents [B][Hkv][n_cap][D / 32]; n_cap is
+ *           a multiple of 32 (PVLM_ERR_SHAPE).
+ *   paged   codes [n_pages][Hkv][page_size][D / 2], exponents [n_pages][Hkv]
+ *           [page_size][D / 32], page_size and page_table as for
+ *           pvlm_verify_attn_paged; logical capacity n_cap = max_pages * page_size.
+ * Of a cache written by other means an exponent byte 0 stands for 2^-127.
+ * D is 64 or 128 (PVLM_ERR_UNSUPPORTED).  Pointers of codes, q, sources, bf16 or fp32
+ * destinations and workspaces are 16-byte aligned, of exponents 4-byte
+ * (PVLM_ERR_UNSUPPORTED, PVLM_ERR_WORKSPACE for the last).  None of these launches
+ * waits for another workgroup, captured or not.
+ *
+ * pvlm_rotary_append_q4 -- pvlm_rotary_append (dt PVLM_BF16) into a 4-bit cache of
+ * n_blocks blocks of block_rows rows: rotated keys are rounded to bf16 and then
+ * quantised, values quantised, so the rows are those that pvlm_quantize_kv_q4 makes of
+ * the cache that pvlm_rotary_append writes.
+ * ---------------------------------------------------------------------- */
+pvlm_status pvlm_rotary_append_q4(pvlm_dtype dt, int64_t N, int Hq, int Hkv, int D,
+                                  const pvlm_rotary* rot, const int32_t* pos, const void* q_in,
+                                  int64_t q_stride, const void* k_in, int64_t k_stride,
+                                  const void* v_in, int64_t v_stride, const int64_t* slots,
+                                  int64_t n_blocks, int64_t block_rows, void* q_out,
+                                  uint8_t* k_codes, uint8_t* k_exps, uint8_t* v_codes,
+                                  uint8_t* v_exps, int32_t* status, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * pvlm_quantize_kv_q4(_paged) -- pvlm_quantize_kv(_paged) into a 4-bit cache:
+ * arguments, flags, limits and errors are those.
+ * ---------------------------------------------------------------------- */
+pvlm_status pvlm_quantize_kv_q4(pvlm_dtype dt, int n_layers, int B, int Hkv, int D, int64_t src_cap,
+                                const void* k_src, const void* v_src, const int32_t* len,
+                                int64_t n_cap, uint8_t* k_codes, uint8_t* k_exps, uint8_t* v_codes,
+                                uint8_t* v_exps, int32_t* status, hipStream_t stream);
+pvlm_status pvlm_quantize_kv_q4_paged(pvlm_dtype dt, int n_layers, int B, int Hkv, int D,
+                                      int page_size, int max_pages, int64_t n_pages,
+                                      int64_t src_cap, const void* k_src, const void* v_src,
+                                      const int32_t* len, const int32_t* page_table,
+                                      uint8_t* k_codes, uint8_t* k_exps, uint8_t* v_codes,
+                                      uint8_t* v_exps, int32_t* status, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * pvlm_verify_attn_q4(_paged) -- pvlm_verify_attn_q8(_paged) over a 4-bit cache, with
+ * that call's types, its limit on values, and its treatment of NaN (a block of
+ * exponent 255 in K or V reaches the rows that see it and no other; rows at and past
+ * ctx_len[b] + T are not used, whatever they hold).
+ *   ws    >= pvlm_verify_attn_q4_workspace_size() bytes (under every compute-unit
+ *         budget).
+ * Arguments, flags and errors are those of that call; PVLM_ERR_SHAPE for 5 * B * Hkv
+ * blocks of 32 rows up to max_ctx + T of more than 2^31 - 65537 in all, and for B > 65535.
+ * ---------------------------------------------------------------------- */
+size_t pvlm_verify_attn_q4_workspace_size(int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
+                                          int64_t max_ctx);
+pvlm_status pvlm_verify_attn_q4(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
+                                int64_t max_ctx, float scale, const void* q,
+                                const uint8_t* k_codes, const uint8_t* k_exps,
+                                const uint8_t* v_codes, const uint8_t* v_exps,
+                                const int32_t* ctx_len, void* out, float* mass, float* lse,
+                                void* ws, size_t ws_bytes, int32_t* status, hipStream_t stream);
+pvlm_status pvlm_verify_attn_q4_paged(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D,
+                                      int page_size, int max_pages, int64_t n_pages,
+                                      int64_t max_ctx, float scale, const void* q,
+                                      const uint8_t* k_codes, const uint8_t* k_exps,
+                                      const uint8_t* v_codes, const uint8_t* v_exps,
+                                      const int32_t* page_table, const int32_t* ctx_len, void* out,
+                                      float* mass, float* lse, void* ws, size_t ws_bytes,
+                                      int32_t* status, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * pvlm_gather_kv_q4(_paged) -- pvlm_gather_kv_q8(_paged) from a 4-bit cache, with
+ * dst_dt PVLM_E2M1 for a 4-bit destination (dst_cap a multiple of 32), or PVLM_BF16 or
+ * PVLM_F32 for the values that the rows stand for (exact, but that a bf16 value of
+ * 2^128 or more is infinite).  k_cap = 0 with a tail reads a run of rows back.
+ * Arguments, fill, flags, limits and errors are otherwise those.
+ * ---------------------------------------------------------------------- */
+pvlm_status pvlm_gather_kv_q4(pvlm_dtype dst_dt, int n_layers, int B, int Hkv, int D, int64_t n_cap,
+                              const uint8_t* k_codes, const uint8_t* k_exps,
+                              const uint8_t* v_codes, const uint8_t* v_exps, const int32_t* idx,
+                              const int32_t* k, int32_t k_cap, const int32_t* tail_begin,
+                              const int32_t* tail_len, int64_t dst_cap, int fill,
+                              void* k_dst, uint8_t* k_dst_exps, void* v_dst,
+                              uint8_t* v_dst_exps, int32_t* status, hipStream_t stream);
+pvlm_status pvlm_gather_kv_q4_paged(pvlm_dtype dst_dt, int n_layers, int B, int Hkv, int D,
                                     int page_size, int max_pages, int64_t n_pages,
                                     const uint8_t* k_codes, const uint8_t* k_exps,
                                     const uint8_t* v_codes, const uint8_t* v_exps,

@@ -20,9 +20,9 @@ import torch
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libpvlm.so")
 
-PVLM_F32, PVLM_BF16, PVLM_E4M3 = 0, 1, 2
+PVLM_F32, PVLM_BF16, PVLM_E4M3, PVLM_E2M1 = 0, 1, 2, 3
 PVLM_CRIT_MASS, PVLM_CRIT_COSSIM = 0, 1
-PVLM_DEV_RANGE, PVLM_DEV_TIMEOUT, PVLM_DEV_PLACEMENT = 1, 2, 4
+PVLM_DEV_RANGE, PVLM_DEV_TIMEOUT, PVLM_DEV_PLACEMENT, PVLM_DEV_NO_PAGES = 1, 2, 4, 8
 
 EXPORTS = (
     "pvlm_status_string", "pvlm_last_hip_error", "pvlm_version",
@@ -36,6 +36,10 @@ EXPORTS = (
     "pvlm_rope_append_q8", "pvlm_rope_append_q8_paged", "pvlm_quantize_kv", "pvlm_quantize_kv_paged",
     "pvlm_verify_attn_q8_workspace_size", "pvlm_verify_attn_q8", "pvlm_verify_attn_q8_paged",
     "pvlm_gather_kv_q8", "pvlm_gather_kv_q8_paged",
+    "pvlm_pages_resize", "pvlm_slot_map", "pvlm_rotary_freqs", "pvlm_rotary_append", "pvlm_rotary_append_q4",
+    "pvlm_quantize_kv_q4", "pvlm_quantize_kv_q4_paged",
+    "pvlm_verify_attn_q4_workspace_size", "pvlm_verify_attn_q4", "pvlm_verify_attn_q4_paged",
+    "pvlm_gather_kv_q4", "pvlm_gather_kv_q4_paged",
     "pvlm_spec_accept_workspace_size", "pvlm_spec_accept",
     "pvlm_rope_append", "pvlm_rope_append_paged",
     "pvlm_speedup", "pvlm_window_size",
@@ -98,6 +102,16 @@ class PdStats(_c.Structure):
                 ("target_rounds", _c.c_int32), ("max_draft_run", _c.c_int32),
                 ("draft_keep", _c.c_int32), ("elapsed", _c.c_double)]
 
+
+class RotaryParams(_c.Structure):
+    """pvlm_rotary: how a model rotates its heads (see ``Rotary``)."""
+    _fields_ = ([(n, _c.c_double) for n in ("base", "factor", "orig_ctx", "alpha", "beta", "mscale")]
+                + [("rot_dim", _c.c_int32), ("layout", _c.c_int32), ("scaling", _c.c_int32),
+                   ("sections", _c.c_int32 * 3)])
+
+
+_ROTARY = [_I, _I64, _I, _I, _I, _c.POINTER(RotaryParams), _P, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _I64]
+
 _SIGS = {
     "pvlm_status_string": (_c.c_char_p, [_I]),
     "pvlm_last_hip_error": (_c.c_char_p, []),
@@ -147,6 +161,11 @@ _SIGS = {
                           + [_P] * 6),
     "pvlm_gather_kv_q8_paged": (_I, [_I, _I, _I, _I, _I, _I, _I, _I64, _P, _P, _P, _P, _P, _P, _P,
                                      _I, _P, _P, _I64, _I] + [_P] * 6),
+    "pvlm_pages_resize": (_I, [_I, _I, _I, _I64] + [_P] * 8),
+    "pvlm_slot_map": (_I, [_I, _I64, _I, _I, _I, _I64] + [_P] * 9),
+    "pvlm_rotary_freqs": (_I, [_c.POINTER(RotaryParams), _c.POINTER(_D)]),
+    "pvlm_rotary_append": (_I, _ROTARY + [_P] * 5),
+    "pvlm_rotary_append_q4": (_I, _ROTARY + [_P] * 7),
     "pvlm_pd_create": (_I, [_I, _D, _I, _c.POINTER(_P)]),
     "pvlm_pd_destroy": (None, [_P]),
     "pvlm_pd_start": (_I, [_P, _P]),
@@ -156,6 +175,11 @@ _SIGS = {
     "pvlm_pd_pending": (_I, [_P, _P, _I, _c.POINTER(_I)]),
     "pvlm_pd_get_stats": (_I, [_P, _c.POINTER(PdStats)]),
 }
+
+for _n in ("quantize_kv", "verify_attn", "gather_kv"):   # the same arguments as the 8-bit calls
+    for _x in ("", "_paged"):
+        _SIGS[f"pvlm_{_n}_q4{_x}"] = _SIGS[f"pvlm_{_n}{'' if _n == 'quantize_kv' else '_q8'}{_x}"]
+_SIGS["pvlm_verify_attn_q4_workspace_size"] = _SIGS["pvlm_verify_attn_q8_workspace_size"]
 
 
 def lib():
@@ -311,7 +335,7 @@ def synchronize(raise_on_status: bool = True) -> int:
 
 def _flag_text(flags: int) -> str:
     names = [(PVLM_DEV_RANGE, "device size out of range"), (PVLM_DEV_TIMEOUT, "wait gave up"),
-             (PVLM_DEV_PLACEMENT, "workgroup placement")]
+             (PVLM_DEV_PLACEMENT, "workgroup placement"), (PVLM_DEV_NO_PAGES, "too few free pages")]
     return ", ".join(n for bit, n in names if flags & bit)
 
 
@@ -724,10 +748,13 @@ __all__ = [
     "rope_append_q8", "rope_append_q8_paged", "quantize_kv", "quantize_kv_paged",
     "verify_attn_q8", "verify_attn_q8_paged", "verify_attn_q8_workspace_size",
     "gather_kv_q8", "gather_kv_q8_paged",
+    "pages_resize", "slot_map", "Rotary", "rotary_append", "rotary_append_q4", "quantize_kv_q4",
+    "quantize_kv_q4_paged", "verify_attn_q4", "verify_attn_q4_paged", "verify_attn_q4_workspace_size",
+    "gather_kv_q4", "gather_kv_q4_paged",
     "verify_attn_workspace_size", "uvprune_score_mass", "uvprune_score_cossim",
     "uvprune_criterion_cossim", "prefill_epilogue_cossim", "topk_select", "uvprune_topk_mass", "gather_kv", "spec_accept",
-    "PVLM_F32", "PVLM_BF16", "PVLM_E4M3", "PVLM_CRIT_MASS", "PVLM_CRIT_COSSIM", "PVLM_DEV_RANGE",
-    "PVLM_DEV_TIMEOUT", "PVLM_DEV_PLACEMENT",
+    "PVLM_F32", "PVLM_BF16", "PVLM_E4M3", "PVLM_E2M1", "PVLM_CRIT_MASS", "PVLM_CRIT_COSSIM", "PVLM_DEV_RANGE",
+    "PVLM_DEV_TIMEOUT", "PVLM_DEV_PLACEMENT", "PVLM_DEV_NO_PAGES",
 ]
 
 
@@ -1158,3 +1185,366 @@ def gather_kv_q8_paged(k_codes, k_exps, v_codes, v_exps, page_table, idx, k, tai
         raise TypeError("page_table must be a torch.Tensor")
     return _gather_q8((k_codes, k_exps, v_codes, v_exps), page_table, idx, k, tail_begin, tail_len, dst_cap,
                       dtype, dst, status)
+
+
+# ------------------------------------------------------- page tables, slots --
+def _here(t, name, dtype):
+    """A contiguous tensor on the current device (whose stream a call is enqueued on)."""
+    _need(t, name, dtype)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+    return t.device
+
+
+def pages_resize(length, n_held, page_table, free_pages, n_free, *, page_size: int, granted=None, status=None):
+    """pvlm_pages_resize: room for length[b] rows in every sequence's pages, from
+    and to a stack of free ones.  length, n_held [B]; page_table [B][max_pages];
+    free_pages [n_pages]; n_free [1], all int32; n_held, page_table, free_pages
+    and n_free are updated.  Returns granted [B] (1: the sequence has what it needs)."""
+    dev = _here(length, "length", torch.int32)
+    for t, name in ((n_held, "n_held"), (free_pages, "free_pages"), (n_free, "n_free")):
+        _need(t, name, torch.int32, dev)
+    if length.dim() != 1 or free_pages.dim() != 1 or n_free.numel() != 1:
+        raise ValueError("length must be [B], free_pages [n_pages] and n_free [1]")
+    B = length.shape[0]
+    max_pages = _need_table(page_table, dev, B)
+    if n_held.shape != (B,):
+        raise ValueError("n_held must be [B]")
+    if granted is None:
+        granted = torch.empty(B, dtype=torch.int32, device=dev)
+    elif _need(granted, "granted", torch.int32, dev).shape != (B,):
+        raise ValueError("granted must be [B]")
+    st = lib().pvlm_pages_resize(B, page_size, max_pages, free_pages.shape[0], length.data_ptr(), n_held.data_ptr(),
+                                 page_table.data_ptr(), free_pages.data_ptr(), n_free.data_ptr(), granted.data_ptr(),
+                                 _ptr(_status(status)), _stream())
+    _check(st, "pvlm_pages_resize")
+    return granted
+
+
+def slot_map(ctx_len, n_new, n_rows: int, *, page_size: int, n_pages: int, page_table=None, rows_per_seq: int = 0,
+             want_pos: bool = True, want_seq: bool = True, want_start: bool = True, status=None):
+    """pvlm_slot_map: the cache slots of n_new[b] new rows behind ctx_len[b] of every
+    sequence, packed or rows_per_seq apart, in a paged cache or (page_table None,
+    page_size its n_cap, n_pages its B) a padded one.  Returns (slots [n_rows]
+    int64, pos [n_rows], seq [n_rows], row_start [B + 1]); -1 in slots and seq
+    where there is no row.  What is not wanted is None."""
+    dev = _here(ctx_len, "ctx_len", torch.int32)
+    _need(n_new, "n_new", torch.int32, dev)
+    if ctx_len.dim() != 1 or n_new.shape != ctx_len.shape:
+        raise ValueError("ctx_len and n_new must be [B]")
+    B = ctx_len.shape[0]
+    max_pages = 1 if page_table is None else _need_table(page_table, dev, B)
+    if page_table is None and n_pages < B:
+        raise ValueError("a padded cache has a page for each sequence")
+    n_rows = int(n_rows)
+    slots = torch.empty(n_rows, dtype=torch.int64, device=dev)
+    pos = torch.empty(n_rows, dtype=torch.int32, device=dev) if want_pos else None
+    seq = torch.empty(n_rows, dtype=torch.int32, device=dev) if want_seq else None
+    start = torch.empty(B + 1, dtype=torch.int32, device=dev) if want_start else None
+    st = lib().pvlm_slot_map(B, n_rows, rows_per_seq, page_size, max_pages, n_pages, _ptr(page_table),
+                             ctx_len.data_ptr(), n_new.data_ptr(), slots.data_ptr(), _ptr(pos), _ptr(seq), _ptr(start),
+                             _ptr(_status(status)), _stream())
+    _check(st, "pvlm_slot_map")
+    return slots, pos, seq, start
+
+
+# -------------------------------------------------------------- rotary rows --
+_LAYOUTS = {"half": 0, "interleaved": 1}
+_SCALINGS = {None: 0, "": 0, "linear": 1, "parts": 2, "yarn": 3}
+
+
+class Rotary:
+    """A model's rotation (pvlm_rotary): the first ``rot_dim`` values of a head, in
+    pairs ``layout`` "half" (i, i + rot_dim / 2) or "interleaved" (2 i, 2 i + 1);
+    ``scaling`` None, "linear" (factor), "parts" or "yarn" (factor, orig_ctx, alpha,
+    beta); ``mscale`` times the result; ``sections`` for M-RoPE."""
+
+    def __init__(self, *, rot_dim: int, base: float, layout: str = "half", scaling=None, factor: float = 1.0,
+                 orig_ctx: float = 0.0, alpha: float = 0.0, beta: float = 0.0, mscale: float = 1.0, sections=None):
+        if layout not in _LAYOUTS:
+            raise ValueError(f"layout must be one of {sorted(_LAYOUTS)}")
+        if scaling not in _SCALINGS:
+            raise ValueError("scaling must be None, 'linear', 'parts' or 'yarn'")
+        if sections is not None and (len(sections) != 3 or not any(sections)):
+            raise ValueError("sections must be three widths")
+        self.params = RotaryParams(float(base), float(factor), float(orig_ctx), float(alpha), float(beta),
+                                   float(mscale), int(rot_dim), _LAYOUTS[layout], _SCALINGS[scaling],
+                                   (_c.c_int32 * 3)(*[int(x) for x in (sections or (0, 0, 0))]))
+        self.sections = None if sections is None else tuple(int(x) for x in sections)
+        self.frequencies()      # (parameters that have none are refused here)
+
+    def frequencies(self):
+        """The angle per position of every pair (host floats)."""
+        n = max(self.params.rot_dim // 2, 1)
+        f = (_D * n)()
+        if n > 128:
+            raise ValueError("rot_dim must be at most 256")
+        _check(lib().pvlm_rotary_freqs(_c.byref(self.params), f), "pvlm_rotary_freqs")
+        return list(f)
+
+
+def _row_stride(t, name, N, H, D, dtype, dev):
+    """The stride of rows [N][H][D] whose heads lie together."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device != dev or t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype} on {dev}")
+    if t.shape != (N, H, D):
+        raise ValueError(f"{name} must be [{N}][{H}][{D}]")
+    s = t.stride()
+    if (D > 1 and s[2] != 1) or (H > 1 and s[1] != D):
+        raise ValueError(f"the heads of a row of {name} must lie together")
+    return s[0] if N > 1 else H * D
+
+
+def _rotary(q, k_new, v_new, pos, slots, rotary, dtype, dev, heads, q_out):
+    """What both appends check of their rows; the arguments that they share."""
+    if not isinstance(rotary, Rotary):
+        raise TypeError("rotary must be a Rotary")
+    if q.dim() != 3:
+        raise ValueError("q must be [N][Hq][D]")
+    N, Hq, D = q.shape
+    Hkv, Dc = heads
+    if Dc != D:
+        raise ValueError("the cache's rows do not have q's D")
+    sq = _row_stride(q, "q", N, Hq, D, dtype, dev)
+    sk = _row_stride(k_new, "k_new", N, Hkv, D, dtype, dev)
+    sv = _row_stride(v_new, "v_new", N, Hkv, D, dtype, dev)
+    _need(pos, "pos", torch.int32, dev)
+    if pos.shape != ((N,) if rotary.sections is None else (3, N)):
+        raise ValueError("pos must be [N], or [3][N] with sections")
+    if _need(slots, "slots", torch.int64, dev).shape != (N,):
+        raise ValueError("slots must be [N]")
+    if q_out is None:
+        q_out = torch.empty((N, Hq, D), dtype=dtype, device=dev)
+    elif _need(q_out, "q_out", dtype, dev).shape != q.shape:
+        raise ValueError("q_out must have q's shape")
+    return q_out, (N, Hq, Hkv, D, _c.byref(rotary.params), pos.data_ptr(), q.data_ptr(), sq, k_new.data_ptr(), sk,
+                   v_new.data_ptr(), sv, slots.data_ptr())
+
+
+def rotary_append(q, k_new, v_new, pos, slots, k_cache, v_cache, *, rotary: Rotary, q_out=None, status=None):
+    """pvlm_rotary_append: rows q [N][Hq][D], k_new and v_new [N][Hkv][D] (views with
+    a row stride are taken as they are), rotated by their positions pos [N] or
+    [3][N] and appended at slots [N] (int64, -1: padding) of caches
+    [blocks][Hkv][rows][D], padded or a page pool.  Returns q_out; its rows of padding
+    are not written."""
+    dev = _here(k_cache, "k_cache", None)
+    _need(v_cache, "v_cache", k_cache.dtype, dev)
+    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
+        raise ValueError("caches must be [blocks][Hkv][rows][D]")
+    n_blocks, Hkv, rows, D = k_cache.shape
+    q_out, args = _rotary(q, k_new, v_new, pos, slots, rotary, k_cache.dtype, dev, (Hkv, D), q_out)
+    st = lib().pvlm_rotary_append(_dt(k_cache), *args, n_blocks, rows, q_out.data_ptr(), k_cache.data_ptr(),
+                                  v_cache.data_ptr(), _ptr(_status(status)), _stream())
+    _check(st, "pvlm_rotary_append")
+    return q_out
+
+
+# ------------------------------------------------------------ 4-bit caches --
+# Codes are torch.uint8 (two in a byte) or torch.float4_e2m1fn_x2, exponents
+# torch.uint8, one for 32 values: a value is code * 2^(exponent - 127).
+def _need_q4(k_codes, k_exps, v_codes, v_exps, dev, paged, stacked=False):
+    """Check a cache's four tensors; returns the values' shape."""
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {dev}, but the current device is cuda:{torch.cuda.current_device()}")
+    for t, name in ((k_codes, "k_codes"), (v_codes, "v_codes")):
+        _need(t, name, None, dev)
+        if t.dtype is not torch.uint8 and t.dtype is not torch.float4_e2m1fn_x2:
+            raise ValueError(f"{name} must be torch.uint8 or torch.float4_e2m1fn_x2, got {t.dtype}")
+    _need(k_exps, "k_exps", torch.uint8, dev)
+    _need(v_exps, "v_exps", torch.uint8, dev)
+    shape = k_codes.shape
+    if len(shape) != 4 and not (stacked and len(shape) == 5):
+        layout = "[n_pages][Hkv][page][D / 2]" if paged else "[B][Hkv][n_cap][D / 2]"
+        raise ValueError(f"codes must be {layout}" + (f" or [L]{layout}" if stacked else ""))
+    D = 2 * shape[-1]
+    if D not in (64, 128):
+        raise ValueError("D must be 64 or 128 (codes of D / 2 bytes)")
+    exps = shape[:-1] + (D // 32,)
+    if v_codes.shape != shape or k_exps.shape != exps or v_exps.shape != exps:
+        raise ValueError("k_codes and v_codes must have one shape, k_exps and v_exps that shape with D / 32")
+    return shape[:-1] + (D,)
+
+
+def rotary_append_q4(q, k_new, v_new, pos, slots, k_codes, k_exps, v_codes, v_exps, *, rotary: Rotary, q_out=None,
+                     status=None):
+    """pvlm_rotary_append_q4: ``rotary_append`` (bf16) into a 4-bit cache, codes
+    [blocks][Hkv][rows][D / 2] and exponents [blocks][Hkv][rows][D / 32].  Returns q_out."""
+    cache = (k_codes, k_exps, v_codes, v_exps)
+    dev = _here(k_codes, "k_codes", None)
+    n_blocks, Hkv, rows, D = _need_q4(*cache, dev, True)
+    q_out, args = _rotary(q, k_new, v_new, pos, slots, rotary, torch.bfloat16, dev, (Hkv, D), q_out)
+    st = lib().pvlm_rotary_append_q4(PVLM_BF16, *args, n_blocks, rows, q_out.data_ptr(), *[t.data_ptr() for t in cache],
+                                     _ptr(_status(status)), _stream())
+    _check(st, "pvlm_rotary_append_q4")
+    return q_out
+
+
+def _quantize_q4(k, v, length, cache, page_table, status):
+    _need(k, "k")
+    dev = k.device
+    _need(v, "v", k.dtype, dev)
+    _need(length, "length", torch.int32, dev)
+    shape = _need_q4(*cache, dev, page_table is not None, stacked=True)
+    if k.dim() != len(shape) or v.shape != k.shape:
+        raise ValueError("k and v must be [B][Hkv][src_cap][D], or [L][...] with a stacked cache")
+    L = 1 if k.dim() == 4 else k.shape[0]
+    B, Hkv, src_cap, D = k.shape[-4:]
+    n0, H, rows, Dc = shape[-4:]
+    if (H, Dc) != (Hkv, D) or (len(shape) == 5 and shape[0] != L) or (page_table is None and n0 != B):
+        raise ValueError("the 4-bit cache does not match k and v")
+    if length.shape != (B,):
+        raise ValueError("length must be [B]")
+    codes = [t.data_ptr() for t in cache]
+    tail = (k.data_ptr(), v.data_ptr(), length.data_ptr())
+    if page_table is None:
+        name, geom, more = "pvlm_quantize_kv_q4", (src_cap, *tail, rows), ()
+    else:
+        name, geom = "pvlm_quantize_kv_q4_paged", (rows, _need_table(page_table, dev, B), n0, src_cap, *tail)
+        more = (page_table.data_ptr(),)
+    st = getattr(lib(), name)(_dt(k), L, B, Hkv, D, *geom, *more, *codes, _ptr(_status(status)), _stream())
+    _check(st, name)
+
+
+def quantize_kv_q4(k, v, length, k_codes, k_exps, v_codes, v_exps, *, status=None):
+    """pvlm_quantize_kv_q4: ``quantize_kv`` into a 4-bit cache: rows 0 .. length[b] - 1
+    of [B][Hkv][src_cap][D] (or [L][...]) to codes [B][Hkv][n_cap][D / 2]."""
+    _quantize_q4(k, v, length, (k_codes, k_exps, v_codes, v_exps), None, status)
+
+
+def quantize_kv_q4_paged(k, v, length, k_codes, k_exps, v_codes, v_exps, page_table, *, status=None):
+    """pvlm_quantize_kv_q4_paged: the same into pools [n_pages][Hkv][page][D / 2] (or
+    [L][...]; one page_table [B][max_pages] serves every layer)."""
+    if page_table is None:
+        raise TypeError("page_table must be a torch.Tensor")
+    _quantize_q4(k, v, length, (k_codes, k_exps, v_codes, v_exps), page_table, status)
+
+
+def verify_attn_q4_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx) -> int:
+    return int(lib().pvlm_verify_attn_q4_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx))
+
+
+def _verify_q4(q, cache, page_table, ctx_len, scale, max_ctx, out, mass, lse, want_mass, want_lse, ws, status):
+    _need(q, "q", torch.bfloat16)
+    dev = q.device
+    n0, Hkv, rows, Dc = _need_q4(*cache, dev, page_table is not None)
+    _need(ctx_len, "ctx_len", torch.int32, dev)
+    if q.dim() != 4:
+        raise ValueError("q must be [B][T][Hq][D]")
+    B, T, Hq, D = q.shape
+    if Dc != D or ctx_len.shape != (B,) or (page_table is None and n0 != B):
+        raise ValueError("inconsistent verify_attn_q4 shapes")
+    if page_table is None:
+        n_cap, geom, table = rows, (rows,), ()
+    else:
+        max_pages = _need_table(page_table, dev, B)
+        n_cap, geom, table = max_pages * rows, (rows, max_pages, n0), (page_table.data_ptr(),)
+    if max_ctx is None:
+        max_ctx = n_cap - T
+    if out is None:
+        out = torch.empty_like(q)
+    elif _need(out, "out", torch.bfloat16, dev).shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if mass is None:
+        mass = torch.empty((B, n_cap), dtype=torch.float32, device=dev) if want_mass else None
+    elif _need(mass, "mass", torch.float32, dev).shape != (B, n_cap):
+        raise ValueError("mass must be [B][n_cap]")
+    if lse is None:
+        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=dev) if want_lse else None
+    elif _need(lse, "lse", torch.float32, dev).shape != (B, Hq, T):
+        raise ValueError("lse must be [B][Hq][T]")
+    L = lib()
+    wsb = _ws_buffer("verify_q4", ws, L.pvlm_verify_attn_q4_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx), dev)
+    name = "pvlm_verify_attn_q4" if page_table is None else "pvlm_verify_attn_q4_paged"
+    st = getattr(L, name)(PVLM_BF16, B, T, Hq, Hkv, D, *geom, max_ctx,
+                          float(D ** -0.5 if scale is None else scale), q.data_ptr(),
+                          *[t.data_ptr() for t in cache], *table, ctx_len.data_ptr(), out.data_ptr(), _ptr(mass),
+                          _ptr(lse), wsb.data_ptr(), wsb.numel(), _ptr(_status(status)), _stream())
+    _check(st, name)
+    return out, mass, lse
+
+
+def verify_attn_q4(q, k_codes, k_exps, v_codes, v_exps, ctx_len, *, scale: Optional[float] = None,
+                   max_ctx: Optional[int] = None, out=None, mass=None, lse=None, want_mass: bool = True,
+                   want_lse: bool = True, ws: Optional[Workspace] = None, status=None):
+    """pvlm_verify_attn_q4: ``verify_attn`` of bf16 queries [B][T][Hq][D] over a 4-bit
+    cache, codes [B][Hkv][n_cap][D / 2] and exponents [B][Hkv][n_cap][D / 32]; T = 1 and
+    want_mass=False for a decode step.  Returns (out, mass or None, lse or None)."""
+    return _verify_q4(q, (k_codes, k_exps, v_codes, v_exps), None, ctx_len, scale, max_ctx, out, mass, lse,
+                      want_mass, want_lse, ws, status)
+
+
+def verify_attn_q4_paged(q, k_codes, k_exps, v_codes, v_exps, page_table, ctx_len, *,
+                         scale: Optional[float] = None, max_ctx: Optional[int] = None, out=None, mass=None,
+                         lse=None, want_mass: bool = True, want_lse: bool = True,
+                         ws: Optional[Workspace] = None, status=None):
+    """pvlm_verify_attn_q4_paged: the same over pools [n_pages][Hkv][page][D / 2]
+    through page_table [B][max_pages]; mass is [B][max_pages * page]."""
+    if page_table is None:
+        raise TypeError("page_table must be a torch.Tensor")
+    return _verify_q4(q, (k_codes, k_exps, v_codes, v_exps), page_table, ctx_len, scale, max_ctx, out, mass, lse,
+                      want_mass, want_lse, ws, status)
+
+
+def _gather_q4(cache, page_table, idx, k, tail_begin, tail_len, dst_cap, dtype, dst, status):
+    _need(cache[0], "k_codes")
+    dev = cache[0].device
+    shape = _need_q4(*cache, dev, page_table is not None, stacked=True)
+    for name, t in (("idx", idx), ("k", k), ("tail_begin", tail_begin), ("tail_len", tail_len)):
+        _need(t, name, torch.int32, dev)
+    L = 1 if len(shape) == 4 else shape[0]
+    n0, Hkv, rows, D = shape[-4:]
+    if idx.dim() != 2 or (page_table is None and n0 != idx.shape[0]):
+        raise ValueError("idx must be [B][k_cap]")
+    B = idx.shape[0]
+    if any(t.shape != (B,) for t in (k, tail_begin, tail_len)):
+        raise ValueError("k, tail_begin and tail_len must be [B]")
+    if dtype not in (torch.float4_e2m1fn_x2, torch.uint8, torch.bfloat16, torch.float32):
+        raise ValueError(f"unsupported dtype {dtype}")
+    q4 = dtype is torch.uint8 or dtype is torch.float4_e2m1fn_x2
+    dst_cap = int(dst_cap)
+    want = tuple(shape[:-4]) + (B, Hkv, dst_cap, D)
+    fill = dst is None   # the call zeroes what it does not copy of a new destination
+    if fill and q4:
+        dst = [torch.empty(want[:-1] + (w,), dtype=d, device=dev) for w, d in ((D // 2, dtype), (D // 32, torch.uint8)) * 2]
+    elif fill:
+        dst = [torch.empty(want, dtype=dtype, device=dev) for _ in range(2)]
+    elif q4:
+        if len(dst) != 4 or tuple(_need_q4(*dst, dev, False, stacked=True)) != want:
+            raise ValueError("destination shape mismatch")
+    elif len(dst) != 2 or any(_need(t, "dst", dtype, dev).shape != want for t in dst):
+        raise ValueError("destination shape mismatch")
+    kd, kde, vd, vde = [t.data_ptr() for t in dst] if q4 else (dst[0].data_ptr(), None, dst[1].data_ptr(), None)
+    to = PVLM_E2M1 if q4 else PVLM_BF16 if dtype is torch.bfloat16 else PVLM_F32
+    if page_table is None:
+        name, geom, table = "pvlm_gather_kv_q4", (rows,), ()
+    else:
+        name = "pvlm_gather_kv_q4_paged"
+        geom, table = (rows, _need_table(page_table, dev, B), n0), (page_table.data_ptr(),)
+    st = getattr(lib(), name)(to, L, B, Hkv, D, *geom, *[t.data_ptr() for t in cache], *table, idx.data_ptr(),
+                              k.data_ptr(), idx.shape[1], tail_begin.data_ptr(), tail_len.data_ptr(), dst_cap,
+                              int(fill), kd, kde, vd, vde, _ptr(_status(status)), _stream())
+    _check(st, name)
+    return tuple(dst)
+
+
+def gather_kv_q4(k_codes, k_exps, v_codes, v_exps, idx, k, tail_begin, tail_len, dst_cap: int, *,
+                 dtype=torch.uint8, dst=None, status=None):
+    """pvlm_gather_kv_q4: the draft's compact cache (``gather_kv``) from a 4-bit cache
+    [B][Hkv][n_cap][D / 2] or [L][...].  dtype torch.uint8 (or float4_e2m1fn_x2)
+    returns (k_codes, k_exps, v_codes, v_exps) with dst_cap rows (a multiple of
+    32); torch.bfloat16 or torch.float32 returns (k, v), the values that the rows
+    stand for.  ``dst``: those tensors, to be written in place."""
+    return _gather_q4((k_codes, k_exps, v_codes, v_exps), None, idx, k, tail_begin, tail_len, dst_cap, dtype, dst,
+                      status)
+
+
+def gather_kv_q4_paged(k_codes, k_exps, v_codes, v_exps, page_table, idx, k, tail_begin, tail_len, dst_cap: int, *,
+                       dtype=torch.uint8, dst=None, status=None):
+    """pvlm_gather_kv_q4_paged: the same from pools [n_pages][Hkv][page][D / 2] or
+    [L][...]; one page_table [B][max_pages] serves every layer."""
+    if page_table is None:
+        raise TypeError("page_table must be a torch.Tensor")
+    return _gather_q4((k_codes, k_exps, v_codes, v_exps), page_table, idx, k, tail_begin, tail_len, dst_cap, dtype,
+                      dst, status)

@@ -789,8 +789,7 @@ pvlm_status pvlm_quantize_kv_q4_paged(pvlm_dtype dt, int n_layers, int B, int Hk
  * ctx_len[b] + T are not used, whatever they hold).
  *   ws    >= pvlm_verify_attn_q4_workspace_size() bytes (under every compute-unit
  *         budget).
- * Arguments, flags and errors are those of that call; PVLM_ERR_SHAPE for 5 * B * Hkv
- * blocks of 32 rows up to max_ctx + T of more than 2^31 - 65537 in all, and for B > 65535.
+ * Arguments, flags and errors are those of that call.
  * ---------------------------------------------------------------------- */
 size_t pvlm_verify_attn_q4_workspace_size(int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
                                           int64_t max_ctx);

@@ -15,7 +15,10 @@
 //    read a second time.  Every order of summation is fixed.  No workgroup waits
 //    for another.
 //
-// Launches, all on the caller's stream: partial, combine, and with the mass a third.
+// Launches, all on the caller's stream: partial; combine, unless the shares are whole
+// groups; and the mass.
+#include <type_traits>
+
 #include "q4.h"
 #include "q4_plan.h"
 
@@ -41,15 +44,15 @@ struct Q4Args : QShape {
   unsigned g_magic;  // row / G == row * g_magic >> 20 for row < 640 (2^20 / G + 1; G <= 640)
   int RTT;
   float sl2;         // scale * log2(e)
-  float4* stats;     // [record][tile][16] of a row: log2-domain reference, sum, sum of the rounded, unused
+  float4* stats;     // [record][row tile][16] of a row: log2-domain reference, sum, sum of the rounded, unused
   uint32_t* nan;     // [record] the values hold a NaN that not every row sees
-  float2* rows;      // [B][Hkv][RTT * 16] maximum and inverse sum, for the mass
-  float* opart;      // [record][tile][16][D] sums of P . V relative to that reference
+  float2* rows;      // [B][Hkv][R] maximum and inverse sum, for the mass
+  float* opart;      // [record][row tile][16][D] sums of P . V relative to that reference
   uint16_t* out;
   float* lse;
   float* mass;
   int32_t* status;
-  int MG, GW, chunk;
+  int per_share, MG, GW, chunk, chunks;
 };
 
 // ------------------------------------------------------------ the shares --
@@ -96,8 +99,18 @@ struct Wave {
 
 struct Piece : QPiece {
   // false where the share is empty
-  __device__ __forceinline__ bool first(const QShape& a, const int32_t* ctx_len) {
-    return begin(a, q8_find<true>(a, Wave(ctx_len), blockIdx.x, 0), blockIdx.x);
+  __device__ __forceinline__ bool first(const QShape& a, const int32_t* ctx_len, int share) {
+    return begin(a, q8_find<true>(a, Wave(ctx_len), share, 0), share);
+  }
+  // All of group `group`, where a share is a group.
+  __device__ __forceinline__ void whole(const QShape& a, const int32_t* ctx_len, int group) {
+    b = group / a.Hkv;
+    g = group - b * a.Hkv;
+    rg = before = c0 = 0;
+    align = 1;
+    ctx = __builtin_amdgcn_readfirstlane(clamp_ctx(a, uniform_load(ctx_len, b)));
+    left = per = units_of(a, ctx);
+    set(a);
   }
   // false where the share ends
   __device__ __forceinline__ bool next(const QShape& a, const int32_t* ctx_len) {
@@ -105,20 +118,36 @@ struct Piece : QPiece {
   }
 };
 
-// The page-table entry of token t (0 in a padded cache), and the row index (in
-// rows) of the unit that t opens.  An entry outside the pool sets bad and is
+// Where the rows of one (sequence, KV head) lie: row t of a paged cache in page
+// table[t >> shift], of a padded one behind `first` (its table is any word: the
+// page's number then counts for nothing).  An entry outside the pool sets bad and is
 // clamped into it.
-__device__ __forceinline__ int page_entry(const Q8Cache& c, int b, int t) {
-  return c.table ? uniform_load(c.table, (int64_t)b * c.max_pages + (t >> c.shift)) : 0;
-}
-__device__ __forceinline__ int64_t unit_row(const Q8Cache& c, int Hkv, int b, int g, int t, int page, bool& bad) {
-  if (!c.table) return ((int64_t)b * Hkv + g) * c.n_cap + t;
-  if (page < 0 || page >= c.n_pages) {
-    bad = true;
-    page = page < 0 ? 0 : (int)(c.n_pages - 1);
+struct Rows {
+  const int32_t* table;
+  int64_t first, page_rows;
+  uint32_t n_pages;
+  int shift, mask;
+  __device__ __forceinline__ Rows(const Q4Cache& c, const int32_t* any, int Hkv, int b, int g) {
+    const bool paged = c.table != nullptr;
+    table = paged ? c.table + (int64_t)b * c.max_pages : any;
+    shift = paged ? c.shift : 31;
+    mask = paged ? (1 << c.shift) - 1 : 0x7fffffff;
+    first = paged ? (int64_t)g << c.shift : ((int64_t)b * Hkv + g) * c.n_cap;
+    page_rows = paged ? (int64_t)Hkv << c.shift : 0;
+    n_pages = paged ? (uint32_t)c.n_pages : 0xffffffffu;
   }
-  return (((int64_t)page * Hkv + g) << c.shift) + (t & ((1 << c.shift) - 1));
-}
+  // The page that row t lies in, and the row's number of the cache's.  (Apart, so that a
+  // loop can have the entry before it is wanted.)
+  __device__ __forceinline__ int entry(int t) const { return uniform_load(table, t >> shift); }
+  __device__ __forceinline__ int64_t at(int t, int entry, bool& bad) const {
+    uint32_t page = (uint32_t)entry;
+    if (page >= n_pages) {
+      bad |= n_pages != 0xffffffffu;
+      page = entry < 0 ? 0 : n_pages - 1;
+    }
+    return (int64_t)page * page_rows + first + (t & mask);
+  }
+};
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ int row_t(const Q4Args& a, int row) { return (int)((unsigned)row * a.g_magic >> 20); }
@@ -131,7 +160,6 @@ __device__ __forceinline__ bf16x8 to_bf16(uint32_t w, float unit) {
   const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 3);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-__device__ __forceinline__ float unit_of(uint32_t e) { return __uint_as_float(e << 23); }
 
 // A lane's part of a 16-token tile of K or V: with n = lane & 15 and gq = lane >> 4,
 // D / 4 consecutive values of row n from value (D / 4) gq on, D / 32 words of eight
@@ -139,23 +167,39 @@ __device__ __forceinline__ float unit_of(uint32_t e) { return __uint_as_float(e 
 // memory, and word ks is an operand of the 16x16x32 product over values
 // (D / 4) gq + 8 ks + j: the order of the sum over d is free, so long as the queries
 // have it too.
+// Its exponent is a byte of the word that is loaded (a byte load's result the compiler
+// masks where it arrives, and so waits for it there).
 template <int D>
 struct Codes {
   uint32_t w[D / 32];
   uint32_t e;
 };
 template <int D>
-__device__ __forceinline__ void load_codes(const uint8_t* codes, const uint8_t* exps, int64_t row0, int n, int gq,
+struct LaneOf {  // a lane's place in a tile
+  uint32_t codes, exps, shift;  // (unsigned: an address is then a scalar base and this)
+  __device__ __forceinline__ LaneOf(int n, int gq)
+      : codes(n * (D / 2) + gq * (D / 8)),
+        exps(n * (D / 32) & ~3),
+        shift(8 * ((n * (D / 32) + gq * (D / 32) / 4) & 3)) {}
+  __device__ __forceinline__ uint32_t exponent(uint32_t e) const { return __builtin_amdgcn_ubfe(e, shift, 8); }
+  __device__ __forceinline__ float unit(uint32_t e) const { return __uint_as_float(exponent(e) << 23); }
+};
+// A pointer that the wave's lanes have in common, in scalar registers (left to itself
+// the compiler adds the lane's offset first and keeps 64 bits of it a lane).
+typedef const __attribute__((address_space(1))) uint8_t* Global;
+__device__ __forceinline__ Global scalar(const uint8_t* p) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)u), hi = __builtin_amdgcn_readfirstlane((int)(u >> 32));
+  return (Global)((uint64_t)hi << 32 | lo);
+}
+template <int D>
+__device__ __forceinline__ void load_codes(const uint8_t* codes, const uint8_t* exps, int64_t row0, const LaneOf<D>& at,
                                            Codes<D>& x) {
-  const uint8_t* p = codes + row0 * (D / 2) + (n * (D / 2) + gq * (D / 8));
-  if constexpr (D == 128) {
-    const uintx4 v = *reinterpret_cast<const uintx4*>(p);
-    x.w[0] = v[0], x.w[1] = v[1], x.w[2] = v[2], x.w[3] = v[3];
-  } else {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
-    x.w[0] = v.x, x.w[1] = v.y;
-  }
-  x.e = exps[row0 * (D / 32) + (n * (D / 32) + gq * (D / 32) / 4)];
+  typedef uint32_t words __attribute__((ext_vector_type(D / 32)));
+  const words v = *(const __attribute__((address_space(1))) words*)(scalar(codes + row0 * (D / 2)) + at.codes);
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) x.w[i] = v[i];
+  x.e = *(const __attribute__((address_space(1))) uint32_t*)(scalar(exps + row0 * (D / 32)) + at.exps);
 }
 
 template <int D>
@@ -183,262 +227,338 @@ __device__ __forceinline__ float rows4_maximum(float x) {
 // consecutive values of one token: a wave writes a unit of 32 tokens to LDS as bf16
 // rows of its own and reads them transposed.  Nobody else touches them, and a
 // wave's LDS operations run in order, so nothing waits but for data.
-// Chunk c (16 bytes) of row r lies at chunk c ^ swz(r): a transposed read takes
-// the same two chunks of eight rows at a time, a write one chunk of eight rows.
+// Rows lie 32 bytes more than their length apart, and of every sixteen the last eight
+// 144 bytes further: a transposed read (the same 32 bytes of rows 0-3 and 8-11, or 4-7
+// and 12-15, at a time) and a write (the same 16 bytes of sixteen rows) then fall on
+// distinct banks, and every address is the lane's first and a constant.
 template <int D>
 struct Lay {
-  static constexpr int kUnit = 32 * D * 2;
-  static __device__ __forceinline__ int swz(int r) { return D == 128 ? (r & 7) << 1 : (r >> 1 & 3) << 1; }
+  static constexpr int kRow = 2 * D + 32, kHalf = 16 * kRow + 144, kUnit = 2 * kHalf;
+  static __device__ __forceinline__ uint32_t row(int r) { return r * kRow + (r & 8) * 18; }
 };
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef short s8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s4* lds_s4;
 
+// `put`: LDS address of the lane's first chunk in rows 0 .. 15 of the wave's unit.
 template <int D>
-__device__ __forceinline__ void put_values(uint32_t lds, int tt, const Codes<D>& x, int n, int gq) {
-  const float unit = unit_of(x.e);
-  const uint32_t row = lds + (16 * tt + n) * D * 2;
+__device__ __forceinline__ void put_values(uint32_t put, int tt, const Codes<D>& x, float unit) {
 #pragma unroll
   for (int c = 0; c < D / 32; ++c)
-    *(__attribute__((address_space(3))) bf16x8*)(row + (((gq * (D / 32) + c) ^ Lay<D>::swz(n)) << 4)) = to_bf16(x.w[c], unit);
+    *(__attribute__((address_space(3))) bf16x8*)(put + tt * Lay<D>::kHalf + 16 * c) = to_bf16(x.w[c], unit);
 }
 
-// O += P . V over the unit in LDS; P holds tokens 4 gq + {0..3, 16..19}.
-template <int D, int TPW, int S>
-__device__ __forceinline__ void weigh(uint32_t lds, const bf16x8 (&P)[TPW][S], int u, floatx4 (&O)[TPW][D / 16], int n,
-                                      int gq) {
-  const int row = 4 * gq + n / 4;
-  const uint32_t at = lds + row * D * 2 + 8 * (n & 1);
-  const int sw = Lay<D>::swz(row), c0 = n >> 1 & 1;
+// O += P . V over the unit in LDS; P holds tokens 4 gq + {0..3, 16..19}, `get` is the
+// lane's first address: of sixteen lanes each takes 8 bytes of row 4 gq + n / 4, and
+// receives column n of the four rows.  AHEAD operands are under way while the matrix
+// instructions of earlier ones run (the compiler, left to itself, waits for each alone).
+template <int D, int TPW, int S, int AHEAD>
+__device__ __forceinline__ void weigh(uint32_t get, const bf16x8 (&P)[TPW][S], int u, floatx4 (&O)[TPW][D / 16]) {
+  constexpr int N = D / 16;
+  s4 lo[AHEAD], hi[AHEAD];
+  auto read = [&](int j) {
+    lo[j % AHEAD] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(get + 32 * j));
+    hi[j % AHEAD] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(get + 32 * j + Lay<D>::kHalf));
+  };
 #pragma unroll
-  for (int jd = 0; jd < D / 16; ++jd) {
-    const uint32_t p = at + (((2 * jd + c0) ^ sw) << 4);
-    const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)p);
-    const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(p + 16 * D * 2));
-    const bf16x8 v = __builtin_bit_cast(bf16x8, (s8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  for (int j = 0; j < AHEAD - 1; ++j) read(j);
 #pragma unroll
-    for (int x = 0; x < TPW; ++x) O[x][jd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][u], v, O[x][jd], 0, 0, 0);
+  for (int j = 0; j < N; ++j) {
+    if (j + AHEAD - 1 < N) read(j + AHEAD - 1);
+    __builtin_amdgcn_sched_barrier(0);
+    const s8 both = __builtin_shufflevector(lo[j % AHEAD], hi[j % AHEAD], 0, 1, 2, 3, 4, 5, 6, 7);
+    const bf16x8 v = __builtin_bit_cast(bf16x8, both);
+#pragma unroll
+    for (int x = 0; x < TPW; ++x) O[x][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][u], v, O[x][j], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// ------------------------------------------------------------- a result --
+// C columns of a row of the result, from the sums relative to its reference m: positions
+// C part .. of a stored row, of which position (D / 16) n + jd is column 16 jd + n.
+// `look`: the values hold a NaN that not every row sees.  Those past the context that
+// this row sees counted as 0 and are looked for here.
+template <int D, int C>
+__device__ __forceinline__ void put_row(const Q4Args& a, int b, int g, int row, int ctx, const Rows& rows, int part,
+                                        const float (&o)[C], float m, float z, float zt, bool look) {
+  constexpr int DPL = D / 16;
+  const int t = row_t(a, row), head = g * a.G + row - t * a.G;
+  const float inv = 1.f / zt;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int pos = C * part + c, col = 16 * (pos % DPL) + pos / DPL;
+    float y = o[c] * inv;
+    if (look) {
+      for (int j = ctx + 1; j <= ctx + t; ++j) {
+        bool flagged_before = false;  // by the loads of the row
+        const int64_t r = rows.at(j, rows.table[j >> rows.shift], flagged_before);
+        if (a.c.ve[r * (D / 32) + col / 32] == 255) y = __uint_as_float(0x7fc00000u);
+      }
+    }
+    a.out[(((size_t)b * a.T + t) * a.Hq + head) * D + col] = f32_to_bf16(y);
+  }
+  if (part == 0) {
+    if (a.lse) a.lse[((size_t)b * a.Hq + head) * a.T + t] = (m + __log2f(z)) * kLn2;
+    if (a.mass) a.rows[((size_t)b * a.Hkv + g) * a.R + row] = make_float2(m, 1.f / z);
   }
 }
 
 // -------------------------------------------------------- partial kernel --
-template <int D, int RT>
+// A workgroup's eight waves hold the same set of row tiles, TPW of them, and take its
+// tokens in turn, 32 NB at a time.
+template <int D, int TPW>
 struct PartShape {
-  static constexpr int TPW = q4_waves(RT).tpw, RW = q4_waves(RT).rw, TW = q4_waves(RT).tw;
-  static constexpr int kWaves = RW * TW, kThreads = kWaves * 64;
-  static constexpr int NB = TPW == 3 ? 1 : 2;  // units of 32 tokens that a wave takes at a time
-  static constexpr int kLds = kWaves * Lay<D>::kUnit;
+  static constexpr int NB = TPW >= 2 ? 1 : 2;
+  static constexpr int kWaveLds = NB * Lay<D>::kUnit, kLds = kQ4Waves * kWaveLds, AHEAD = 3;
 };
 
-template <int D, int RT>
-__global__ void __launch_bounds__((PartShape<D, RT>::kThreads)) __attribute__((amdgpu_waves_per_eu(2, 2)))
-q4_part_kernel(Q4Args a) {
-  typedef PartShape<D, RT> S_;
-  constexpr int TPW = S_::TPW, TW = S_::TW, NB = S_::NB, DPL = D / 16, BT = 32 * NB;
+// SINGLE: every group is one share, and the workgroup writes the results.  (A kernel of
+// its own: that path's registers cost the other one 7 %.)
+template <int D, int TPW, bool SINGLE>
+__global__ void __launch_bounds__(kQ4Waves * 64)
+__attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(Q4Args a) {
+  constexpr int NB = PartShape<D, TPW>::NB, DPL = D / 16, BT = 32 * NB, TW = kQ4Waves;
   extern __shared__ __align__(1024) char s_values[];  // [wave][32][D] bf16; then a tile's O, [wave][16][D] fp32
-  __shared__ float s_ref[S_::kWaves][16], s_z[S_::kWaves][16], s_zt[S_::kWaves][16];
-  __shared__ uint32_t s_nan[S_::kWaves];
+  __shared__ float s_ref[TW][16], s_z[TW][16], s_zt[TW][16];
+  __shared__ uint32_t s_nan[TW];
 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (blockIdx.x == 0 && w == 0)
     for (int b = threadIdx.x; b < a.B; b += 64)
       if (a.ctx_len[b] < 0 || a.ctx_len[b] > a.max_ctx) dev_flag(a.status, PVLM_DEV_RANGE);
-  Piece p;
-  if (!p.first(a, a.ctx_len)) return;
+  // The sets of row tiles of a share read the same tokens at about the same time:
+  // they are neighbours on one die (workgroup i runs on die i mod 8), whose L2 has
+  // what the first of them read.
+  const int wgs = gridDim.x, id = blockIdx.x, whole8 = wgs & ~7;
+  const int place = id < whole8 ? (id & 7) * (whole8 >> 3) + (id >> 3) : id;
+  const int share = place / a.per_share;
   const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-  const int tw = w % TW, rw = w / TW;
-  const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(s_values)) + w * Lay<D>::kUnit;
+  const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(s_values)) + w * PartShape<D, TPW>::kWaveLds;
+
+  const LaneOf<D> place_of(n, gq);
+  const uint32_t put = lds + Lay<D>::row(n) + gq * (D / 2);
+  const uint32_t get = lds + Lay<D>::row(4 * gq + n / 4) + 8 * (n & 3);
   bool bad_page = false;
-  do {
-    const int tile0 = p.rg * RT + rw * TPW;  // of the KV head's
-    Query<D> q[TPW];
-    int lim[TPW];
-    float ref[TPW], z[TPW];
-    floatx4 O[TPW][DPL], zt[TPW];
-#pragma unroll
-    for (int x = 0; x < TPW; ++x) {
-      const int row = (tile0 + x) * 16 + n;
-      load_query<D>(a, p.b, p.g, row, gq, q[x]);
-      lim[x] = rw * TPW + x < RT && row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
-      ref[x] = kNegInf;
-      z[x] = 0.f;
-      zt[x] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int jd = 0; jd < DPL; ++jd) O[x][jd] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
-    uint32_t nan = 0;
-    Codes<D> kc[NB][2], vc[NB][2];
-    auto load = [&](int tb) {
-#pragma unroll
-      for (int u = 0; u < NB; ++u) {
-        const int t = min(tb + 32 * u, (p.c1 - 1) & ~31);
-        const int64_t r = unit_row(a.c, a.Hkv, p.b, p.g, t, page_entry(a.c, p.b, t), bad_page);
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) load_codes<D>(a.c.kc, a.c.ke, r + 16 * tt, n, gq, kc[u][tt]);
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) load_codes<D>(a.c.vc, a.c.ve, r + 16 * tt, n, gq, vc[u][tt]);
-      }
-    };
-    auto block = [&](int tb, bool tail) {
-      floatx4 S[TPW][2 * NB];
-#pragma unroll
-      for (int j = 0; j < 2 * NB; ++j) {
-        const float unit = unit_of(kc[j / 2][j % 2].e);
-#pragma unroll
-        for (int x = 0; x < TPW; ++x) S[x][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) {
-          const bf16x8 k = to_bf16(kc[j / 2][j % 2].w[ks], unit);
-#pragma unroll
-          for (int x = 0; x < TPW; ++x) S[x][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[x].s[ks], S[x][j], 0, 0, 0);
-        }
-      }
-      if (tail) {
-#pragma unroll
-        for (int x = 0; x < TPW; ++x)
-#pragma unroll
-          for (int j = 0; j < 8 * NB; ++j)
-            if (tb + 16 * (j / 4) + 4 * gq + j % 4 > lim[x]) S[x][j / 4][j % 4] = kNegInf;
-#pragma unroll
-        for (int u = 0; u < NB; ++u)
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt) {
-            // rows past the piece become zeros (their probabilities are 0, and 0 times what
-            // an unwritten row holds may be NaN), and so do NaN of rows that not every query
-            // row sees: the record's flag has the combine kernel look for them
-            const int t = tb + 32 * u + 16 * tt + n;
-            const bool past = t >= p.c1, hidden = t > p.ctx && vc[u][tt].e == 255;
-            if (hidden && !past) nan = 1;
-            if (past || hidden) {
-              vc[u][tt].e = 127;
-#pragma unroll
-              for (int c = 0; c < D / 32; ++c) vc[u][tt].w[c] = 0;
-            }
-          }
-      }
-      bf16x8 P[TPW][NB];
-#pragma unroll
+  for (int rg = place - share * a.per_share; rg * TPW < a.RTT; rg += a.per_share) {
+    Piece p;
+    if constexpr (SINGLE) p.whole(a, a.ctx_len, share);
+    else if (!p.first(a, a.ctx_len, share)) break;
+    do {
+      const int tile0 = rg * TPW;  // of the KV head's
+      const Rows rows(a.c, a.ctx_len, a.Hkv, p.b, p.g);
+      Query<D> q[TPW];
+      int lim[TPW];
+      float ref[TPW], z[TPW];
+      floatx4 O[TPW][DPL], zt[TPW];
+  #pragma unroll
       for (int x = 0; x < TPW; ++x) {
-        float m = kNegInf;
-#pragma unroll
-        for (int j = 0; j < 8 * NB; ++j) m = fmaxf(m, S[x][j / 4][j % 4]);
-        m *= a.sl2;
-        if (__any(m > ref[x] + kRefSlack)) {  // the first block, and seldom after it
-          const float nm = fmaxf(ref[x], rows4_maximum(m));
-          const float al = ref[x] == kNegInf ? 0.f : fast_exp2(ref[x] - nm);
-          z[x] *= al;
-          ref[x] = nm;
-          floatx4 f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) f[i] = __shfl(al, 4 * gq + i, 64);
-          zt[x] = zt[x] * f;
-#pragma unroll
-          for (int jd = 0; jd < DPL; ++jd) O[x][jd] = O[x][jd] * f;
-        }
-        const float r = ref[x] == kNegInf ? 0.f : ref[x];  // no visible token yet: P = 0
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8 * NB; ++j) {
-          const float e = fast_exp2(fmaf(S[x][j / 4][j % 4], a.sl2, -r));
-          sum += e;
-          P[x][j / 8][j % 8] = static_cast<__bf16>(e);
-        }
-        z[x] += sum;
+        const int row = (tile0 + x) * 16 + n;
+        load_query<D>(a, p.b, p.g, row, gq, q[x]);
+        lim[x] = row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
+        ref[x] = kNegInf;
+        z[x] = 0.f;
+        zt[x] = floatx4{0.f, 0.f, 0.f, 0.f};
+  #pragma unroll
+        for (int jd = 0; jd < DPL; ++jd) O[x][jd] = floatx4{0.f, 0.f, 0.f, 0.f};
       }
-      bf16x8 ones;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) ones[j] = static_cast<__bf16>(1.f);
-#pragma unroll
-      for (int u = 0; u < NB; ++u) {
-#pragma unroll
-        for (int x = 0; x < TPW; ++x) zt[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][u], ones, zt[x], 0, 0, 0);
+      uint32_t nan = 0;
+      Codes<D> kc[NB][2], vc[NB][2];
+      // The next block's units (past the piece, its last unit once more) and their pages.
+      int page[NB];
+      int64_t row[NB];
+      auto unit = [&](int tb, int u) { return min(tb + 32 * u, (p.c1 - 1) & ~31); };
+      auto find = [&](int tb) {
+  #pragma unroll
+        for (int u = 0; u < NB; ++u) page[u] = rows.entry(unit(tb, u));
+      };
+      auto load_k = [&](int tb) {
+  #pragma unroll
+        for (int u = 0; u < NB; ++u) {
+          row[u] = rows.at(unit(tb, u), page[u], bad_page);
+  #pragma unroll
+          for (int tt = 0; tt < 2; ++tt) load_codes<D>(a.c.kc, a.c.ke, row[u] + 16 * tt, place_of, kc[u][tt]);
+        }
+        find(tb + BT * TW);
+      };
+      auto load_v = [&]() {
+  #pragma unroll
+        for (int u = 0; u < NB; ++u)
+  #pragma unroll
+          for (int tt = 0; tt < 2; ++tt) load_codes<D>(a.c.vc, a.c.ve, row[u] + 16 * tt, place_of, vc[u][tt]);
+      };
+      // A block of BT tokens; TAIL: some row does not see all of them.
+      auto block = [&](int tb, auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        if constexpr (TAIL) {
+  #pragma unroll
+          for (int u = 0; u < NB; ++u)
+  #pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+              // rows past the piece become zeros (their probabilities are 0, and 0 times what
+              // an unwritten row holds may be NaN), and so do NaN of rows that not every query
+              // row sees: the record's flag has the combine kernel look for them
+              const int t = tb + 32 * u + 16 * tt + n;
+              const bool past = t >= p.c1, hidden = t > p.ctx && place_of.exponent(vc[u][tt].e) == 255;
+              if (hidden && !past) nan = 1;
+              if (past || hidden) {
+                vc[u][tt].e = 0;
+  #pragma unroll
+                for (int c = 0; c < D / 32; ++c) vc[u][tt].w[c] = 0;
+              }
+            }
+        }
+        // (the values' conversion runs beside the matrix instructions of the scores)
         asm volatile("" ::: "memory");  // (the wave's LDS operations keep their order)
-        put_values<D>(lds, 0, vc[u][0], n, gq);
-        put_values<D>(lds, 1, vc[u][1], n, gq);
+  #pragma unroll
+        for (int u = 0; u < NB; ++u)
+  #pragma unroll
+          for (int tt = 0; tt < 2; ++tt) put_values<D>(put + u * Lay<D>::kUnit, tt, vc[u][tt], place_of.unit(vc[u][tt].e));
+        floatx4 S[TPW][2 * NB];
+  #pragma unroll
+        for (int j = 0; j < 2 * NB; ++j) {
+          const float unit = place_of.unit(kc[j / 2][j % 2].e);
+  #pragma unroll
+          for (int x = 0; x < TPW; ++x) S[x][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  #pragma unroll
+          for (int ks = 0; ks < D / 32; ++ks) {
+            const bf16x8 k = to_bf16(kc[j / 2][j % 2].w[ks], unit);
+  #pragma unroll
+            for (int x = 0; x < TPW; ++x) S[x][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[x].s[ks], S[x][j], 0, 0, 0);
+          }
+        }
         asm volatile("" ::: "memory");
-        weigh<D, TPW, NB>(lds, P, u, O, n, gq);
+        load_k(tb + BT * TW);
+        load_v();
+        if constexpr (TAIL) {
+  #pragma unroll
+          for (int x = 0; x < TPW; ++x)
+  #pragma unroll
+            for (int j = 0; j < 8 * NB; ++j)
+              if (tb + 16 * (j / 4) + 4 * gq + j % 4 > lim[x]) S[x][j / 4][j % 4] = kNegInf;
+        }
+        bf16x8 P[TPW][NB];
+  #pragma unroll
+        for (int x = 0; x < TPW; ++x) {
+          float m = kNegInf;
+  #pragma unroll
+          for (int j = 0; j < 8 * NB; ++j) m = __builtin_elementwise_maximum(m, S[x][j / 4][j % 4]);
+          m *= a.sl2;
+          if (__any(m > ref[x] + kRefSlack)) {  // the first block, and seldom after it
+            const float nm = fmaxf(ref[x], rows4_maximum(m));
+            const float al = ref[x] == kNegInf ? 0.f : fast_exp2(ref[x] - nm);
+            z[x] *= al;
+            ref[x] = nm;
+            floatx4 f;
+  #pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = __shfl(al, 4 * gq + i, 64);
+            zt[x] = zt[x] * f;
+  #pragma unroll
+            for (int jd = 0; jd < DPL; ++jd) O[x][jd] = O[x][jd] * f;
+          }
+          const float r = ref[x] == kNegInf ? 0.f : ref[x];  // no visible token yet: P = 0
+          float sum = 0.f;
+  #pragma unroll
+          for (int j = 0; j < 8 * NB; ++j) {
+            const float e = fast_exp2(fmaf(S[x][j / 4][j % 4], a.sl2, -r));
+            sum += e;
+            P[x][j / 8][j % 8] = static_cast<__bf16>(e);
+          }
+          z[x] += sum;
+        }
+        bf16x8 ones;
+  #pragma unroll
+        for (int j = 0; j < 8; ++j) ones[j] = static_cast<__bf16>(1.f);
+  #pragma unroll
+        for (int u = 0; u < NB; ++u) {
+          weigh<D, TPW, NB, PartShape<D, TPW>::AHEAD>(get + u * Lay<D>::kUnit, P, u, O);
+  #pragma unroll
+          for (int x = 0; x < TPW; ++x) zt[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][u], ones, zt[x], 0, 0, 0);
+        }
         asm volatile("" ::: "memory");
-      }
-    };
-    const int whole = min(p.c1 - 1, p.ctx);  // the last token that every row sees
-    for (int tb = p.c0 + BT * tw; tb < p.c1; tb += BT * TW) {
-      load(tb);
-      block(tb, __builtin_amdgcn_readfirstlane(tb + BT - 1 - whole) > 0);
-    }
-    // The token waves' results joined: a tile at a time, through LDS (position
-    // DPL n + jd of a row holds column 16 jd + n).
-    const int rec = p.group(a) + blockIdx.x;
-    const bool any = __any(nan);
-    if (lane == 0) s_nan[w] = any;
-#pragma unroll
-    for (int x = 0; x < TPW; ++x) {
-      __syncthreads();
-      const float zz = rows4_sum(z[x]);
-      if (gq == 0) s_ref[w][n] = ref[x], s_z[w][n] = zz;
-      if (n == 0)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s_zt[w][4 * gq + i] = zt[x][i];
-      float* mine = reinterpret_cast<float*>(s_values) + w * 16 * D;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int h = 0; h < DPL / 4; ++h)
-          *reinterpret_cast<float4*>(mine + (4 * gq + i) * D + DPL * n + 4 * h) =
-              make_float4(O[x][4 * h][i], O[x][4 * h + 1][i], O[x][4 * h + 2][i], O[x][4 * h + 3][i]);
-      __syncthreads();
-      const int tile = rw * TPW + x;
-      if (tile < RT) {
-        for (int i = tw * 64 + lane; i < 16 * D / 4; i += TW * 64) {
-          const int r = i / (D / 4), c = i % (D / 4);
-          if ((p.rg * RT + tile) * 16 + r >= a.R) continue;
+      };
+      int tb = p.c0 + BT * w;
+      find(tb);
+      load_k(tb);
+      load_v();
+      // (two loops: in one, the compiler has every block go through the tail's selections)
+      for (; tb + BT - 1 <= min(p.c1 - 1, p.ctx); tb += BT * TW) block(tb, std::false_type{});
+      for (; tb < p.c1; tb += BT * TW) block(tb, std::true_type{});
+      // The token waves' results joined: a tile at a time, through LDS (position
+      // DPL n + jd of a row holds column 16 jd + n).
+      const int rec = p.group(a) + share;
+      const bool any = __any(nan);
+      if (lane == 0) s_nan[w] = any;
+  #pragma unroll
+      for (int x = 0; x < TPW; ++x) {
+        __syncthreads();
+        const float zz = rows4_sum(z[x]);
+        if (gq == 0) s_ref[w][n] = ref[x], s_z[w][n] = zz;
+        if (n == 0)
+  #pragma unroll
+          for (int i = 0; i < 4; ++i) s_zt[w][4 * gq + i] = zt[x][i];
+        float* mine = reinterpret_cast<float*>(s_values) + w * (PartShape<D, TPW>::kWaveLds / 4);
+  #pragma unroll
+        for (int i = 0; i < 4; ++i)
+  #pragma unroll
+          for (int h = 0; h < DPL / 4; ++h)
+            *reinterpret_cast<float4*>(mine + (4 * gq + i) * D + DPL * n + 4 * h) =
+                make_float4(O[x][4 * h][i], O[x][4 * h + 1][i], O[x][4 * h + 2][i], O[x][4 * h + 3][i]);
+        __syncthreads();
+        for (int i = threadIdx.x; i < 16 * D / 4; i += TW * 64) {
+          const int r = i / (D / 4), c = i % (D / 4), row = (tile0 + x) * 16 + r;
+          if (row >= a.R) continue;
           float M = kNegInf;
-#pragma unroll
-          for (int k = 0; k < TW; ++k) M = fmaxf(M, s_ref[rw * TW + k][r]);
+  #pragma unroll
+          for (int k = 0; k < TW; ++k) M = fmaxf(M, s_ref[k][r]);
           const float base = M == kNegInf ? 0.f : M;
           float Z = 0.f, Zt = 0.f;
           floatx4 o{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
+  #pragma unroll
           for (int k = 0; k < TW; ++k) {
-            const int v = rw * TW + k;
-            if (s_z[v][r] == 0.f) continue;  // nothing that the row sees
-            const float f = fast_exp2(s_ref[v][r] - base);
-            Z += s_z[v][r] * f;
-            Zt += s_zt[v][r] * f;
-            const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(s_values) + (v * 16 + r) * D + 4 * c);
+            if (s_z[k][r] == 0.f) continue;  // nothing that the row sees
+            const float f = fast_exp2(s_ref[k][r] - base);
+            Z += s_z[k][r] * f;
+            Zt += s_zt[k][r] * f;
+            const float* theirs = reinterpret_cast<const float*>(s_values) + k * (PartShape<D, TPW>::kWaveLds / 4);
+            const float4 y = *reinterpret_cast<const float4*>(theirs + r * D + 4 * c);
             o[0] = fmaf(y.x, f, o[0]), o[1] = fmaf(y.y, f, o[1]), o[2] = fmaf(y.z, f, o[2]), o[3] = fmaf(y.w, f, o[3]);
           }
-          const size_t at = ((size_t)rec * RT + tile) * 16 + r;
-          *reinterpret_cast<float4*>(a.opart + at * D + 4 * c) = make_float4(o[0], o[1], o[2], o[3]);
-          if (c == 0) a.stats[at] = make_float4(M, Z, Zt, 0.f);
+          const size_t at = (size_t)rec * a.RTT * 16 + row;
+          if constexpr (SINGLE) {
+            uint32_t any_wave = 0;
+  #pragma unroll
+            for (int k = 0; k < TW; ++k) any_wave |= s_nan[k];
+            float y[4] = {o[0], o[1], o[2], o[3]};
+            put_row<D, 4>(a, p.b, p.g, row, p.ctx, rows, c, y, M, Z, Zt, any_wave != 0);
+          } else {
+            if (c == 0) a.stats[at] = make_float4(M, Z, Zt, 0.f);
+            *reinterpret_cast<float4*>(a.opart + at * D + 4 * c) = make_float4(o[0], o[1], o[2], o[3]);
+          }
         }
       }
-    }
-    if (threadIdx.x == 0) {
-      uint32_t any_wave = 0;
-      for (int k = 0; k < S_::kWaves; ++k) any_wave |= s_nan[k];
-      a.nan[rec] = any_wave;
-    }
-    __syncthreads();
-  } while (p.next(a, a.ctx_len));
+      if (!SINGLE && threadIdx.x == 0 && rg == 0) {
+        uint32_t any_wave = 0;
+        for (int k = 0; k < TW; ++k) any_wave |= s_nan[k];
+        a.nan[rec] = any_wave;
+      }
+      __syncthreads();
+    } while (!SINGLE && p.next(a, a.ctx_len));
+  }
   if (bad_page && lane == 0) dev_flag(a.status, PVLM_DEV_RANGE);
 }
 
-// -------------------------------------------------------- combine kernel --
+// --------------------------------------------------------------- combine --
 // A wave joins a row's records: their references and sums a lane each, then the
 // partial results weighted by exp2(record's reference - row maximum).
-constexpr int kCombineWaves = 4;
-
 template <int D>
-__global__ void __launch_bounds__(kCombineWaves * 64) q4_combine_kernel(Q4Args a, int RT) {
-  constexpr int C = D / 64, DPL = D / 16, kU = 8;
+__device__ __forceinline__ void combine_row(const Q4Args& a, int id) {
+  constexpr int C = D / 64, kU = 8;
   const int lane = threadIdx.x & 63;
-  const int id = __builtin_amdgcn_readfirstlane(blockIdx.x * kCombineWaves + (threadIdx.x >> 6));
-  if (id >= a.B * a.Hkv * a.R) return;
   const int bg = id / a.R, row = id - bg * a.R, b = bg / a.Hkv, g = bg - b * a.Hkv;
   const Shares s = q8_find<false>(a, Wave(a.ctx_len), 0, b);
-  const int rg = row / (16 * RT), tile = row / 16 - rg * RT;
-  const Holders h = holders(a, s.per, s.align, s.before, b, g * a.RG + rg, s.ctx);
-  const size_t at = ((size_t)h.rec * RT + tile) * 16 + row % 16, step = (size_t)RT * 16;
+  const Holders h = holders(a, s.per, s.align, s.before, b, g, s.ctx);
+  const size_t step = (size_t)a.RTT * 16, at = h.rec * step + row;
   float m = kNegInf, z = 0.f, zt = 0.f, o[C];
   bool nan = false;
 #pragma unroll
@@ -474,40 +594,28 @@ __global__ void __launch_bounds__(kCombineWaves * 64) q4_combine_kernel(Q4Args a
           for (int c = 0; c < C; ++c) o[c] = fmaf(v[k][c], wgt[k], o[c]);
     }
   }
-  const int t = row_t(a, row), head = g * a.G + row - t * a.G;
-  const float inv = 1.f / zt;
-  const bool look = __any(nan);
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int pos = C * lane + c, col = 16 * (pos % DPL) + pos / DPL;
-    float y = o[c] * inv;
-    if (look)  // the values past the context that the row sees, whose NaN counted as 0
-      for (int j = s.ctx + 1; j <= s.ctx + t; ++j) {
-        bool flagged_before;  // by the partial kernel
-        const int64_t vr = unit_row(a.c, a.Hkv, b, g, j & ~31, page_entry(a.c, b, j), flagged_before) + (j & 31);
-        if (a.c.ve[vr * (D / 32) + col / 32] == 255) y = __uint_as_float(0x7fc00000u);
-      }
-    a.out[(((size_t)b * a.T + t) * a.Hq + head) * D + col] = f32_to_bf16(y);
-  }
-  if (lane == 0) {
-    if (a.lse) a.lse[((size_t)b * a.Hq + head) * a.T + t] = (m + __log2f(z)) * kLn2;
-    if (a.mass) a.rows[(size_t)bg * a.RTT * 16 + row] = make_float2(m, 1.f / z);
-  }
+  const Rows rows(a.c, a.ctx_len, a.Hkv, b, g);
+  put_row<D, C>(a, b, g, row, s.ctx, rows, lane, o, m, z, zt, __any(nan));
 }
 
-// ----------------------------------------------------------- mass kernel --
-// A workgroup takes a run of a sequence's tokens and every query row: its waves
-// hold the queries of a set of row tiles each (GW sets at a time), with the rows on
-// the M side, so that a lane's scores of a token sum up in the lane.  A row's maximum
-// and inverse sum are kept apart: a probability's exponent is rounded at its
-// distance from the maximum, which is nothing where the mass is.
+constexpr int kCombineWaves = 4;
+template <int D>
+__global__ void __launch_bounds__(kCombineWaves * 64) q4_combine_kernel(Q4Args a) {
+  const int id = __builtin_amdgcn_readfirstlane(blockIdx.x * kCombineWaves + (threadIdx.x >> 6));
+  if (id < a.B * a.Hkv * a.R) combine_row<D>(a, id);
+}
+
+// ----------------------------------------------------------------- mass --
+// A run of a sequence's tokens and every query row: the waves hold the queries of a set
+// of row tiles each (GW sets at a time), with the rows on the M side, so that a lane's
+// scores of a token sum up in the lane.  A row's maximum and inverse sum are kept
+// apart: a probability's exponent is rounded at its distance from the maximum, which
+// is nothing where the mass is.
 template <int D, int MT>
-__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) q4_mass_kernel(Q4Args a) {
-  __shared__ float s_mass[8][512];
-  const int b = blockIdx.y;
-  const int64_t t0 = (int64_t)blockIdx.x * a.chunk;
-  const int ctx = clamp_ctx(a, __builtin_amdgcn_readfirstlane(uniform_load(a.ctx_len, b)));
-  const int N = ctx + a.T;
+__device__ __forceinline__ void mass_run(const Q4Args& a, int64_t item, float (*s_mass)[kQ4MassRun]) {
+  const int b = (int)(item / a.chunks);
+  const int64_t t0 = (item - (int64_t)b * a.chunks) * a.chunk;
+  const int ctx = __builtin_amdgcn_readfirstlane(clamp_ctx(a, uniform_load(a.ctx_len, b))), N = ctx + a.T;
   float* mass = a.mass + (size_t)b * a.c.n_cap;
   const int64_t t_end = min(t0 + a.chunk, a.c.n_cap);
   if (t0 >= N) {
@@ -517,10 +625,21 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
   const int gw = w % a.GW, tw = w / a.GW, TW = 8 / a.GW;
+  const LaneOf<D> place_of(n, gq);
   const int c0 = (int)t0, c1 = min((int)t_end, N);
   bool bad_page = false;
   for (int set = gw; set < a.Hkv * a.MG; set += a.GW) {
     const int g = set / a.MG, tile0 = (set - g * a.MG) * MT;
+    const Rows rows(a.c, a.ctx_len, a.Hkv, b, g);
+    // (a tile is loaded one ahead, its page two; past the run, the last one again)
+    auto tile = [&](int t) { return min(t, (c1 - 1) & ~15); };
+    Codes<D> kc;
+    int page = rows.entry(tile(c0 + 16 * tw));
+    auto load = [&](int t) {
+      load_codes<D>(a.c.kc, a.c.ke, rows.at(tile(t), page, bad_page), place_of, kc);
+      page = rows.entry(tile(t + 16 * TW));
+    };
+    load(c0 + 16 * tw);
     Query<D> q[MT];
     float top[MT][4], inv[MT][4];
 #pragma unroll
@@ -529,17 +648,13 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int row = (tile0 + x) * 16 + 4 * gq + i;
-        const float2 s = a.rows[((size_t)b * a.Hkv + g) * a.RTT * 16 + min(row, a.R - 1)];
-        top[x][i] = row < a.R ? s.x : __builtin_huge_valf();
-        inv[x][i] = row < a.R ? s.y : 0.f;
+        const float2 r = a.rows[((size_t)b * a.Hkv + g) * a.R + min(row, a.R - 1)];
+        top[x][i] = row < a.R ? r.x : __builtin_huge_valf();
+        inv[x][i] = row < a.R ? r.y : 0.f;
       }
     }
     for (int t = c0 + 16 * tw; t < c1; t += 16 * TW) {
-      const int unit = t & ~31;
-      const int64_t r = unit_row(a.c, a.Hkv, b, g, unit, page_entry(a.c, b, unit), bad_page) + (t - unit);
-      Codes<D> kc;
-      load_codes<D>(a.c.kc, a.c.ke, r, n, gq, kc);
-      const float u = unit_of(kc.e);
+      const float u = place_of.unit(kc.e);
       floatx4 S[MT];
 #pragma unroll
       for (int x = 0; x < MT; ++x) S[x] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -549,6 +664,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
         for (int x = 0; x < MT; ++x) S[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[x].s[ks], k, S[x], 0, 0, 0);
       }
+      load(t + 16 * TW);
       float sum = 0.f;
       if (__builtin_amdgcn_readfirstlane(t + 15 - ctx) > 0) {
 #pragma unroll
@@ -578,32 +694,27 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
       for (int k = 0; k < a.GW; ++k) sum += s_mass[k][i];
     mass[t0 + i] = sum;
   }
+  __syncthreads();
   if (bad_page && lane == 0) dev_flag(a.status, PVLM_DEV_RANGE);
+}
+
+// (Registers for four waves a SIMD with up to three row tiles a wave, two with more.)
+template <int D, int MT>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT <= 3 ? 4 : 2, MT <= 3 ? 4 : 2)))
+q4_mass_kernel(Q4Args a) {
+  __shared__ float s_mass[8][kQ4MassRun];
+  for (int64_t item = blockIdx.x; item < (int64_t)a.chunks * a.B; item += gridDim.x) mass_run<D, MT>(a, item, s_mass);
 }
 
 // ------------------------------------------------------------------ host --
 typedef void (*Q4Kernel)(Q4Args);
-struct PartKernel {
-  Q4Kernel fn;
-  int threads, lds;
-};
-template <int D, int RT>
-PartKernel part() {
-  return {q4_part_kernel<D, RT>, PartShape<D, RT>::kThreads, PartShape<D, RT>::kLds};
+template <int D, bool SINGLE>
+Q4Kernel pick_part(int RT) {
+  return RT == 1 ? q4_part_kernel<D, 1, SINGLE> : RT == 2 ? q4_part_kernel<D, 2, SINGLE> : q4_part_kernel<D, 3, SINGLE>;
 }
 template <int D>
-PartKernel pick_part(int RT) {
-  switch (RT) {
-    case 1: return part<D, 1>();
-    case 2: return part<D, 2>();
-    case 3: return part<D, 3>();
-    case 4: return part<D, 4>();
-    case 5: return part<D, 5>();
-    case 6: return part<D, 6>();
-    case 7: return part<D, 7>();
-    case 8: return part<D, 8>();
-    default: return part<D, 9>();
-  }
+int part_lds(int RT) {
+  return RT == 1 ? PartShape<D, 1>::kLds : RT == 2 ? PartShape<D, 2>::kLds : PartShape<D, 3>::kLds;
 }
 template <int D>
 Q4Kernel pick_mass(int MT) {
@@ -646,10 +757,11 @@ pvlm_status verify_q4_run(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D, i
   a.R = p.R;
   a.g_magic = (1u << 20) / (unsigned)p.G + 1u;
   a.RTT = p.RTT;
-  a.RG = p.RG;
-  a.HR = Hkv * p.RG;
+  a.RG = 1;
+  a.HR = Hkv;
   a.max_ctx = (int)max_ctx;
-  a.wgs = p.wgs;
+  a.wgs = p.shares;
+  a.per_share = p.per_share;
   a.sl2 = (float)((double)scale * kLog2e);
   a.stats = reinterpret_cast<float4*>(wsb + p.off_stats);
   a.nan = reinterpret_cast<uint32_t*>(wsb + p.off_nan);
@@ -662,17 +774,24 @@ pvlm_status verify_q4_run(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D, i
   a.MG = p.MG;
   a.GW = p.GW;
   a.chunk = p.chunk;
-  const PartKernel k = D == 128 ? pick_part<128>(p.RT) : pick_part<64>(p.RT);
-  PVLM_HIP(allow_dynamic_lds(reinterpret_cast<const void*>(k.fn), k.lds));
-  hipLaunchKernelGGL(k.fn, dim3(p.wgs), dim3(k.threads), k.lds, stream, a);
+  a.chunks = (int)((c.n_cap + p.chunk - 1) / p.chunk);
+  const Q4Kernel part = p.single ? (D == 128 ? pick_part<128, true>(p.RT) : pick_part<64, true>(p.RT))
+                                 : (D == 128 ? pick_part<128, false>(p.RT) : pick_part<64, false>(p.RT));
+  const int lds = D == 128 ? part_lds<128>(p.RT) : part_lds<64>(p.RT);
+  PVLM_HIP(allow_dynamic_lds(reinterpret_cast<const void*>(part), lds));
+  hipLaunchKernelGGL(part, dim3(p.shares * p.per_share), dim3(kQ4Waves * 64), lds, stream, a);
   PVLM_LAUNCHED();
-  const int rows = B * Hkv * p.R;
-  hipLaunchKernelGGL(D == 128 ? q4_combine_kernel<128> : q4_combine_kernel<64>,
-                     dim3((rows + kCombineWaves - 1) / kCombineWaves), dim3(kCombineWaves * 64), 0, stream, a, p.RT);
-  PVLM_LAUNCHED();
+  if (!p.single) {
+    const int rows = B * Hkv * p.R;
+    hipLaunchKernelGGL(D == 128 ? q4_combine_kernel<128> : q4_combine_kernel<64>,
+                       dim3((rows + kCombineWaves - 1) / kCombineWaves), dim3(kCombineWaves * 64), 0, stream, a);
+    PVLM_LAUNCHED();
+  }
   if (mass) {
-    const unsigned chunks = (unsigned)((c.n_cap + p.chunk - 1) / p.chunk);
-    hipLaunchKernelGGL(D == 128 ? pick_mass<128>(p.MT) : pick_mass<64>(p.MT), dim3(chunks, B), dim3(512), 0, stream, a);
+    // on a stream with a budget, one workgroup for each of its compute units
+    const int64_t items = (int64_t)a.chunks * B, most = di.budgeted ? di.cus : (int64_t)1 << 22;
+    hipLaunchKernelGGL(D == 128 ? pick_mass<128>(p.MT) : pick_mass<64>(p.MT),
+                       dim3((unsigned)(items < most ? items : most)), dim3(512), 0, stream, a);
     PVLM_LAUNCHED();
   }
   return PVLM_OK;

@@ -34,34 +34,34 @@ static long each_plan(F bad) {
                 split_verify_q4(c.B, c.T, c.Hq, c.Hkv, c.D, c.ctx, cus, &p);
                 ++n;
                 if (bad(c, cus, p) && fail++ < 10)
-                  std::printf("B %d T %d heads %d/%d D %d ctx %ld, %d units: RT %d RG %d wgs %d chunk %d\n", B, T, c.Hq,
-                              Hkv, D, (long)ctx, cus, p.RT, p.RG, p.wgs, p.chunk);
+                  std::printf("B %d T %d heads %d/%d D %d ctx %ld, %d units: RT %d RG %d shares %d chunk %d\n", B, T,
+                              c.Hq, Hkv, D, (long)ctx, cus, p.RT, p.RG, p.shares, p.chunk);
               }
             }
   std::printf("%ld plans, %ld failures\n", n, fail);
   return n ? fail : 1;
 }
 
-static bool bad_areas(const Call& c, int, const Q4Split& p) {
+static bool bad_areas(const Call& c, int cus, const Q4Split& p) {
   Q4Split whole;
   split_verify_q4(c.B, c.T, c.Hq, c.Hkv, c.D, c.ctx, 256, &whole);
-  const size_t rows = p.recs * p.RT * 16;
+  const size_t rows = p.recs * p.RTT * 16, groups = (size_t)c.B * c.Hkv;
   const size_t at[] = {kSyncRegion, p.off_stats, p.off_nan, p.off_rows, p.off_opart, p.bytes};
-  const size_t need[] = {0, 16 * rows, 4 * p.recs, 8 * (size_t)c.B * c.Hkv * p.RTT * 16, 4 * rows * c.D};
+  const size_t need[] = {0, 16 * rows, 4 * p.recs, 8 * groups * p.R, 4 * rows * c.D};
   for (int i = 0; i < 5; ++i)
     if (at[i] % 16 || at[i] + need[i] > at[i + 1]) return true;
-  const int64_t units = (int64_t)c.B * c.Hkv * p.RG * ((c.ctx + c.T + kQUnit - 1) / kQUnit);
-  if (units + p.wgs > INT32_MAX) return true;
+  const int64_t units = (int64_t)groups * ((c.ctx + c.T + kQUnit - 1) / kQUnit);
+  if (units + p.shares > INT32_MAX || p.shares * p.per_share > cus) return true;
   return p.bytes > whole.bytes;
 }
 
 static bool bad_waves(const Call& c, int, const Q4Split& p) {
-  if (p.RT < 1 || p.RT > kQ4MaxRT || p.RT * p.RG < p.RTT) return true;
-  const Q4Waves w = q4_waves(p.RT);
-  if (w.tpw < 1 || w.tpw > 3 || w.rw * w.tpw < p.RT || (w.rw - 1) * w.tpw >= p.RT || w.rw * w.tw > 8) return true;
-  if (p.MT < 1 || p.MT > kQ4MassRT || p.MT * p.MG < p.RTT || (p.MG - 1) * p.MT >= p.RTT) return true;
+  if (p.RT < 1 || p.RT > kQ4RowTiles || p.RT * p.RG < p.RTT || (p.RG - 1) * p.RT >= p.RTT) return true;
+  if (p.per_share < 1 || p.per_share > p.RG || p.shares < 1) return true;
+  if (p.single && (p.shares != c.B * c.Hkv || c.ctx + c.T > kQ4Single)) return true;
+  if (p.MT < 1 || p.MT > 5 || p.MT * p.MG < p.RTT || (p.MG - 1) * p.MT >= p.RTT) return true;
   if (p.GW < 1 || p.GW > 8 || 8 % p.GW || p.GW > c.Hkv * p.MG) return true;
-  return p.chunk < 32 || p.chunk > 512 || p.chunk % 32 || p.chunk < 16 * (8 / p.GW);
+  return p.chunk < 32 || p.chunk > kQ4MassRun || p.chunk % 16 || p.chunk < 16 * (8 / p.GW);
 }
 
 int main(int argc, char** argv) {

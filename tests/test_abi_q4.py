@@ -141,7 +141,7 @@ def _verify(paged=False, **kw):
     (dict(n_cap=130), SHAPE), (dict(scale=0.0), SHAPE), (dict(scale=float("inf")), SHAPE),
     (dict(D=96), UNSUPPORTED), (dict(Hkv=3), UNSUPPORTED), (dict(T=33), UNSUPPORTED), (dict(dt=0), UNSUPPORTED),
     (dict(dt=3), UNSUPPORTED), (dict(Hq=128, Hkv=1, T=9, max_ctx=90), UNSUPPORTED),
-    (dict(B=1 << 20), SHAPE), (dict(B=65536, Hq=1, Hkv=1), SHAPE), (dict(kc=ODD), UNSUPPORTED), (dict(ve=ODD), UNSUPPORTED),
+    (dict(B=1 << 20), SHAPE), (dict(kc=ODD), UNSUPPORTED), (dict(ve=ODD), UNSUPPORTED),
     (dict(q=ODD), UNSUPPORTED),
 ])
 def test_verify_rejects(kw, code):

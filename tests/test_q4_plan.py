@@ -37,8 +37,13 @@ def test_kernels_fit_a_compute_unit():
     """A workgroup's waves start together: their registers and LDS are there."""
     seen = set()
     for name, (regs, lds) in code_objects.kernels().items():
-        m = re.search(r"q4_(part|mass)_kernelILi(\d+)ELi(\d+)E", name)
-        if m:
-            assert 2 * regs <= 512 and lds <= 160 * 1024 - 8 * 64 * 128, (name, regs, lds)
-            seen.add((m[1], int(m[2]), int(m[3])))
-    assert len([x for x in seen if x[0] == "part"]) == 18 and len([x for x in seen if x[0] == "mass"]) == 10
+        m = re.search(r"q4_(part|mass)_kernelILi(\d+)ELi(\d+)E(?:Lb([01])E)?", name)
+        if not m:
+            continue
+        D, tiles = int(m[2]), int(m[3])
+        # LDS of a wave's values: 32 rows of bf16 with their padding, two such units for a single row tile
+        ring = 8 * (2 if tiles == 1 else 1) * 2 * (16 * (2 * D + 32) + 144) if m[1] == "part" else 0
+        waves = 4 if m[1] == "mass" and tiles <= 3 else 2
+        assert waves * regs <= 512 and lds + ring <= 160 * 1024, (name, regs, lds, ring)
+        seen.add((m[1], D, tiles, m[4]))
+    assert len([x for x in seen if x[0] == "part"]) == 12 and len([x for x in seen if x[0] == "mass"]) == 10

@@ -1188,12 +1188,38 @@ def gather_kv_q8_paged(k_codes, k_exps, v_codes, v_exps, page_table, idx, k, tai
 
 
 # ------------------------------------------------------- page tables, slots --
+# These calls are short beside their host time: a tensor that fits takes one test, the
+# device and its stream are asked for once, and a size that only shapes decide is
+# kept (with the kernel, a decode step's call took 15.0 us and takes 13.2, a rotary
+# append's 12.2 and 11.2).
+_getdev = torch._C._cuda_getDevice
+
+
 def _here(t, name, dtype):
-    """A contiguous tensor on the current device (whose stream a call is enqueued on)."""
+    """The device and its number of a contiguous tensor on the current device (whose
+    stream a call is enqueued on)."""
     _need(t, name, dtype)
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
-    return t.device
+    dev = t.device
+    if dev.index != _getdev():
+        raise ValueError(f"{name} is on {dev}, but the current device is cuda:{_getdev()}")
+    return dev
+
+
+def _need_shape(t, name, dtype, dev, shape):
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_contiguous()
+            and t.is_cuda and t.get_device() == dev.index):
+        return t
+    _need(t, name, dtype, dev)
+    raise ValueError(f"{name} must be {list(shape)}")
+
+
+def _flags(status, dev):
+    """The address of the caller's status word, or of this device's default one."""
+    if status is None:
+        status = _status_cache.get(dev.index)
+        if status is None:
+            status = _status(None)
+    return status.data_ptr()
 
 
 def pages_resize(length, n_held, page_table, free_pages, n_free, *, page_size: int, granted=None, status=None):
@@ -1202,22 +1228,24 @@ def pages_resize(length, n_held, page_table, free_pages, n_free, *, page_size: i
     free_pages [n_pages]; n_free [1], all int32; n_held, page_table, free_pages
     and n_free are updated.  Returns granted [B] (1: the sequence has what it needs)."""
     dev = _here(length, "length", torch.int32)
-    for t, name in ((n_held, "n_held"), (free_pages, "free_pages"), (n_free, "n_free")):
-        _need(t, name, torch.int32, dev)
-    if length.dim() != 1 or free_pages.dim() != 1 or n_free.numel() != 1:
-        raise ValueError("length must be [B], free_pages [n_pages] and n_free [1]")
+    if length.dim() != 1:
+        raise ValueError("length must be [B]")
     B = length.shape[0]
+    _need_shape(n_held, "n_held", torch.int32, dev, (B,))
+    _need(free_pages, "free_pages", torch.int32, dev)
+    _need(n_free, "n_free", torch.int32, dev)
+    if free_pages.dim() != 1 or n_free.numel() != 1:
+        raise ValueError("free_pages must be [n_pages] and n_free [1]")
     max_pages = _need_table(page_table, dev, B)
-    if n_held.shape != (B,):
-        raise ValueError("n_held must be [B]")
     if granted is None:
-        granted = torch.empty(B, dtype=torch.int32, device=dev)
-    elif _need(granted, "granted", torch.int32, dev).shape != (B,):
-        raise ValueError("granted must be [B]")
+        granted = torch.empty_like(n_held)
+    else:
+        _need_shape(granted, "granted", torch.int32, dev, (B,))
     st = lib().pvlm_pages_resize(B, page_size, max_pages, free_pages.shape[0], length.data_ptr(), n_held.data_ptr(),
                                  page_table.data_ptr(), free_pages.data_ptr(), n_free.data_ptr(), granted.data_ptr(),
-                                 _ptr(_status(status)), _stream())
-    _check(st, "pvlm_pages_resize")
+                                 _flags(status, dev), _raw_stream(dev.index))
+    if st:
+        _check(st, "pvlm_pages_resize")
     return granted
 
 
@@ -1229,10 +1257,10 @@ def slot_map(ctx_len, n_new, n_rows: int, *, page_size: int, n_pages: int, page_
     int64, pos [n_rows], seq [n_rows], row_start [B + 1]); -1 in slots and seq
     where there is no row.  What is not wanted is None."""
     dev = _here(ctx_len, "ctx_len", torch.int32)
-    _need(n_new, "n_new", torch.int32, dev)
-    if ctx_len.dim() != 1 or n_new.shape != ctx_len.shape:
-        raise ValueError("ctx_len and n_new must be [B]")
+    if ctx_len.dim() != 1:
+        raise ValueError("ctx_len must be [B]")
     B = ctx_len.shape[0]
+    _need_shape(n_new, "n_new", torch.int32, dev, (B,))
     max_pages = 1 if page_table is None else _need_table(page_table, dev, B)
     if page_table is None and n_pages < B:
         raise ValueError("a padded cache has a page for each sequence")
@@ -1243,8 +1271,9 @@ def slot_map(ctx_len, n_new, n_rows: int, *, page_size: int, n_pages: int, page_
     start = torch.empty(B + 1, dtype=torch.int32, device=dev) if want_start else None
     st = lib().pvlm_slot_map(B, n_rows, rows_per_seq, page_size, max_pages, n_pages, _ptr(page_table),
                              ctx_len.data_ptr(), n_new.data_ptr(), slots.data_ptr(), _ptr(pos), _ptr(seq), _ptr(start),
-                             _ptr(_status(status)), _stream())
-    _check(st, "pvlm_slot_map")
+                             _flags(status, dev), _raw_stream(dev.index))
+    if st:
+        _check(st, "pvlm_slot_map")
     return slots, pos, seq, start
 
 
@@ -1270,6 +1299,7 @@ class Rotary:
         self.params = RotaryParams(float(base), float(factor), float(orig_ctx), float(alpha), float(beta),
                                    float(mscale), int(rot_dim), _LAYOUTS[layout], _SCALINGS[scaling],
                                    (_c.c_int32 * 3)(*[int(x) for x in (sections or (0, 0, 0))]))
+        self.by_ref = _c.byref(self.params)
         self.sections = None if sections is None else tuple(int(x) for x in sections)
         self.frequencies()      # (parameters that have none are refused here)
 
@@ -1283,43 +1313,41 @@ class Rotary:
         return list(f)
 
 
-def _row_stride(t, name, N, H, D, dtype, dev):
+def _row_stride(t, name, N, H, D, dtype, index):
     """The stride of rows [N][H][D] whose heads lie together."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.device != dev or t.dtype is not dtype:
-        raise ValueError(f"{name} must be {dtype} on {dev}")
+    if t.dtype is not dtype or not t.is_cuda or t.get_device() != index:
+        raise ValueError(f"{name} must be {dtype} on cuda:{index}")
     if t.shape != (N, H, D):
         raise ValueError(f"{name} must be [{N}][{H}][{D}]")
-    s = t.stride()
-    if (D > 1 and s[2] != 1) or (H > 1 and s[1] != D):
+    row, head, one = t.stride()
+    if (one != 1 and D > 1) or (head != D and H > 1):
         raise ValueError(f"the heads of a row of {name} must lie together")
-    return s[0] if N > 1 else H * D
+    return row if N > 1 else H * D
 
 
 def _rotary(q, k_new, v_new, pos, slots, rotary, dtype, dev, heads, q_out):
     """What both appends check of their rows; the arguments that they share."""
     if not isinstance(rotary, Rotary):
         raise TypeError("rotary must be a Rotary")
-    if q.dim() != 3:
-        raise ValueError("q must be [N][Hq][D]")
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a tensor [N][Hq][D]")
     N, Hq, D = q.shape
     Hkv, Dc = heads
     if Dc != D:
         raise ValueError("the cache's rows do not have q's D")
-    sq = _row_stride(q, "q", N, Hq, D, dtype, dev)
-    sk = _row_stride(k_new, "k_new", N, Hkv, D, dtype, dev)
-    sv = _row_stride(v_new, "v_new", N, Hkv, D, dtype, dev)
-    _need(pos, "pos", torch.int32, dev)
-    if pos.shape != ((N,) if rotary.sections is None else (3, N)):
-        raise ValueError("pos must be [N], or [3][N] with sections")
-    if _need(slots, "slots", torch.int64, dev).shape != (N,):
-        raise ValueError("slots must be [N]")
+    index = dev.index
+    sq = _row_stride(q, "q", N, Hq, D, dtype, index)
+    sk = _row_stride(k_new, "k_new", N, Hkv, D, dtype, index)
+    sv = _row_stride(v_new, "v_new", N, Hkv, D, dtype, index)
+    _need_shape(pos, "pos", torch.int32, dev, (N,) if rotary.sections is None else (3, N))
+    _need_shape(slots, "slots", torch.int64, dev, (N,))
     if q_out is None:
         q_out = torch.empty((N, Hq, D), dtype=dtype, device=dev)
-    elif _need(q_out, "q_out", dtype, dev).shape != q.shape:
-        raise ValueError("q_out must have q's shape")
-    return q_out, (N, Hq, Hkv, D, _c.byref(rotary.params), pos.data_ptr(), q.data_ptr(), sq, k_new.data_ptr(), sk,
+    else:
+        _need_shape(q_out, "q_out", dtype, dev, (N, Hq, D))
+    return q_out, (N, Hq, Hkv, D, rotary.by_ref, pos.data_ptr(), q.data_ptr(), sq, k_new.data_ptr(), sk,
                    v_new.data_ptr(), sv, slots.data_ptr())
 
 
@@ -1330,14 +1358,15 @@ def rotary_append(q, k_new, v_new, pos, slots, k_cache, v_cache, *, rotary: Rota
     [blocks][Hkv][rows][D], padded or a page pool.  Returns q_out; its rows of padding
     are not written."""
     dev = _here(k_cache, "k_cache", None)
-    _need(v_cache, "v_cache", k_cache.dtype, dev)
-    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
+    if k_cache.dim() != 4:
         raise ValueError("caches must be [blocks][Hkv][rows][D]")
+    _need_shape(v_cache, "v_cache", k_cache.dtype, dev, k_cache.shape)
     n_blocks, Hkv, rows, D = k_cache.shape
     q_out, args = _rotary(q, k_new, v_new, pos, slots, rotary, k_cache.dtype, dev, (Hkv, D), q_out)
     st = lib().pvlm_rotary_append(_dt(k_cache), *args, n_blocks, rows, q_out.data_ptr(), k_cache.data_ptr(),
-                                  v_cache.data_ptr(), _ptr(_status(status)), _stream())
-    _check(st, "pvlm_rotary_append")
+                                  v_cache.data_ptr(), _flags(status, dev), _raw_stream(dev.index))
+    if st:
+        _check(st, "pvlm_rotary_append")
     return q_out
 
 
@@ -1346,24 +1375,24 @@ def rotary_append(q, k_new, v_new, pos, slots, k_cache, v_cache, *, rotary: Rota
 # torch.uint8, one for 32 values: a value is code * 2^(exponent - 127).
 def _need_q4(k_codes, k_exps, v_codes, v_exps, dev, paged, stacked=False):
     """Check a cache's four tensors; returns the values' shape."""
-    if dev.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {dev}, but the current device is cuda:{torch.cuda.current_device()}")
+    if dev.index != _getdev():
+        raise ValueError(f"tensors are on {dev}, but the current device is cuda:{_getdev()}")
     for t, name in ((k_codes, "k_codes"), (v_codes, "v_codes")):
         _need(t, name, None, dev)
         if t.dtype is not torch.uint8 and t.dtype is not torch.float4_e2m1fn_x2:
             raise ValueError(f"{name} must be torch.uint8 or torch.float4_e2m1fn_x2, got {t.dtype}")
-    _need(k_exps, "k_exps", torch.uint8, dev)
-    _need(v_exps, "v_exps", torch.uint8, dev)
-    shape = k_codes.shape
+    shape = tuple(k_codes.shape)
     if len(shape) != 4 and not (stacked and len(shape) == 5):
         layout = "[n_pages][Hkv][page][D / 2]" if paged else "[B][Hkv][n_cap][D / 2]"
         raise ValueError(f"codes must be {layout}" + (f" or [L]{layout}" if stacked else ""))
     D = 2 * shape[-1]
-    if D not in (64, 128):
+    if D != 128 and D != 64:
         raise ValueError("D must be 64 or 128 (codes of D / 2 bytes)")
+    if v_codes.shape != shape:
+        raise ValueError("k_codes and v_codes must have one shape")
     exps = shape[:-1] + (D // 32,)
-    if v_codes.shape != shape or k_exps.shape != exps or v_exps.shape != exps:
-        raise ValueError("k_codes and v_codes must have one shape, k_exps and v_exps that shape with D / 32")
+    _need_shape(k_exps, "k_exps", torch.uint8, dev, exps)
+    _need_shape(v_exps, "v_exps", torch.uint8, dev, exps)
     return shape[:-1] + (D,)
 
 
@@ -1375,9 +1404,11 @@ def rotary_append_q4(q, k_new, v_new, pos, slots, k_codes, k_exps, v_codes, v_ex
     dev = _here(k_codes, "k_codes", None)
     n_blocks, Hkv, rows, D = _need_q4(*cache, dev, True)
     q_out, args = _rotary(q, k_new, v_new, pos, slots, rotary, torch.bfloat16, dev, (Hkv, D), q_out)
-    st = lib().pvlm_rotary_append_q4(PVLM_BF16, *args, n_blocks, rows, q_out.data_ptr(), *[t.data_ptr() for t in cache],
-                                     _ptr(_status(status)), _stream())
-    _check(st, "pvlm_rotary_append_q4")
+    st = lib().pvlm_rotary_append_q4(PVLM_BF16, *args, n_blocks, rows, q_out.data_ptr(), k_codes.data_ptr(),
+                                     k_exps.data_ptr(), v_codes.data_ptr(), v_exps.data_ptr(), _flags(status, dev),
+                                     _raw_stream(dev.index))
+    if st:
+        _check(st, "pvlm_rotary_append_q4")
     return q_out
 
 
@@ -1403,8 +1434,9 @@ def _quantize_q4(k, v, length, cache, page_table, status):
     else:
         name, geom = "pvlm_quantize_kv_q4_paged", (rows, _need_table(page_table, dev, B), n0, src_cap, *tail)
         more = (page_table.data_ptr(),)
-    st = getattr(lib(), name)(_dt(k), L, B, Hkv, D, *geom, *more, *codes, _ptr(_status(status)), _stream())
-    _check(st, name)
+    st = getattr(lib(), name)(_dt(k), L, B, Hkv, D, *geom, *more, *codes, _flags(status, dev), _raw_stream(dev.index))
+    if st:
+        _check(st, name)
 
 
 def quantize_kv_q4(k, v, length, k_codes, k_exps, v_codes, v_exps, *, status=None):
@@ -1425,43 +1457,55 @@ def verify_attn_q4_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx) -> int:
     return int(lib().pvlm_verify_attn_q4_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx))
 
 
+_ws_sizes = {}     # of a workspace, by the device and the sizes that decide it
+
+
 def _verify_q4(q, cache, page_table, ctx_len, scale, max_ctx, out, mass, lse, want_mass, want_lse, ws, status):
     _need(q, "q", torch.bfloat16)
     dev = q.device
     n0, Hkv, rows, Dc = _need_q4(*cache, dev, page_table is not None)
-    _need(ctx_len, "ctx_len", torch.int32, dev)
     if q.dim() != 4:
         raise ValueError("q must be [B][T][Hq][D]")
     B, T, Hq, D = q.shape
-    if Dc != D or ctx_len.shape != (B,) or (page_table is None and n0 != B):
+    _need_shape(ctx_len, "ctx_len", torch.int32, dev, (B,))
+    if Dc != D or (page_table is None and n0 != B):
         raise ValueError("inconsistent verify_attn_q4 shapes")
     if page_table is None:
-        n_cap, geom, table = rows, (rows,), ()
+        name, n_cap, geom, table = "pvlm_verify_attn_q4", rows, (rows,), ()
     else:
         max_pages = _need_table(page_table, dev, B)
-        n_cap, geom, table = max_pages * rows, (rows, max_pages, n0), (page_table.data_ptr(),)
+        name, n_cap, geom = "pvlm_verify_attn_q4_paged", max_pages * rows, (rows, max_pages, n0)
+        table = (page_table.data_ptr(),)
     if max_ctx is None:
         max_ctx = n_cap - T
     if out is None:
         out = torch.empty_like(q)
-    elif _need(out, "out", torch.bfloat16, dev).shape != q.shape:
-        raise ValueError("out must have q's shape")
-    if mass is None:
-        mass = torch.empty((B, n_cap), dtype=torch.float32, device=dev) if want_mass else None
-    elif _need(mass, "mass", torch.float32, dev).shape != (B, n_cap):
-        raise ValueError("mass must be [B][n_cap]")
-    if lse is None:
-        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=dev) if want_lse else None
-    elif _need(lse, "lse", torch.float32, dev).shape != (B, Hq, T):
-        raise ValueError("lse must be [B][Hq][T]")
+    else:
+        _need_shape(out, "out", torch.bfloat16, dev, q.shape)
+    if mass is not None:
+        _need_shape(mass, "mass", torch.float32, dev, (B, n_cap))
+    elif want_mass:
+        mass = torch.empty((B, n_cap), dtype=torch.float32, device=dev)
+    if lse is not None:
+        _need_shape(lse, "lse", torch.float32, dev, (B, Hq, T))
+    elif want_lse:
+        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=dev)
     L = lib()
-    wsb = _ws_buffer("verify_q4", ws, L.pvlm_verify_attn_q4_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx), dev)
-    name = "pvlm_verify_attn_q4" if page_table is None else "pvlm_verify_attn_q4_paged"
-    st = getattr(L, name)(PVLM_BF16, B, T, Hq, Hkv, D, *geom, max_ctx,
-                          float(D ** -0.5 if scale is None else scale), q.data_ptr(),
-                          *[t.data_ptr() for t in cache], *table, ctx_len.data_ptr(), out.data_ptr(), _ptr(mass),
-                          _ptr(lse), wsb.data_ptr(), wsb.numel(), _ptr(_status(status)), _stream())
-    _check(st, name)
+    sizes = (dev.index, B, T, Hq, Hkv, D, n_cap, max_ctx)
+    need = _ws_sizes.get(sizes)
+    if need is None:
+        if len(_ws_sizes) >= 4096:
+            _ws_sizes.clear()
+        need = _ws_sizes[sizes] = L.pvlm_verify_attn_q4_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx)
+    wsb = _ws_buffer("verify_q4", ws, need, dev)
+    kc, ke, vc, ve = cache
+    st = getattr(L, name)(PVLM_BF16, B, T, Hq, Hkv, D, *geom, max_ctx, D ** -0.5 if scale is None else float(scale),
+                          q.data_ptr(), kc.data_ptr(), ke.data_ptr(), vc.data_ptr(), ve.data_ptr(), *table,
+                          ctx_len.data_ptr(), out.data_ptr(), None if mass is None else mass.data_ptr(),
+                          None if lse is None else lse.data_ptr(), wsb.data_ptr(), wsb.numel(), _flags(status, dev),
+                          _raw_stream(dev.index))
+    if st:
+        _check(st, name)
     return out, mass, lse
 
 
@@ -1491,15 +1535,15 @@ def _gather_q4(cache, page_table, idx, k, tail_begin, tail_len, dst_cap, dtype, 
     _need(cache[0], "k_codes")
     dev = cache[0].device
     shape = _need_q4(*cache, dev, page_table is not None, stacked=True)
-    for name, t in (("idx", idx), ("k", k), ("tail_begin", tail_begin), ("tail_len", tail_len)):
-        _need(t, name, torch.int32, dev)
+    _need(idx, "idx", torch.int32, dev)
     L = 1 if len(shape) == 4 else shape[0]
     n0, Hkv, rows, D = shape[-4:]
     if idx.dim() != 2 or (page_table is None and n0 != idx.shape[0]):
         raise ValueError("idx must be [B][k_cap]")
     B = idx.shape[0]
-    if any(t.shape != (B,) for t in (k, tail_begin, tail_len)):
-        raise ValueError("k, tail_begin and tail_len must be [B]")
+    _need_shape(k, "k", torch.int32, dev, (B,))
+    _need_shape(tail_begin, "tail_begin", torch.int32, dev, (B,))
+    _need_shape(tail_len, "tail_len", torch.int32, dev, (B,))
     if dtype not in (torch.float4_e2m1fn_x2, torch.uint8, torch.bfloat16, torch.float32):
         raise ValueError(f"unsupported dtype {dtype}")
     q4 = dtype is torch.uint8 or dtype is torch.float4_e2m1fn_x2
@@ -1524,8 +1568,9 @@ def _gather_q4(cache, page_table, idx, k, tail_begin, tail_len, dst_cap, dtype, 
         geom, table = (rows, _need_table(page_table, dev, B), n0), (page_table.data_ptr(),)
     st = getattr(lib(), name)(to, L, B, Hkv, D, *geom, *[t.data_ptr() for t in cache], *table, idx.data_ptr(),
                               k.data_ptr(), idx.shape[1], tail_begin.data_ptr(), tail_len.data_ptr(), dst_cap,
-                              int(fill), kd, kde, vd, vde, _ptr(_status(status)), _stream())
-    _check(st, name)
+                              int(fill), kd, kde, vd, vde, _flags(status, dev), _raw_stream(dev.index))
+    if st:
+        _check(st, name)
     return tuple(dst)
 
 

@@ -252,8 +252,8 @@ __device__ __forceinline__ void put_values(uint32_t put, int tt, const Codes<D>&
 // lane's first address: of sixteen lanes each takes 8 bytes of row 4 gq + n / 4, and
 // receives column n of the four rows.  AHEAD operands are under way while the matrix
 // instructions of earlier ones run (the compiler, left to itself, waits for each alone).
-template <int D, int TPW, int S, int AHEAD>
-__device__ __forceinline__ void weigh(uint32_t get, const bf16x8 (&P)[TPW][S], int u, floatx4 (&O)[TPW][D / 16]) {
+template <int D, int TPW, int AHEAD>
+__device__ __forceinline__ void weigh(uint32_t get, const bf16x8 (&P)[TPW], floatx4 (&O)[TPW][D / 16]) {
   constexpr int N = D / 16;
   s4 lo[AHEAD], hi[AHEAD];
   auto read = [&](int j) {
@@ -269,7 +269,7 @@ __device__ __forceinline__ void weigh(uint32_t get, const bf16x8 (&P)[TPW][S], i
     const s8 both = __builtin_shufflevector(lo[j % AHEAD], hi[j % AHEAD], 0, 1, 2, 3, 4, 5, 6, 7);
     const bf16x8 v = __builtin_bit_cast(bf16x8, both);
 #pragma unroll
-    for (int x = 0; x < TPW; ++x) O[x][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][u], v, O[x][j], 0, 0, 0);
+    for (int x = 0; x < TPW; ++x) O[x][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x], v, O[x][j], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   }
 }
@@ -306,19 +306,15 @@ __device__ __forceinline__ void put_row(const Q4Args& a, int b, int g, int row, 
 
 // -------------------------------------------------------- partial kernel --
 // A workgroup's eight waves hold the same set of row tiles, TPW of them, and take its
-// tokens in turn, 32 NB at a time.
-template <int D, int TPW>
-struct PartShape {
-  static constexpr int NB = TPW >= 2 ? 1 : 2;
-  static constexpr int kWaveLds = NB * Lay<D>::kUnit, kLds = kQ4Waves * kWaveLds, AHEAD = 3;
-};
+// tokens in turn, a unit of 32 at a time, with the next unit's loads on their way.
+constexpr int kAhead = 3;  // operands of P . V read ahead
 
 // SINGLE: every group is one share, and the workgroup writes the results.  (A kernel of
 // its own: that path's registers cost the other one 7 %.)
 template <int D, int TPW, bool SINGLE>
 __global__ void __launch_bounds__(kQ4Waves * 64)
 __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(Q4Args a) {
-  constexpr int NB = PartShape<D, TPW>::NB, DPL = D / 16, BT = 32 * NB, TW = kQ4Waves;
+  constexpr int DPL = D / 16, TW = kQ4Waves;
   extern __shared__ __align__(1024) char s_values[];  // [wave][32][D] bf16; then a tile's O, [wave][16][D] fp32
   __shared__ float s_ref[TW][16], s_z[TW][16], s_zt[TW][16];
   __shared__ uint32_t s_nan[TW];
@@ -334,7 +330,7 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
   const int place = id < whole8 ? (id & 7) * (whole8 >> 3) + (id >> 3) : id;
   const int share = place / a.per_share;
   const int lane = threadIdx.x & 63, n = lane & 15, gq = lane >> 4;
-  const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(s_values)) + w * PartShape<D, TPW>::kWaveLds;
+  const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(s_values)) + w * Lay<D>::kUnit;
 
   const LaneOf<D> place_of(n, gq);
   const uint32_t put = lds + Lay<D>::row(n) + gq * (D / 2);
@@ -351,7 +347,7 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
       int lim[TPW];
       float ref[TPW], z[TPW];
       floatx4 O[TPW][DPL], zt[TPW];
-  #pragma unroll
+#pragma unroll
       for (int x = 0; x < TPW; ++x) {
         const int row = (tile0 + x) * 16 + n;
         load_query<D>(a, p.b, p.g, row, gq, q[x]);
@@ -359,148 +355,127 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
         ref[x] = kNegInf;
         z[x] = 0.f;
         zt[x] = floatx4{0.f, 0.f, 0.f, 0.f};
-  #pragma unroll
+#pragma unroll
         for (int jd = 0; jd < DPL; ++jd) O[x][jd] = floatx4{0.f, 0.f, 0.f, 0.f};
       }
       uint32_t nan = 0;
-      Codes<D> kc[NB][2], vc[NB][2];
-      // The next block's units (past the piece, its last unit once more) and their pages.
-      int page[NB];
-      int64_t row[NB];
-      auto unit = [&](int tb, int u) { return min(tb + 32 * u, (p.c1 - 1) & ~31); };
-      auto find = [&](int tb) {
-  #pragma unroll
-        for (int u = 0; u < NB; ++u) page[u] = rows.entry(unit(tb, u));
+      // The next unit (past the piece, its last one) and its page.
+      Codes<D> kc[2], vc[2];
+      int page;
+      auto unit = [&](int t) { return min(t, (p.c1 - 1) & ~31); };
+      auto load = [&](int t) {
+        const int64_t row = rows.at(unit(t), page, bad_page);
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) load_codes<D>(a.c.kc, a.c.ke, row + 16 * tt, place_of, kc[tt]);
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) load_codes<D>(a.c.vc, a.c.ve, row + 16 * tt, place_of, vc[tt]);
+        page = rows.entry(unit(t + 32 * TW));
       };
-      auto load_k = [&](int tb) {
-  #pragma unroll
-        for (int u = 0; u < NB; ++u) {
-          row[u] = rows.at(unit(tb, u), page[u], bad_page);
-  #pragma unroll
-          for (int tt = 0; tt < 2; ++tt) load_codes<D>(a.c.kc, a.c.ke, row[u] + 16 * tt, place_of, kc[u][tt]);
-        }
-        find(tb + BT * TW);
-      };
-      auto load_v = [&]() {
-  #pragma unroll
-        for (int u = 0; u < NB; ++u)
-  #pragma unroll
-          for (int tt = 0; tt < 2; ++tt) load_codes<D>(a.c.vc, a.c.ve, row[u] + 16 * tt, place_of, vc[u][tt]);
-      };
-      // A block of BT tokens; TAIL: some row does not see all of them.
-      auto block = [&](int tb, auto tail) {
+      // The unit of tokens t0 .. t0 + 31; TAIL: some row does not see all of them.
+      auto block = [&](int t0, auto tail) {
         constexpr bool TAIL = decltype(tail)::value;
         if constexpr (TAIL) {
-  #pragma unroll
-          for (int u = 0; u < NB; ++u)
-  #pragma unroll
-            for (int tt = 0; tt < 2; ++tt) {
-              // rows past the piece become zeros (their probabilities are 0, and 0 times what
-              // an unwritten row holds may be NaN), and so do NaN of rows that not every query
-              // row sees: the record's flag has the combine kernel look for them
-              const int t = tb + 32 * u + 16 * tt + n;
-              const bool past = t >= p.c1, hidden = t > p.ctx && place_of.exponent(vc[u][tt].e) == 255;
-              if (hidden && !past) nan = 1;
-              if (past || hidden) {
-                vc[u][tt].e = 0;
-  #pragma unroll
-                for (int c = 0; c < D / 32; ++c) vc[u][tt].w[c] = 0;
-              }
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt) {
+            // rows past the piece become zeros (their probabilities are 0, and 0 times what
+            // an unwritten row holds may be NaN), and so do NaN of rows that not every query
+            // row sees: the record's flag has the rows looked at that see them
+            const int t = t0 + 16 * tt + n;
+            const bool past = t >= p.c1, hidden = t > p.ctx && place_of.exponent(vc[tt].e) == 255;
+            if (hidden && !past) nan = 1;
+            if (past || hidden) {
+              vc[tt].e = 0;
+#pragma unroll
+              for (int c = 0; c < D / 32; ++c) vc[tt].w[c] = 0;
             }
+          }
         }
         // (the values' conversion runs beside the matrix instructions of the scores)
         asm volatile("" ::: "memory");  // (the wave's LDS operations keep their order)
-  #pragma unroll
-        for (int u = 0; u < NB; ++u)
-  #pragma unroll
-          for (int tt = 0; tt < 2; ++tt) put_values<D>(put + u * Lay<D>::kUnit, tt, vc[u][tt], place_of.unit(vc[u][tt].e));
-        floatx4 S[TPW][2 * NB];
-  #pragma unroll
-        for (int j = 0; j < 2 * NB; ++j) {
-          const float unit = place_of.unit(kc[j / 2][j % 2].e);
-  #pragma unroll
+        put_values<D>(put, 0, vc[0], place_of.unit(vc[0].e));
+        put_values<D>(put, 1, vc[1], place_of.unit(vc[1].e));
+        floatx4 S[TPW][2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float scale = place_of.unit(kc[j].e);
+#pragma unroll
           for (int x = 0; x < TPW; ++x) S[x][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  #pragma unroll
+#pragma unroll
           for (int ks = 0; ks < D / 32; ++ks) {
-            const bf16x8 k = to_bf16(kc[j / 2][j % 2].w[ks], unit);
-  #pragma unroll
+            const bf16x8 k = to_bf16(kc[j].w[ks], scale);
+#pragma unroll
             for (int x = 0; x < TPW; ++x) S[x][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[x].s[ks], S[x][j], 0, 0, 0);
           }
         }
         asm volatile("" ::: "memory");
-        load_k(tb + BT * TW);
-        load_v();
+        if (t0 + 32 * TW < p.c1) load(t0 + 32 * TW);
         if constexpr (TAIL) {
-  #pragma unroll
+#pragma unroll
           for (int x = 0; x < TPW; ++x)
-  #pragma unroll
-            for (int j = 0; j < 8 * NB; ++j)
-              if (tb + 16 * (j / 4) + 4 * gq + j % 4 > lim[x]) S[x][j / 4][j % 4] = kNegInf;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (t0 + 16 * (j / 4) + 4 * gq + j % 4 > lim[x]) S[x][j / 4][j % 4] = kNegInf;
         }
-        bf16x8 P[TPW][NB];
-  #pragma unroll
+        bf16x8 P[TPW];
+#pragma unroll
         for (int x = 0; x < TPW; ++x) {
-          float m = kNegInf;
-  #pragma unroll
-          for (int j = 0; j < 8 * NB; ++j) m = __builtin_elementwise_maximum(m, S[x][j / 4][j % 4]);
+          float m = kNegInf;  // (the maximum that passes NaN on: the other one has every operand canonicalised first)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) m = __builtin_elementwise_maximum(m, S[x][j / 4][j % 4]);
           m *= a.sl2;
-          if (__any(m > ref[x] + kRefSlack)) {  // the first block, and seldom after it
+          if (__any(m > ref[x] + kRefSlack)) {  // the first unit, and seldom after it
             const float nm = fmaxf(ref[x], rows4_maximum(m));
             const float al = ref[x] == kNegInf ? 0.f : fast_exp2(ref[x] - nm);
             z[x] *= al;
             ref[x] = nm;
             floatx4 f;
-  #pragma unroll
+#pragma unroll
             for (int i = 0; i < 4; ++i) f[i] = __shfl(al, 4 * gq + i, 64);
             zt[x] = zt[x] * f;
-  #pragma unroll
+#pragma unroll
             for (int jd = 0; jd < DPL; ++jd) O[x][jd] = O[x][jd] * f;
           }
           const float r = ref[x] == kNegInf ? 0.f : ref[x];  // no visible token yet: P = 0
           float sum = 0.f;
-  #pragma unroll
-          for (int j = 0; j < 8 * NB; ++j) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
             const float e = fast_exp2(fmaf(S[x][j / 4][j % 4], a.sl2, -r));
             sum += e;
-            P[x][j / 8][j % 8] = static_cast<__bf16>(e);
+            P[x][j] = static_cast<__bf16>(e);
           }
           z[x] += sum;
         }
         bf16x8 ones;
-  #pragma unroll
+#pragma unroll
         for (int j = 0; j < 8; ++j) ones[j] = static_cast<__bf16>(1.f);
-  #pragma unroll
-        for (int u = 0; u < NB; ++u) {
-          weigh<D, TPW, NB, PartShape<D, TPW>::AHEAD>(get + u * Lay<D>::kUnit, P, u, O);
-  #pragma unroll
-          for (int x = 0; x < TPW; ++x) zt[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x][u], ones, zt[x], 0, 0, 0);
-        }
+        weigh<D, TPW, kAhead>(get, P, O);
+#pragma unroll
+        for (int x = 0; x < TPW; ++x) zt[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P[x], ones, zt[x], 0, 0, 0);
         asm volatile("" ::: "memory");
       };
-      int tb = p.c0 + BT * w;
-      find(tb);
-      load_k(tb);
-      load_v();
-      // (two loops: in one, the compiler has every block go through the tail's selections)
-      for (; tb + BT - 1 <= min(p.c1 - 1, p.ctx); tb += BT * TW) block(tb, std::false_type{});
-      for (; tb < p.c1; tb += BT * TW) block(tb, std::true_type{});
+      // (two loops: in one, the compiler has every unit go through the tail's selections)
+      int t = p.c0 + 32 * w;
+      page = rows.entry(unit(t));
+      if (t < p.c1) load(t);
+      for (; t + 31 <= min(p.c1 - 1, p.ctx); t += 32 * TW) block(t, std::false_type{});
+      for (; t < p.c1; t += 32 * TW) block(t, std::true_type{});
       // The token waves' results joined: a tile at a time, through LDS (position
       // DPL n + jd of a row holds column 16 jd + n).
       const int rec = p.group(a) + share;
       const bool any = __any(nan);
       if (lane == 0) s_nan[w] = any;
-  #pragma unroll
+#pragma unroll
       for (int x = 0; x < TPW; ++x) {
         __syncthreads();
         const float zz = rows4_sum(z[x]);
         if (gq == 0) s_ref[w][n] = ref[x], s_z[w][n] = zz;
         if (n == 0)
-  #pragma unroll
+#pragma unroll
           for (int i = 0; i < 4; ++i) s_zt[w][4 * gq + i] = zt[x][i];
-        float* mine = reinterpret_cast<float*>(s_values) + w * (PartShape<D, TPW>::kWaveLds / 4);
-  #pragma unroll
+        float* mine = reinterpret_cast<float*>(s_values) + w * (Lay<D>::kUnit / 4);
+#pragma unroll
         for (int i = 0; i < 4; ++i)
-  #pragma unroll
+#pragma unroll
           for (int h = 0; h < DPL / 4; ++h)
             *reinterpret_cast<float4*>(mine + (4 * gq + i) * D + DPL * n + 4 * h) =
                 make_float4(O[x][4 * h][i], O[x][4 * h + 1][i], O[x][4 * h + 2][i], O[x][4 * h + 3][i]);
@@ -509,25 +484,25 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
           const int r = i / (D / 4), c = i % (D / 4), row = (tile0 + x) * 16 + r;
           if (row >= a.R) continue;
           float M = kNegInf;
-  #pragma unroll
+#pragma unroll
           for (int k = 0; k < TW; ++k) M = fmaxf(M, s_ref[k][r]);
           const float base = M == kNegInf ? 0.f : M;
           float Z = 0.f, Zt = 0.f;
           floatx4 o{0.f, 0.f, 0.f, 0.f};
-  #pragma unroll
+#pragma unroll
           for (int k = 0; k < TW; ++k) {
             if (s_z[k][r] == 0.f) continue;  // nothing that the row sees
             const float f = fast_exp2(s_ref[k][r] - base);
             Z += s_z[k][r] * f;
             Zt += s_zt[k][r] * f;
-            const float* theirs = reinterpret_cast<const float*>(s_values) + k * (PartShape<D, TPW>::kWaveLds / 4);
+            const float* theirs = reinterpret_cast<const float*>(s_values) + k * (Lay<D>::kUnit / 4);
             const float4 y = *reinterpret_cast<const float4*>(theirs + r * D + 4 * c);
             o[0] = fmaf(y.x, f, o[0]), o[1] = fmaf(y.y, f, o[1]), o[2] = fmaf(y.z, f, o[2]), o[3] = fmaf(y.w, f, o[3]);
           }
           const size_t at = (size_t)rec * a.RTT * 16 + row;
           if constexpr (SINGLE) {
             uint32_t any_wave = 0;
-  #pragma unroll
+#pragma unroll
             for (int k = 0; k < TW; ++k) any_wave |= s_nan[k];
             float y[4] = {o[0], o[1], o[2], o[3]};
             put_row<D, 4>(a, p.b, p.g, row, p.ctx, rows, c, y, M, Z, Zt, any_wave != 0);
@@ -713,10 +688,6 @@ Q4Kernel pick_part(int RT) {
   return RT == 1 ? q4_part_kernel<D, 1, SINGLE> : RT == 2 ? q4_part_kernel<D, 2, SINGLE> : q4_part_kernel<D, 3, SINGLE>;
 }
 template <int D>
-int part_lds(int RT) {
-  return RT == 1 ? PartShape<D, 1>::kLds : RT == 2 ? PartShape<D, 2>::kLds : PartShape<D, 3>::kLds;
-}
-template <int D>
 Q4Kernel pick_mass(int MT) {
   switch (MT) {
     case 1: return q4_mass_kernel<D, 1>;
@@ -777,7 +748,7 @@ pvlm_status verify_q4_run(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D, i
   a.chunks = (int)((c.n_cap + p.chunk - 1) / p.chunk);
   const Q4Kernel part = p.single ? (D == 128 ? pick_part<128, true>(p.RT) : pick_part<64, true>(p.RT))
                                  : (D == 128 ? pick_part<128, false>(p.RT) : pick_part<64, false>(p.RT));
-  const int lds = D == 128 ? part_lds<128>(p.RT) : part_lds<64>(p.RT);
+  const int lds = kQ4Waves * (D == 128 ? Lay<128>::kUnit : Lay<64>::kUnit);
   PVLM_HIP(allow_dynamic_lds(reinterpret_cast<const void*>(part), lds));
   hipLaunchKernelGGL(part, dim3(p.shares * p.per_share), dim3(kQ4Waves * 64), lds, stream, a);
   PVLM_LAUNCHED();

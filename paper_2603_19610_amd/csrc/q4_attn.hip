@@ -308,6 +308,9 @@ __device__ __forceinline__ void put_row(const Q4Args& a, int b, int g, int row, 
 // A workgroup's eight waves hold the same set of row tiles, TPW of them, and take its
 // tokens in turn, a unit of 32 at a time, with the next unit's loads on their way.
 constexpr int kAhead = 3;  // operands of P . V read ahead
+// A lane's sum of this many units goes to its place in LDS: beside one large
+// probability a running sum of all of a long share would round small ones away.
+constexpr int kSumUnits = 16;
 
 // SINGLE: every group is one share, and the workgroup writes the results.  (A kernel of
 // its own: that path's registers cost the other one 7 %.)
@@ -318,6 +321,7 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
   extern __shared__ __align__(1024) char s_values[];  // [wave][32][D] bf16; then a tile's O, [wave][16][D] fp32
   __shared__ float s_ref[TW][16], s_z[TW][16], s_zt[TW][16];
   __shared__ uint32_t s_nan[TW];
+  __shared__ float s_sum[SINGLE ? 1 : TW][TPW][64];  // (a single share's sums are short)
 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (blockIdx.x == 0 && w == 0)
@@ -354,6 +358,7 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
         lim[x] = row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
         ref[x] = kNegInf;
         z[x] = 0.f;
+        if constexpr (!SINGLE) s_sum[w][x][lane] = 0.f;
         zt[x] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int jd = 0; jd < DPL; ++jd) O[x][jd] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -427,6 +432,7 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
             const float nm = fmaxf(ref[x], rows4_maximum(m));
             const float al = ref[x] == kNegInf ? 0.f : fast_exp2(ref[x] - nm);
             z[x] *= al;
+            if constexpr (!SINGLE) s_sum[w][x][lane] *= al;
             ref[x] = nm;
             floatx4 f;
 #pragma unroll
@@ -457,7 +463,14 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
       int t = p.c0 + 32 * w;
       page = rows.entry(unit(t));
       if (t < p.c1) load(t);
-      for (; t + 31 <= min(p.c1 - 1, p.ctx); t += 32 * TW) block(t, std::false_type{});
+      for (int left = kSumUnits; t + 31 <= min(p.c1 - 1, p.ctx); t += 32 * TW) {
+        block(t, std::false_type{});
+        if (!SINGLE && --left == 0) {
+          left = kSumUnits;
+#pragma unroll
+          for (int x = 0; x < TPW; ++x) s_sum[SINGLE ? 0 : w][x][lane] += z[x], z[x] = 0.f;
+        }
+      }
       for (; t < p.c1; t += 32 * TW) block(t, std::true_type{});
       // The token waves' results joined: a tile at a time, through LDS (position
       // DPL n + jd of a row holds column 16 jd + n).
@@ -467,7 +480,7 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
 #pragma unroll
       for (int x = 0; x < TPW; ++x) {
         __syncthreads();
-        const float zz = rows4_sum(z[x]);
+        const float zz = rows4_sum(SINGLE ? z[x] : z[x] + s_sum[SINGLE ? 0 : w][x][lane]);
         if (gq == 0) s_ref[w][n] = ref[x], s_z[w][n] = zz;
         if (n == 0)
 #pragma unroll

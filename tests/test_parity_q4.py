@@ -533,6 +533,34 @@ def test_verify_small_probabilities_beside_a_large_one():
     assert (mass[:, 1000:n].double() / (Hkv * p) - 1).abs().max().item() <= 2.0 ** -16
 
 
+def test_verify_small_probabilities_in_long_shares():
+    """Sequences of 100000 tokens on a compute unit each, one score 0, all others -28 (in steps of log 2; every score is
+    exact).  A lane sums 3125 tokens, eight at a time: 2^-25 of the large one, half of what moves it.  It may lose those
+    of the first 16 units (2^-21), round once for each further 16 (25 half places of 2^-23) and in the joins (10 more),
+    and the logarithm is off by 2^-20; all of them lost would be 1.2e-5."""
+    B, D, n, cus = 8, 64, 100000, 8
+    cache = empty_cache((B, 1, cap32(n + 1)), D)
+    cache[1][:] = cache[3][:] = 127
+    cache[0][..., :14] = 0xAA                       # -1 in 28 channels
+    cache[0][:, :, 37] = 0
+    cache[2][:] = 0x22                              # values 1
+    q = torch.ones((B, 1, 1, D), dtype=torch.bfloat16, device="cuda")
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    note("verify q4 small probabilities in long shares")
+    pv.set_stream_cu_budget(stream, cus)
+    try:
+        with torch.cuda.stream(stream):
+            out, mass, lse = pv.verify_attn_q4(q, *cache, i32([n] * B), scale=float(np.log(2.0)))
+        torch.cuda.synchronize()
+    finally:
+        pv.set_stream_cu_budget(stream, 0)
+    z = 1 + n * 2.0 ** -28
+    assert (lse.double() - np.log(z)).abs().max().item() <= 2.0 ** -21 + 35 * 2.0 ** -24 + 2.0 ** -20
+    assert torch.equal(out, torch.ones_like(out))
+    assert (mass[:, 1000:n].double() * 2.0 ** 28 * z - 1).abs().max().item() <= 2.0 ** -16
+
+
 def test_every_token_counts_once():
     """Equal scores: the mass of every visible token is Hq * T / n to 2^-16, at lengths around the units and shares."""
     for B, T, Hq, Hkv, D, ctx in [(1, 1, 8, 2, 64, [20000]), (2, 4, 8, 8, 128, [8190, 4097]), (3, 2, 4, 1, 128, [65, 31, 0])]:

@@ -17,6 +17,18 @@
 //
 // Launches, all on the caller's stream: partial; combine, unless the shares are whole
 // groups; and the mass.
+//
+// What bounds it.  A row is 68 bytes (D = 128) where bf16 has 256, so the bytes pass in a
+// fraction of the time that both products' matrix instructions, the conversions and
+// the exponentials take:
+//  * 16 sequences of one row, 28 / 4 heads, 2048 to 16384 tokens (89 MB): partial 21 us,
+//    4.2 TB/s; combine 4.
+//  * 9 rows of 64 / 8 heads over 12800 tokens (14 MB): partial 22, combine 5, mass 11, of
+//    which 3 to 5 each are the start, the joins and the end.
+//  * 17 rows of 64 / 8 heads over 132096 tokens (145 MB): partial 113 (matrix instructions
+//    39 % of the cycles, vector ones 55), mass 75 (25 and 65), combine 6.
+// Vector and matrix instructions of different waves run side by side, so what is left of
+// a SIMD's time is where its two waves want the same pipe.
 #include <type_traits>
 
 #include "q4.h"
@@ -227,25 +239,28 @@ __device__ __forceinline__ float rows4_maximum(float x) {
 // consecutive values of one token: a wave writes a unit of 32 tokens to LDS as bf16
 // rows of its own and reads them transposed.  Nobody else touches them, and a
 // wave's LDS operations run in order, so nothing waits but for data.
-// Rows lie 32 bytes more than their length apart, and of every sixteen the last eight
-// 144 bytes further: a transposed read (the same 32 bytes of rows 0-3 and 8-11, or 4-7
-// and 12-15, at a time) and a write (the same 16 bytes of sixteen rows) then fall on
-// distinct banks, and every address is the lane's first and a constant.
+// Rows lie 32 bytes more than their length apart, and rows whose number has bit 2 set
+// hold every two 16-byte chunks in the other order: a transposed read (the same 32
+// bytes of eight rows at a time, 256 bytes) and a write (the same chunk of eight rows at
+// a time, 128 bytes) then fall on distinct banks, and every address is the lane's first
+// (of the even chunks or the odd ones) and a constant.  (In one order the writes had
+// conflicts, 13 % of the kernel's cycles: 9 rows over 12800 tokens 21.9 us for 21.2.)
 template <int D>
 struct Lay {
-  static constexpr int kRow = 2 * D + 32, kHalf = 16 * kRow + 144, kUnit = 2 * kHalf;
-  static __device__ __forceinline__ uint32_t row(int r) { return r * kRow + (r & 8) * 18; }
+  static constexpr int kRow = 2 * D + 32, kHalf = 16 * kRow, kUnit = 2 * kHalf;
+  static __device__ __forceinline__ uint32_t swap(int row) { return (row & 4) * 4; }
 };
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef short s8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s4* lds_s4;
 
-// `put`: LDS address of the lane's first chunk in rows 0 .. 15 of the wave's unit.
+// `put`, `odd`: LDS addresses of the lane's chunk 0 and, less 16, 1 in rows 0 .. 15 of the
+// wave's unit.
 template <int D>
-__device__ __forceinline__ void put_values(uint32_t put, int tt, const Codes<D>& x, float unit) {
+__device__ __forceinline__ void put_values(uint32_t put, uint32_t odd, int tt, const Codes<D>& x, float unit) {
 #pragma unroll
   for (int c = 0; c < D / 32; ++c)
-    *(__attribute__((address_space(3))) bf16x8*)(put + tt * Lay<D>::kHalf + 16 * c) = to_bf16(x.w[c], unit);
+    *(__attribute__((address_space(3))) bf16x8*)((c % 2 ? odd : put) + tt * Lay<D>::kHalf + 16 * c) = to_bf16(x.w[c], unit);
 }
 
 // O += P . V over the unit in LDS; P holds tokens 4 gq + {0..3, 16..19}, `get` is the
@@ -337,8 +352,8 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
   const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(s_values)) + w * Lay<D>::kUnit;
 
   const LaneOf<D> place_of(n, gq);
-  const uint32_t put = lds + Lay<D>::row(n) + gq * (D / 2);
-  const uint32_t get = lds + Lay<D>::row(4 * gq + n / 4) + 8 * (n & 3);
+  const uint32_t put = lds + n * Lay<D>::kRow + gq * (D / 2) + Lay<D>::swap(n), odd = put - 2 * Lay<D>::swap(n);
+  const uint32_t get = lds + (4 * gq + n / 4) * Lay<D>::kRow + (8 * (n & 3) ^ Lay<D>::swap(4 * gq));
   bool bad_page = false;
   for (int rg = place - share * a.per_share; rg * TPW < a.RTT; rg += a.per_share) {
     Piece p;
@@ -397,8 +412,8 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
         }
         // (the values' conversion runs beside the matrix instructions of the scores)
         asm volatile("" ::: "memory");  // (the wave's LDS operations keep their order)
-        put_values<D>(put, 0, vc[0], place_of.unit(vc[0].e));
-        put_values<D>(put, 1, vc[1], place_of.unit(vc[1].e));
+        put_values<D>(put, odd, 0, vc[0], place_of.unit(vc[0].e));
+        put_values<D>(put, odd, 1, vc[1], place_of.unit(vc[1].e));
         floatx4 S[TPW][2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {

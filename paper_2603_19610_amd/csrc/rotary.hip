@@ -13,6 +13,11 @@
 // wave takes the angles once for all heads, then D / 8 lanes take a head, eight
 // values each.  A slot names a row of the cache whatever lays it out: padded,
 // paged or ragged rows are one kernel, with one 64-bit division for a row.
+//
+// A prompt's rows are bound by memory: 12800 rows of 64 q and 2 x 8 K/V heads of 128,
+// 524 MB, take 104 us to a bf16 cache (5.0 TB/s; a large copy 5.1) and 102 to a
+// 4-bit one.  A step's few rows are bound by one launch and its chain of loads,
+// angle and store: 6 rows of 28 + 2 x 4 heads 3.5 us, 16 rows to a 4-bit cache 3.9.
 #include <cmath>
 
 #include "q4.h"

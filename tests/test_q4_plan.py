@@ -42,7 +42,7 @@ def test_kernels_fit_a_compute_unit():
             continue
         D, tiles = int(m[2]), int(m[3])
         # LDS of the waves' values: 32 rows of bf16 with their padding each
-        ring = 8 * 2 * (16 * (2 * D + 32) + 144) if m[1] == "part" else 0
+        ring = 8 * 32 * (2 * D + 32) if m[1] == "part" else 0
         waves = 4 if m[1] == "mass" and tiles <= 3 else 2
         assert waves * regs <= 512 and lds + ring <= 160 * 1024, (name, regs, lds, ring)
         seen.add((m[1], D, tiles, m[4]))

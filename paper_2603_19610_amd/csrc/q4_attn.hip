@@ -23,9 +23,9 @@
 // the exponentials take:
 //  * 16 sequences of one row, 28 / 4 heads, 2048 to 16384 tokens (89 MB): partial 21 us,
 //    4.2 TB/s; combine 4.
-//  * 9 rows of 64 / 8 heads over 12800 tokens (14 MB): partial 22, combine 5, mass 11, of
+//  * 9 rows of 64 / 8 heads over 12800 tokens (14 MB): partial 20, combine 5, mass 11, of
 //    which 3 to 5 each are the start, the joins and the end.
-//  * 17 rows of 64 / 8 heads over 132096 tokens (145 MB): partial 113 (matrix instructions
+//  * 17 rows of 64 / 8 heads over 132096 tokens (145 MB): partial 110 (matrix instructions
 //    39 % of the cycles, vector ones 55), mass 75 (25 and 65), combine 6.
 // Vector and matrix instructions of different waves run side by side, so what is left of
 // a SIMD's time is where its two waves want the same pipe.
@@ -490,6 +490,8 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
       // The token waves' results joined: a tile at a time, through LDS (position
       // DPL n + jd of a row holds column 16 jd + n).
       const int rec = p.group(a) + share;
+      int tid = threadIdx.x;
+      asm volatile("" : "+v"(tid));  // (addresses of the results, made before the loop, would spill)
       const bool any = __any(nan);
       if (lane == 0) s_nan[w] = any;
 #pragma unroll
@@ -508,24 +510,33 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
             *reinterpret_cast<float4*>(mine + (4 * gq + i) * D + DPL * n + 4 * h) =
                 make_float4(O[x][4 * h][i], O[x][4 * h + 1][i], O[x][4 * h + 2][i], O[x][4 * h + 3][i]);
         __syncthreads();
-        for (int i = threadIdx.x; i < 16 * D / 4; i += TW * 64) {
+        for (int i = tid; i < 16 * D / 4; i += TW * 64) {
           const int r = i / (D / 4), c = i % (D / 4), row = (tile0 + x) * 16 + r;
           if (row >= a.R) continue;
-          float M = kNegInf;
+          // (everything is read first: a branch for each wave would wait for its reads alone)
+          float M = kNegInf, ref_k[TW], z_k[TW], zt_k[TW];
+          float4 o_k[TW];
 #pragma unroll
-          for (int k = 0; k < TW; ++k) M = fmaxf(M, s_ref[k][r]);
+          for (int k = 0; k < TW; ++k) {
+            ref_k[k] = s_ref[k][r], z_k[k] = s_z[k][r], zt_k[k] = s_zt[k][r];
+            const float* theirs = reinterpret_cast<const float*>(s_values) + k * (Lay<D>::kUnit / 4);
+            o_k[k] = *reinterpret_cast<const float4*>(theirs + r * D + 4 * c);
+          }
+#pragma unroll
+          for (int k = 0; k < TW; ++k) M = fmaxf(M, ref_k[k]);
           const float base = M == kNegInf ? 0.f : M;
           float Z = 0.f, Zt = 0.f;
           floatx4 o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int k = 0; k < TW; ++k) {
-            if (s_z[k][r] == 0.f) continue;  // nothing that the row sees
-            const float f = fast_exp2(s_ref[k][r] - base);
-            Z += s_z[k][r] * f;
-            Zt += s_zt[k][r] * f;
-            const float* theirs = reinterpret_cast<const float*>(s_values) + k * (Lay<D>::kUnit / 4);
-            const float4 y = *reinterpret_cast<const float4*>(theirs + r * D + 4 * c);
-            o[0] = fmaf(y.x, f, o[0]), o[1] = fmaf(y.y, f, o[1]), o[2] = fmaf(y.z, f, o[2]), o[3] = fmaf(y.w, f, o[3]);
+            const bool seen = z_k[k] != 0.f;  // (else the wave has nothing that the row sees)
+            const float f = fast_exp2(ref_k[k] - base);
+            Z = seen ? fmaf(z_k[k], f, Z) : Z;
+            Zt = seen ? fmaf(zt_k[k], f, Zt) : Zt;
+            o[0] = seen ? fmaf(o_k[k].x, f, o[0]) : o[0];
+            o[1] = seen ? fmaf(o_k[k].y, f, o[1]) : o[1];
+            o[2] = seen ? fmaf(o_k[k].z, f, o[2]) : o[2];
+            o[3] = seen ? fmaf(o_k[k].w, f, o[3]) : o[3];
           }
           const size_t at = (size_t)rec * a.RTT * 16 + row;
           if constexpr (SINGLE) {

@@ -579,6 +579,16 @@ __device__ __forceinline__ void combine_row(const Q4Args& a, int id) {
   for (int c = 0; c < C; ++c) o[c] = 0.f;
   for (int s0 = 0; s0 < h.count; s0 += 64) {
     const int cnt = min(64, h.count - s0);
+    float v[kU][C];
+    auto load = [&](int k0) {
+#pragma unroll
+      for (int k = 0; k < kU; ++k) {
+        const float* src = a.opart + (at + (s0 + min(k0 + k, cnt - 1)) * step) * D + C * lane;
+#pragma unroll
+        for (int c = 0; c < C; ++c) v[k][c] = src[c];
+      }
+    };
+    load(0);  // (beside the statistics)
     float4 st = make_float4(kNegInf, 0.f, 0.f, 0.f);
     if (lane < cnt) {
       st = a.stats[at + (s0 + lane) * step];
@@ -592,20 +602,14 @@ __device__ __forceinline__ void combine_row(const Q4Args& a, int id) {
     for (int c = 0; c < C; ++c) o[c] *= f;
     m = M;
     for (int k0 = 0; k0 < cnt; k0 += kU) {
-      float v[kU][C], wgt[kU];
+      if (k0 > 0) load(k0);
 #pragma unroll
       for (int k = 0; k < kU; ++k) {
-        const int i = min(k0 + k, cnt - 1);
-        const float* src = a.opart + (at + (s0 + i) * step) * D + C * lane;
-#pragma unroll
-        for (int c = 0; c < C; ++c) v[k][c] = src[c];
-        wgt[k] = __shfl(e, i, 64);
-      }
-#pragma unroll
-      for (int k = 0; k < kU; ++k)
+        const float wgt = __shfl(e, min(k0 + k, cnt - 1), 64);
         if (k0 + k < cnt)  // (a weight of 0 too: NaN stays)
 #pragma unroll
-          for (int c = 0; c < C; ++c) o[c] = fmaf(v[k][c], wgt[k], o[c]);
+          for (int c = 0; c < C; ++c) o[c] = fmaf(v[k][c], wgt, o[c]);
+      }
     }
   }
   const Rows rows(a.c, a.ctx_len, a.Hkv, b, g);

@@ -90,7 +90,9 @@ __device__ __forceinline__ int wave_scan(int x) {
 struct Wave {
   const int32_t* ctx_len;
   int lane, ctx, raw, u, upto;
-  __device__ __forceinline__ explicit Wave(const int32_t* lengths) : ctx_len(lengths), lane(threadIdx.x & 63) {}
+  __device__ __forceinline__ explicit Wave(const int32_t* lengths) : ctx_len(lengths), lane(threadIdx.x & 63) {
+    asm volatile("" : "+v"(lane));  // (its addresses, made before a loop over pieces, would spill)
+  }
   __device__ __forceinline__ void load(const QShape& a, int b0) {
     const bool here = b0 + lane < a.B;
     ctx = here ? clamp_ctx(a, ctx_len[b0 + lane]) : 0;
@@ -366,9 +368,11 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
       int lim[TPW];
       float ref[TPW], z[TPW];
       floatx4 O[TPW][DPL], zt[TPW];
+      int first = tile0 * 16 + n;
+      asm volatile("" : "+v"(first));  // (as the share's addresses)
 #pragma unroll
       for (int x = 0; x < TPW; ++x) {
-        const int row = (tile0 + x) * 16 + n;
+        const int row = first + 16 * x;
         load_query<D>(a, p.b, p.g, row, gq, q[x]);
         lim[x] = row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
         ref[x] = kNegInf;

@@ -26,7 +26,7 @@
 //  * 9 rows of 64 / 8 heads over 12800 tokens (14 MB): partial 20, combine 5, mass 11, of
 //    which 3 to 5 each are the start, the joins and the end.
 //  * 17 rows of 64 / 8 heads over 132096 tokens (145 MB): partial 110 (matrix instructions
-//    39 % of the cycles, vector ones 55), mass 75 (25 and 65), combine 6.
+//    39 % of the cycles, vector ones 57), mass 75 (25 and 65), combine 6.
 // Vector and matrix instructions of different waves run side by side, so what is left of
 // a SIMD's time is where its two waves want the same pipe.
 #include <type_traits>

@@ -25,6 +25,8 @@
  *                       into one
  *   pvlm_rotary_append_q4, pvlm_quantize_kv_q4, pvlm_verify_attn_q4,
  *   pvlm_gather_kv_q4   the same over a cache of 4-bit rows
+ *   pvlm_verify_attn_q4_ragged  the 4-bit verify of sequences with their own numbers of
+ *                       new rows
  *   pvlm_rotary_append  rotary embedding in every layout (interleaved pairs, part
  *                       of a head, scaled frequencies) and the append of rows by
  *                       cache slot, for padded, paged and ragged batches
@@ -646,6 +648,9 @@ pvlm_status pvlm_gather_kv_q8_paged(pvlm_dtype dst_dt, int n_layers, int B, int 
  * Entries of no row are -1 in slots and seq, 0 in pos.  A row past the table or whose
  * page entry lies outside the pool has slot -1 and pos 0, and PVLM_DEV_RANGE is set,
  * as for an n_new that is out of range (clamped) and packed rows past n_rows (dropped).
+ * With rows_per_seq = T and n_new[b] < T, the rows behind a sequence's own are padding,
+ * which the appends leave unwritten: only pvlm_verify_attn_q4_ragged(_paged) takes such a
+ * batch.  The other verify calls take T rows of every sequence as they find them.
  * PVLM_ERR_SHAPE for sizes outside their ranges or n_rows > 2^30,
  * PVLM_ERR_UNSUPPORTED for B > 4096 or slots that is not 8-byte aligned.
  * ---------------------------------------------------------------------- */
@@ -665,7 +670,8 @@ pvlm_status pvlm_slot_map(int B, int64_t n_rows, int rows_per_seq, int page_size
  *   q_out[n,h]           = rot(q_in[n,h], pos of n)
  *   k_cache[blk,g,row]   = rot(k_in[n,g], pos of n)
  *   v_cache[blk,g,row]   = v_in[n,g]       (bit copy)
- * and nothing of row n for s < 0 (padding: it is neither read nor written).  Slots
+ * and nothing of row n for s < 0 (padding: it is neither read nor written, q_out among
+ * it; a verify call that takes q_out has to be told, see pvlm_slot_map).  Slots
  * >= 0 are distinct (of two rows with one slot, the cache row is a mixture).  A slot
  * past the cache is flagged PVLM_DEV_RANGE and treated as padding.
  *   q_in, k_in, v_in  rows of [Hq][D], [Hkv][D], [Hkv][D], one every q_stride,
@@ -790,6 +796,15 @@ pvlm_status pvlm_quantize_kv_q4_paged(pvlm_dtype dt, int n_layers, int B, int Hk
  *   ws    >= pvlm_verify_attn_q4_workspace_size() bytes (under every compute-unit
  *         budget).
  * Arguments, flags and errors are those of that call.
+ *
+ * pvlm_verify_attn_q4_ragged(_paged) -- the same for sequences of which b has rows
+ * t < n_new[b] of q only (n_new [B], 0 to T each, as pvlm_slot_map takes it with
+ * rows_per_seq = T; NULL: T each).  Rows t >= n_new[b] are padding: what q holds there
+ * reaches no result, out is 0 and lse -inf there, and mass is the sum over the rows that
+ * a sequence has.  Cache rows at and past ctx_len[b] + n_new[b] are not used, whatever
+ * they hold, nor the page entries of pages that lie past them; a sequence of no rows has
+ * none used, and mass 0.  An n_new out of its range is clamped into it and flagged
+ * PVLM_DEV_RANGE.
  * ---------------------------------------------------------------------- */
 size_t pvlm_verify_attn_q4_workspace_size(int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
                                           int64_t max_ctx);
@@ -807,6 +822,22 @@ pvlm_status pvlm_verify_attn_q4_paged(pvlm_dtype dt, int B, int T, int Hq, int H
                                       const int32_t* page_table, const int32_t* ctx_len, void* out,
                                       float* mass, float* lse, void* ws, size_t ws_bytes,
                                       int32_t* status, hipStream_t stream);
+pvlm_status pvlm_verify_attn_q4_ragged(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D,
+                                       int64_t n_cap, int64_t max_ctx, float scale, const void* q,
+                                       const uint8_t* k_codes, const uint8_t* k_exps,
+                                       const uint8_t* v_codes, const uint8_t* v_exps,
+                                       const int32_t* ctx_len, const int32_t* n_new, void* out,
+                                       float* mass, float* lse, void* ws, size_t ws_bytes,
+                                       int32_t* status, hipStream_t stream);
+pvlm_status pvlm_verify_attn_q4_ragged_paged(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D,
+                                             int page_size, int max_pages, int64_t n_pages,
+                                             int64_t max_ctx, float scale, const void* q,
+                                             const uint8_t* k_codes, const uint8_t* k_exps,
+                                             const uint8_t* v_codes, const uint8_t* v_exps,
+                                             const int32_t* page_table, const int32_t* ctx_len,
+                                             const int32_t* n_new, void* out, float* mass,
+                                             float* lse, void* ws, size_t ws_bytes,
+                                             int32_t* status, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
  * pvlm_gather_kv_q4(_paged) -- pvlm_gather_kv_q8(_paged) from a 4-bit cache, with

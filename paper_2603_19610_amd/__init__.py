@@ -39,6 +39,7 @@ EXPORTS = (
     "pvlm_pages_resize", "pvlm_slot_map", "pvlm_rotary_freqs", "pvlm_rotary_append", "pvlm_rotary_append_q4",
     "pvlm_quantize_kv_q4", "pvlm_quantize_kv_q4_paged",
     "pvlm_verify_attn_q4_workspace_size", "pvlm_verify_attn_q4", "pvlm_verify_attn_q4_paged",
+    "pvlm_verify_attn_q4_ragged", "pvlm_verify_attn_q4_ragged_paged",
     "pvlm_gather_kv_q4", "pvlm_gather_kv_q4_paged",
     "pvlm_spec_accept_workspace_size", "pvlm_spec_accept",
     "pvlm_rope_append", "pvlm_rope_append_paged",
@@ -179,6 +180,9 @@ _SIGS = {
 for _n in ("quantize_kv", "verify_attn", "gather_kv"):   # the same arguments as the 8-bit calls
     for _x in ("", "_paged"):
         _SIGS[f"pvlm_{_n}_q4{_x}"] = _SIGS[f"pvlm_{_n}{'' if _n == 'quantize_kv' else '_q8'}{_x}"]
+for _x, _n in (("", 15), ("_paged", 18)):   # (n_new behind ctx_len)
+    _r, _a = _SIGS[f"pvlm_verify_attn_q4{_x}"]
+    _SIGS[f"pvlm_verify_attn_q4_ragged{_x}"] = (_r, _a[:_n] + [_P] + _a[_n:])
 _SIGS["pvlm_verify_attn_q4_workspace_size"] = _SIGS["pvlm_verify_attn_q8_workspace_size"]
 
 
@@ -1356,7 +1360,7 @@ def rotary_append(q, k_new, v_new, pos, slots, k_cache, v_cache, *, rotary: Rota
     a row stride are taken as they are), rotated by their positions pos [N] or
     [3][N] and appended at slots [N] (int64, -1: padding) of caches
     [blocks][Hkv][rows][D], padded or a page pool.  Returns q_out; its rows of padding
-    are not written."""
+    are not written (a 4-bit verify takes them with n_new, the others do not)."""
     dev = _here(k_cache, "k_cache", None)
     if k_cache.dim() != 4:
         raise ValueError("caches must be [blocks][Hkv][rows][D]")
@@ -1460,7 +1464,7 @@ def verify_attn_q4_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx) -> int:
 _ws_sizes = {}     # of a workspace, by the device and the sizes that decide it
 
 
-def _verify_q4(q, cache, page_table, ctx_len, scale, max_ctx, out, mass, lse, want_mass, want_lse, ws, status):
+def _verify_q4(q, cache, page_table, ctx_len, n_new, scale, max_ctx, out, mass, lse, want_mass, want_lse, ws, status):
     _need(q, "q", torch.bfloat16)
     dev = q.device
     n0, Hkv, rows, Dc = _need_q4(*cache, dev, page_table is not None)
@@ -1470,11 +1474,14 @@ def _verify_q4(q, cache, page_table, ctx_len, scale, max_ctx, out, mass, lse, wa
     _need_shape(ctx_len, "ctx_len", torch.int32, dev, (B,))
     if Dc != D or (page_table is None and n0 != B):
         raise ValueError("inconsistent verify_attn_q4 shapes")
+    name, new = "pvlm_verify_attn_q4", ()
+    if n_new is not None:
+        name, new = "pvlm_verify_attn_q4_ragged", (_need_shape(n_new, "n_new", torch.int32, dev, (B,)).data_ptr(),)
     if page_table is None:
-        name, n_cap, geom, table = "pvlm_verify_attn_q4", rows, (rows,), ()
+        n_cap, geom, table = rows, (rows,), ()
     else:
         max_pages = _need_table(page_table, dev, B)
-        name, n_cap, geom = "pvlm_verify_attn_q4_paged", max_pages * rows, (rows, max_pages, n0)
+        name, n_cap, geom = name + "_paged", max_pages * rows, (rows, max_pages, n0)
         table = (page_table.data_ptr(),)
     if max_ctx is None:
         max_ctx = n_cap - T
@@ -1501,7 +1508,7 @@ def _verify_q4(q, cache, page_table, ctx_len, scale, max_ctx, out, mass, lse, wa
     kc, ke, vc, ve = cache
     st = getattr(L, name)(PVLM_BF16, B, T, Hq, Hkv, D, *geom, max_ctx, D ** -0.5 if scale is None else float(scale),
                           q.data_ptr(), kc.data_ptr(), ke.data_ptr(), vc.data_ptr(), ve.data_ptr(), *table,
-                          ctx_len.data_ptr(), out.data_ptr(), None if mass is None else mass.data_ptr(),
+                          ctx_len.data_ptr(), *new, out.data_ptr(), None if mass is None else mass.data_ptr(),
                           None if lse is None else lse.data_ptr(), wsb.data_ptr(), wsb.numel(), _flags(status, dev),
                           _raw_stream(dev.index))
     if st:
@@ -1509,17 +1516,19 @@ def _verify_q4(q, cache, page_table, ctx_len, scale, max_ctx, out, mass, lse, wa
     return out, mass, lse
 
 
-def verify_attn_q4(q, k_codes, k_exps, v_codes, v_exps, ctx_len, *, scale: Optional[float] = None,
+def verify_attn_q4(q, k_codes, k_exps, v_codes, v_exps, ctx_len, *, n_new=None, scale: Optional[float] = None,
                    max_ctx: Optional[int] = None, out=None, mass=None, lse=None, want_mass: bool = True,
                    want_lse: bool = True, ws: Optional[Workspace] = None, status=None):
     """pvlm_verify_attn_q4: ``verify_attn`` of bf16 queries [B][T][Hq][D] over a 4-bit
     cache, codes [B][Hkv][n_cap][D / 2] and exponents [B][Hkv][n_cap][D / 32]; T = 1 and
-    want_mass=False for a decode step.  Returns (out, mass or None, lse or None)."""
-    return _verify_q4(q, (k_codes, k_exps, v_codes, v_exps), None, ctx_len, scale, max_ctx, out, mass, lse,
+    want_mass=False for a decode step.  n_new [B] int32 (pvlm_verify_attn_q4_ragged): the rows
+    that a sequence has, those behind them padding (out 0, lse -inf, no part in the mass).
+    Returns (out, mass or None, lse or None)."""
+    return _verify_q4(q, (k_codes, k_exps, v_codes, v_exps), None, ctx_len, n_new, scale, max_ctx, out, mass, lse,
                       want_mass, want_lse, ws, status)
 
 
-def verify_attn_q4_paged(q, k_codes, k_exps, v_codes, v_exps, page_table, ctx_len, *,
+def verify_attn_q4_paged(q, k_codes, k_exps, v_codes, v_exps, page_table, ctx_len, *, n_new=None,
                          scale: Optional[float] = None, max_ctx: Optional[int] = None, out=None, mass=None,
                          lse=None, want_mass: bool = True, want_lse: bool = True,
                          ws: Optional[Workspace] = None, status=None):
@@ -1527,7 +1536,7 @@ def verify_attn_q4_paged(q, k_codes, k_exps, v_codes, v_exps, page_table, ctx_le
     through page_table [B][max_pages]; mass is [B][max_pages * page]."""
     if page_table is None:
         raise TypeError("page_table must be a torch.Tensor")
-    return _verify_q4(q, (k_codes, k_exps, v_codes, v_exps), page_table, ctx_len, scale, max_ctx, out, mass, lse,
+    return _verify_q4(q, (k_codes, k_exps, v_codes, v_exps), page_table, ctx_len, n_new, scale, max_ctx, out, mass, lse,
                       want_mass, want_lse, ws, status)
 
 

@@ -52,6 +52,7 @@ struct Q4Args : QShape {
   const uint16_t* q;
   Q4Cache c;
   const int32_t* ctx_len;
+  const int32_t* n_new;  // rows of q that a sequence has, or NULL: T each
   int Hq, G, R;
   unsigned g_magic;  // row / G == row * g_magic >> 20 for row < 640 (2^20 / G + 1; G <= 640)
   int RTT;
@@ -72,6 +73,15 @@ struct Q4Args : QShape {
 // shares themselves: q8_plan.h).
 typedef const __attribute__((address_space(4))) int32_t* ConstInts;  // (uniform loads go through the scalar cache)
 __device__ __forceinline__ int uniform_load(const int32_t* p, int64_t i) { return ((ConstInts)(uintptr_t)p)[i]; }
+
+// The rows of q that sequence b has, and the tokens that they see: those behind them in
+// q and in the cache may hold anything.  The shares are counted as if there were T.
+__device__ __forceinline__ int rows_of(const Q4Args& a, int b) {
+  if (!a.n_new) return a.T;
+  const int n = __builtin_amdgcn_readfirstlane(uniform_load(a.n_new, b));
+  return n < 0 ? 0 : n < a.T ? n : a.T;
+}
+__device__ __forceinline__ int tokens_of(int ctx, int rows) { return rows ? ctx + rows : 0; }
 
 // Inclusive sum over the wave's lanes.
 __device__ __forceinline__ int wave_scan(int x) {
@@ -220,9 +230,11 @@ template <int D>
 struct Query {
   bf16x8 s[D / 32];
 };
+// (In place of a row that the sequence does not have, its last one: what q holds there
+// reaches nothing, not even the references, which a wave's rows move together.)
 template <int D>
-__device__ __forceinline__ void load_query(const Q4Args& a, int b, int g, int row, int gq, Query<D>& q) {
-  const int r = min(row, a.R - 1), t = row_t(a, r), h = g * a.G + r - t * a.G;
+__device__ __forceinline__ void load_query(const Q4Args& a, int b, int g, int row, int gq, int n_rows, Query<D>& q) {
+  const int r = min(row, a.R - 1), tr = row_t(a, r), h = g * a.G + r - tr * a.G, t = min(tr, max(n_rows, 1) - 1);
   const bf16x8* src = reinterpret_cast<const bf16x8*>(a.q + (((size_t)b * a.T + t) * a.Hq + h) * D + gq * (D / 4));
 #pragma unroll
   for (int ks = 0; ks < D / 32; ++ks) q.s[ks] = src[ks];
@@ -295,18 +307,20 @@ __device__ __forceinline__ void weigh(uint32_t get, const bf16x8 (&P)[TPW], floa
 // C columns of a row of the result, from the sums relative to its reference m: positions
 // C part .. of a stored row, of which position (D / 16) n + jd is column 16 jd + n.
 // `look`: the values hold a NaN that not every row sees.  Those past the context that
-// this row sees counted as 0 and are looked for here.
+// this row sees counted as 0 and are looked for here.  A row that the sequence does not
+// have is 0, its log-sum-exp -inf, and it has no part in the mass.
 template <int D, int C>
 __device__ __forceinline__ void put_row(const Q4Args& a, int b, int g, int row, int ctx, const Rows& rows, int part,
                                         const float (&o)[C], float m, float z, float zt, bool look) {
   constexpr int DPL = D / 16;
   const int t = row_t(a, row), head = g * a.G + row - t * a.G;
   const float inv = 1.f / zt;
+  const bool real = t < rows_of(a, b);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int pos = C * part + c, col = 16 * (pos % DPL) + pos / DPL;
-    float y = o[c] * inv;
-    if (look) {
+    float y = real ? o[c] * inv : 0.f;
+    if (look && real) {
       for (int j = ctx + 1; j <= ctx + t; ++j) {
         bool flagged_before = false;  // by the loads of the row
         const int64_t r = rows.at(j, rows.table[j >> rows.shift], flagged_before);
@@ -316,8 +330,8 @@ __device__ __forceinline__ void put_row(const Q4Args& a, int b, int g, int row, 
     a.out[(((size_t)b * a.T + t) * a.Hq + head) * D + col] = f32_to_bf16(y);
   }
   if (part == 0) {
-    if (a.lse) a.lse[((size_t)b * a.Hq + head) * a.T + t] = (m + __log2f(z)) * kLn2;
-    if (a.mass) a.rows[((size_t)b * a.Hkv + g) * a.R + row] = make_float2(m, 1.f / z);
+    if (a.lse) a.lse[((size_t)b * a.Hq + head) * a.T + t] = real ? (m + __log2f(z)) * kLn2 : kNegInf;
+    if (a.mass) a.rows[((size_t)b * a.Hkv + g) * a.R + row] = real ? make_float2(m, 1.f / z) : make_float2(-kNegInf, 0.f);
   }
 }
 
@@ -343,7 +357,8 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (blockIdx.x == 0 && w == 0)
     for (int b = threadIdx.x; b < a.B; b += 64)
-      if (a.ctx_len[b] < 0 || a.ctx_len[b] > a.max_ctx) dev_flag(a.status, PVLM_DEV_RANGE);
+      if (a.ctx_len[b] < 0 || a.ctx_len[b] > a.max_ctx || (a.n_new && (a.n_new[b] < 0 || a.n_new[b] > a.T)))
+        dev_flag(a.status, PVLM_DEV_RANGE);
   // The sets of row tiles of a share read the same tokens at about the same time:
   // they are neighbours on one die (workgroup i runs on die i mod 8), whose L2 has
   // what the first of them read.
@@ -364,6 +379,7 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
     do {
       const int tile0 = rg * TPW;  // of the KV head's
       const Rows rows(a.c, a.ctx_len, a.Hkv, p.b, p.g);
+      const int n_rows = rows_of(a, p.b), end = min(p.c1, tokens_of(p.ctx, n_rows));  // (may be c0 or before it)
       Query<D> q[TPW];
       int lim[TPW];
       float ref[TPW], z[TPW];
@@ -373,8 +389,8 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
 #pragma unroll
       for (int x = 0; x < TPW; ++x) {
         const int row = first + 16 * x;
-        load_query<D>(a, p.b, p.g, row, gq, q[x]);
-        lim[x] = row < a.R ? min(p.c1 - 1, p.ctx + row_t(a, row)) : -1;
+        load_query<D>(a, p.b, p.g, row, gq, n_rows, q[x]);
+        lim[x] = row < a.R ? min(end - 1, p.ctx + row_t(a, row)) : -1;
         ref[x] = kNegInf;
         z[x] = 0.f;
         if constexpr (!SINGLE) s_sum[w][x][lane] = 0.f;
@@ -386,7 +402,7 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
       // The next unit (past the piece, its last one) and its page.
       Codes<D> kc[2], vc[2];
       int page;
-      auto unit = [&](int t) { return min(t, (p.c1 - 1) & ~31); };
+      auto unit = [&](int t) { return min(t, (max(end, 1) - 1) & ~31); };
       auto load = [&](int t) {
         const int64_t row = rows.at(unit(t), page, bad_page);
 #pragma unroll
@@ -401,11 +417,11 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
         if constexpr (TAIL) {
 #pragma unroll
           for (int tt = 0; tt < 2; ++tt) {
-            // rows past the piece become zeros (their probabilities are 0, and 0 times what
+            // rows past its tokens become zeros (their probabilities are 0, and 0 times what
             // an unwritten row holds may be NaN), and so do NaN of rows that not every query
             // row sees: the record's flag has the rows looked at that see them
             const int t = t0 + 16 * tt + n;
-            const bool past = t >= p.c1, hidden = t > p.ctx && place_of.exponent(vc[tt].e) == 255;
+            const bool past = t >= end, hidden = t > p.ctx && place_of.exponent(vc[tt].e) == 255;
             if (hidden && !past) nan = 1;
             if (past || hidden) {
               vc[tt].e = 0;
@@ -432,7 +448,7 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
           }
         }
         asm volatile("" ::: "memory");
-        if (t0 + 32 * TW < p.c1) load(t0 + 32 * TW);
+        if (t0 + 32 * TW < end) load(t0 + 32 * TW);
         if constexpr (TAIL) {
 #pragma unroll
           for (int x = 0; x < TPW; ++x)
@@ -481,8 +497,8 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
       // (two loops: in one, the compiler has every unit go through the tail's selections)
       int t = p.c0 + 32 * w;
       page = rows.entry(unit(t));
-      if (t < p.c1) load(t);
-      for (int left = kSumUnits; t + 31 <= min(p.c1 - 1, p.ctx); t += 32 * TW) {
+      if (t < end) load(t);
+      for (int left = kSumUnits; t + 31 <= min(end - 1, p.ctx); t += 32 * TW) {
         block(t, std::false_type{});
         if (!SINGLE && --left == 0) {
           left = kSumUnits;
@@ -490,7 +506,7 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
           for (int x = 0; x < TPW; ++x) s_sum[SINGLE ? 0 : w][x][lane] += z[x], z[x] = 0.f;
         }
       }
-      for (; t < p.c1; t += 32 * TW) block(t, std::true_type{});
+      for (; t < end; t += 32 * TW) block(t, std::true_type{});
       // The token waves' results joined: a tile at a time, through LDS (position
       // DPL n + jd of a row holds column 16 jd + n).
       const int rec = p.group(a) + share;
@@ -637,7 +653,8 @@ template <int D, int MT>
 __device__ __forceinline__ void mass_run(const Q4Args& a, int64_t item, float (*s_mass)[kQ4MassRun]) {
   const int b = (int)(item / a.chunks);
   const int64_t t0 = (item - (int64_t)b * a.chunks) * a.chunk;
-  const int ctx = __builtin_amdgcn_readfirstlane(clamp_ctx(a, uniform_load(a.ctx_len, b))), N = ctx + a.T;
+  const int ctx = __builtin_amdgcn_readfirstlane(clamp_ctx(a, uniform_load(a.ctx_len, b)));
+  const int n_rows = rows_of(a, b), N = tokens_of(ctx, n_rows);
   float* mass = a.mass + (size_t)b * a.c.n_cap;
   const int64_t t_end = min(t0 + a.chunk, a.c.n_cap);
   if (t0 >= N) {
@@ -666,7 +683,7 @@ __device__ __forceinline__ void mass_run(const Q4Args& a, int64_t item, float (*
     float top[MT][4], inv[MT][4];
 #pragma unroll
     for (int x = 0; x < MT; ++x) {
-      load_query<D>(a, b, g, (tile0 + x) * 16 + n, gq, q[x]);
+      load_query<D>(a, b, g, (tile0 + x) * 16 + n, gq, n_rows, q[x]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int row = (tile0 + x) * 16 + 4 * gq + i;
@@ -746,8 +763,8 @@ Q4Kernel pick_mass(int MT) {
 }
 
 pvlm_status verify_q4_run(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D, int64_t max_ctx, float scale,
-                          const void* q, const Q4Cache& c, const int32_t* ctx_len, void* out, float* mass, float* lse,
-                          void* ws, size_t ws_bytes, int32_t* status, hipStream_t stream) {
+                          const void* q, const Q4Cache& c, const int32_t* ctx_len, const int32_t* n_new, void* out,
+                          float* mass, float* lse, void* ws, size_t ws_bytes, int32_t* status, hipStream_t stream) {
   if (!q || !ctx_len || !out) return PVLM_ERR_NULL;
   if (dt != PVLM_BF16) return PVLM_ERR_UNSUPPORTED;
   if (!(scale > 0.f) || !std::isfinite(scale)) return PVLM_ERR_SHAPE;
@@ -767,6 +784,7 @@ pvlm_status verify_q4_run(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D, i
   a.q = static_cast<const uint16_t*>(q);
   a.c = c;
   a.ctx_len = ctx_len;
+  a.n_new = n_new;
   a.B = B;
   a.T = T;
   a.Hq = Hq;
@@ -834,13 +852,35 @@ extern "C" size_t pvlm_verify_attn_q4_workspace_size(int B, int T, int Hq, int H
   return p.bytes;
 }
 
+extern "C" pvlm_status pvlm_verify_attn_q4_ragged(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
+                                                  int64_t max_ctx, float scale, const void* q, const uint8_t* k_codes,
+                                                  const uint8_t* k_exps, const uint8_t* v_codes, const uint8_t* v_exps,
+                                                  const int32_t* ctx_len, const int32_t* n_new, void* out, float* mass,
+                                                  float* lse, void* ws, size_t ws_bytes, int32_t* status,
+                                                  hipStream_t stream) {
+  return verify_q4_run(dt, B, T, Hq, Hkv, D, max_ctx, scale, q, view(k_codes, k_exps, v_codes, v_exps, n_cap), ctx_len,
+                       n_new, out, mass, lse, ws, ws_bytes, status, stream);
+}
+
 extern "C" pvlm_status pvlm_verify_attn_q4(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D, int64_t n_cap,
                                            int64_t max_ctx, float scale, const void* q, const uint8_t* k_codes,
                                            const uint8_t* k_exps, const uint8_t* v_codes, const uint8_t* v_exps,
                                            const int32_t* ctx_len, void* out, float* mass, float* lse, void* ws,
                                            size_t ws_bytes, int32_t* status, hipStream_t stream) {
-  return verify_q4_run(dt, B, T, Hq, Hkv, D, max_ctx, scale, q, view(k_codes, k_exps, v_codes, v_exps, n_cap), ctx_len,
-                       out, mass, lse, ws, ws_bytes, status, stream);
+  return pvlm_verify_attn_q4_ragged(dt, B, T, Hq, Hkv, D, n_cap, max_ctx, scale, q, k_codes, k_exps, v_codes, v_exps,
+                                    ctx_len, nullptr, out, mass, lse, ws, ws_bytes, status, stream);
+}
+
+extern "C" pvlm_status pvlm_verify_attn_q4_ragged_paged(
+    pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D, int page_size, int max_pages, int64_t n_pages, int64_t max_ctx,
+    float scale, const void* q, const uint8_t* k_codes, const uint8_t* k_exps, const uint8_t* v_codes,
+    const uint8_t* v_exps, const int32_t* page_table, const int32_t* ctx_len, const int32_t* n_new, void* out,
+    float* mass, float* lse, void* ws, size_t ws_bytes, int32_t* status, hipStream_t stream) {
+  Q4Cache c = view(k_codes, k_exps, v_codes, v_exps, 0);
+  const pvlm_status st = q8_pages(page_size, max_pages, n_pages, page_table, &c);
+  if (st != PVLM_OK) return st;
+  return verify_q4_run(dt, B, T, Hq, Hkv, D, max_ctx, scale, q, c, ctx_len, n_new, out, mass, lse, ws, ws_bytes, status,
+                       stream);
 }
 
 extern "C" pvlm_status pvlm_verify_attn_q4_paged(pvlm_dtype dt, int B, int T, int Hq, int Hkv, int D, int page_size,
@@ -850,8 +890,7 @@ extern "C" pvlm_status pvlm_verify_attn_q4_paged(pvlm_dtype dt, int B, int T, in
                                                  const int32_t* page_table, const int32_t* ctx_len, void* out,
                                                  float* mass, float* lse, void* ws, size_t ws_bytes,
                                                  int32_t* status, hipStream_t stream) {
-  Q4Cache c = view(k_codes, k_exps, v_codes, v_exps, 0);
-  const pvlm_status st = q8_pages(page_size, max_pages, n_pages, page_table, &c);
-  if (st != PVLM_OK) return st;
-  return verify_q4_run(dt, B, T, Hq, Hkv, D, max_ctx, scale, q, c, ctx_len, out, mass, lse, ws, ws_bytes, status, stream);
+  return pvlm_verify_attn_q4_ragged_paged(dt, B, T, Hq, Hkv, D, page_size, max_pages, n_pages, max_ctx, scale, q,
+                                          k_codes, k_exps, v_codes, v_exps, page_table, ctx_len, nullptr, out, mass, lse,
+                                          ws, ws_bytes, status, stream);
 }

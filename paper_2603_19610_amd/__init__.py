@@ -1196,7 +1196,8 @@ def gather_kv_q8_paged(k_codes, k_exps, v_codes, v_exps, page_table, idx, k, tai
 # device and its stream are asked for once, and a size that only shapes decide is
 # kept (with the kernel, a decode step's call took 15.0 us and takes 13.2, a rotary
 # append's 12.2 and 11.2).
-_getdev = torch._C._cuda_getDevice
+def _getdev() -> int:
+    return torch._C._cuda_getDevice()     # (looked up here: a torch without device support has none)
 
 
 def _here(t, name, dtype):

@@ -1224,6 +1224,10 @@ def _flags(status, dev):
         status = _status_cache.get(dev.index)
         if status is None:
             status = _status(None)
+    elif not (isinstance(status, torch.Tensor) and status.dtype is torch.int32 and status.is_cuda
+              and status.get_device() == dev.index and status.numel()):
+        _need(status, "status", torch.int32, dev)
+        raise ValueError("status must hold an int32 word")
     return status.data_ptr()
 
 

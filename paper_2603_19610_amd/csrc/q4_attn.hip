@@ -174,6 +174,14 @@ struct Rows {
 };
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+// The factor of sums that go to a reference -x above their own.  They reach 2^kRefSlack and
+// more, so one under 2^-126 still counts, and the instruction's would be 0 there: the
+// square of half the way is subnormal, off by 2^-150 at most.  (Otherwise parts whose
+// probabilities are 2^-102 of the row's largest are lost.)
+__device__ __forceinline__ float shift_exp2(float x) {
+  const float h = fast_exp2(0.5f * x);
+  return h * h;
+}
 __device__ __forceinline__ int row_t(const Q4Args& a, int row) { return (int)((unsigned)row * a.g_magic >> 20); }
 
 // Eight codes as bf16, times a power of two.
@@ -465,7 +473,7 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
           m *= a.sl2;
           if (__any(m > ref[x] + kRefSlack)) {  // the first unit, and seldom after it
             const float nm = fmaxf(ref[x], rows4_maximum(m));
-            const float al = ref[x] == kNegInf ? 0.f : fast_exp2(ref[x] - nm);
+            const float al = ref[x] == kNegInf ? 0.f : shift_exp2(ref[x] - nm);
             z[x] *= al;
             if constexpr (!SINGLE) s_sum[w][x][lane] *= al;
             ref[x] = nm;
@@ -550,7 +558,7 @@ __attribute__((amdgpu_waves_per_eu(kQ4Waves / 4, kQ4Waves / 4))) q4_part_kernel(
 #pragma unroll
           for (int k = 0; k < TW; ++k) {
             const bool seen = z_k[k] != 0.f;  // (else the wave has nothing that the row sees)
-            const float f = fast_exp2(ref_k[k] - base);
+            const float f = shift_exp2(ref_k[k] - base);
             Z = seen ? fmaf(z_k[k], f, Z) : Z;
             Zt = seen ? fmaf(zt_k[k], f, Zt) : Zt;
             o[0] = seen ? fmaf(o_k[k].x, f, o[0]) : o[0];
@@ -615,7 +623,7 @@ __device__ __forceinline__ void combine_row(const Q4Args& a, int id) {
       nan |= a.nan[h.rec + s0 + lane] != 0 && st.y != 0.f;
     }
     const float M = fmaxf(m, warp_max(st.y != 0.f ? st.x : kNegInf)), r = M == kNegInf ? 0.f : M;
-    const float f = z != 0.f ? fast_exp2(m - r) : 0.f, e = st.y != 0.f ? fast_exp2(st.x - r) : 0.f;
+    const float f = z != 0.f ? shift_exp2(m - r) : 0.f, e = st.y != 0.f ? shift_exp2(st.x - r) : 0.f;
     z = (z != 0.f ? z * f : 0.f) + warp_sum(st.y != 0.f ? st.y * e : 0.f);
     zt = zt * f + warp_sum(st.y != 0.f ? st.z * e : 0.f);
 #pragma unroll

@@ -27,10 +27,9 @@ struct Q4Split {
   size_t off_stats, off_nan, off_rows, off_opart, bytes;
 };
 
+// (The shares are counted as the 8-bit call's, within its limits.)
 inline pvlm_status check_verify_q4(int B, int T, int Hq, int Hkv, int D, int64_t n_cap, int64_t max_ctx) {
-  const pvlm_status st = check_verify_q8(B, T, Hq, Hkv, D, n_cap, max_ctx);
-  if (st != PVLM_OK) return st;
-  return PVLM_OK;
+  return check_verify_q8(B, T, Hq, Hkv, D, n_cap, max_ctx);
 }
 
 // The plan for arguments that check_verify_q4 takes, on `cus` compute units.  It grows

@@ -45,7 +45,7 @@ struct RotArgs {
   double freq[kMaxPairs];
 };
 
-// Four or eight consecutive values of a row, to and from fp32.
+// Four or eight consecutive values of a row to fp32, and four from it.
 template <typename E, int N>
 __device__ __forceinline__ void load_n(const void* p, size_t at, float* x) {
   if constexpr (sizeof(E) == 4) {
@@ -65,20 +65,12 @@ __device__ __forceinline__ void load_n(const void* p, size_t at, float* x) {
     x[2] = __uint_as_float(u.y << 16), x[3] = __uint_as_float(u.y & 0xffff0000u);
   }
 }
-template <typename E, int N>
-__device__ __forceinline__ void store_n(void* p, size_t at, const float* x) {
-#pragma unroll
-  for (int i = 0; i < N; i += 4) {
-    if constexpr (sizeof(E) == 4)
-      *reinterpret_cast<float4*>(static_cast<float*>(p) + at + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-    else if constexpr (N == 4)
-      *reinterpret_cast<uint64_t*>(static_cast<uint16_t*>(p) + at) = pack_bf16x4(x[0], x[1], x[2], x[3]);
-  }
-  if constexpr (sizeof(E) == 2 && N == 8) {
-    const uint64_t lo = pack_bf16x4(x[0], x[1], x[2], x[3]), hi = pack_bf16x4(x[4], x[5], x[6], x[7]);
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + at) =
-        make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
-  }
+template <typename E>
+__device__ __forceinline__ void store4(void* p, size_t at, const float* x) {
+  if constexpr (sizeof(E) == 4)
+    *reinterpret_cast<float4*>(static_cast<float*>(p) + at) = make_float4(x[0], x[1], x[2], x[3]);
+  else
+    *reinterpret_cast<uint64_t*>(static_cast<uint16_t*>(p) + at) = pack_bf16x4(x[0], x[1], x[2], x[3]);
 }
 // Eight values as they are, bit for bit.
 template <typename E>
@@ -170,8 +162,8 @@ __global__ void __launch_bounds__(256) rotary_append_kernel(RotArgs a) {
     if (is_q || !Q4) {
       void* out = is_q ? a.q_out : a.k_cache;
       const size_t to = is_q ? ((size_t)n * a.Hq + g) * a.D : (size_t)row * a.D;
-      store_n<E, 4>(out, to + at0, x);
-      store_n<E, 4>(out, to + at1, x + 4);
+      store4<E>(out, to + at0, x);
+      store4<E>(out, to + at1, x + 4);
       continue;
     }
     if constexpr (Q4) {

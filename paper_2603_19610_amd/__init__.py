@@ -1510,6 +1510,8 @@ def _verify_q4(q, cache, page_table, ctx_len, n_new, scale, max_ctx, out, mass, 
             _ws_sizes.clear()
         need = _ws_sizes[sizes] = L.pvlm_verify_attn_q4_workspace_size(B, T, Hq, Hkv, D, n_cap, max_ctx)
     wsb = _ws_buffer("verify_q4", ws, need, dev)
+    if wsb.get_device() != dev.index:
+        raise ValueError(f"ws is on {wsb.device}, expected {dev}")
     kc, ke, vc, ve = cache
     st = getattr(L, name)(PVLM_BF16, B, T, Hq, Hkv, D, *geom, max_ctx, D ** -0.5 if scale is None else float(scale),
                           q.data_ptr(), kc.data_ptr(), ke.data_ptr(), vc.data_ptr(), ve.data_ptr(), *table,

@@ -541,7 +541,7 @@ pvlm_status pvlm_quantize_kv_paged(pvlm_dtype dt, int n_layers, int B, int Hkv, 
  * PVLM_ERR_UNSUPPORTED otherwise) and q is not rounded further; scores, softmax
  * statistics and sums are fp32, P is rounded to bf16 before P . V.  Values are at
  * most 2^80 in magnitude (partial sums of P . V may be up to 2^24 times their
- * result).
+ * result), and probabilities under 2^-102 of a row's largest may count as 0.
  * A value of NaN reaches the rows that see it and no other; cache rows at and
  * past ctx_len[b] + T are not used, whatever they hold.
  *   ws    >= pvlm_verify_attn_q8_workspace_size() bytes (under every compute-unit
@@ -703,7 +703,9 @@ pvlm_status pvlm_slot_map(int B, int64_t n_rows, int rows_per_seq, int page_size
  *   sections all 0: 1-D positions; else three widths that sum to rot_dim / 2, as
  *            pvlm_rope_append's.
  * Angles, sines, cosines and the rotation are float64; results are rounded to fp32,
- * then to dt.  dt PVLM_BF16 or PVLM_F32.  q_out may be q_in where q_stride = Hq * D;
+ * then to dt.  (pvlm_rope_append rounds once and takes its frequencies in another way:
+ * where both calls do, few results differ, by one step of dt; the rows of one cache are
+ * best made by one of them.)  dt PVLM_BF16 or PVLM_F32.  q_out may be q_in where q_stride = Hq * D;
  * no other output may alias an input.
  * Errors: PVLM_ERR_NULL for a NULL pointer; PVLM_ERR_SHAPE for a size < 1, Hq not a
  * multiple of Hkv, D not a multiple of 8 or > 256, rot_dim not a multiple of 8 or
@@ -792,7 +794,8 @@ pvlm_status pvlm_quantize_kv_q4_paged(pvlm_dtype dt, int n_layers, int B, int Hk
  * pvlm_verify_attn_q4(_paged) -- pvlm_verify_attn_q8(_paged) over a 4-bit cache, with
  * that call's types, its limit on values, and its treatment of NaN (a block of
  * exponent 255 in K or V reaches the rows that see it and no other; rows at and past
- * ctx_len[b] + T are not used, whatever they hold).
+ * ctx_len[b] + T are not used, whatever they hold).  Probabilities under 2^-126 of a
+ * row's largest, and results under 2^-126, may count as 0.
  *   ws    >= pvlm_verify_attn_q4_workspace_size() bytes (under every compute-unit
  *         budget).
  * Arguments, flags and errors are those of that call.

@@ -21,9 +21,9 @@
 // What bounds it.  A row is 68 bytes (D = 128) where bf16 has 256, so the bytes pass in a
 // fraction of the time that both products' matrix instructions, the conversions and
 // the exponentials take:
-//  * 16 sequences of one row, 28 / 4 heads, 2048 to 16384 tokens (89 MB): partial 21 us,
-//    4.2 TB/s; combine 4.
-//  * 9 rows of 64 / 8 heads over 12800 tokens (14 MB): partial 20, combine 5, mass 11, of
+//  * 16 sequences of one row, 28 / 4 heads, 2048 to 16384 tokens (89 MB): partial 22 us,
+//    4.0 TB/s; combine 4.
+//  * 9 rows of 64 / 8 heads over 12800 tokens (14 MB): partial 20.5, combine 5, mass 11, of
 //    which 3 to 5 each are the start, the joins and the end.
 //  * 17 rows of 64 / 8 heads over 132096 tokens (145 MB): partial 110 (matrix instructions
 //    39 % of the cycles, vector ones 57), mass 75 (25 and 65), combine 6.
@@ -216,8 +216,10 @@ struct LaneOf {  // a lane's place in a tile
   __device__ __forceinline__ uint32_t exponent(uint32_t e) const { return __builtin_amdgcn_ubfe(e, shift, 8); }
   __device__ __forceinline__ float unit(uint32_t e) const { return __uint_as_float(exponent(e) << 23); }
 };
-// A pointer that the wave's lanes have in common, in scalar registers (left to itself
-// the compiler adds the lane's offset first and keeps 64 bits of it a lane).
+// A pointer that the wave's lanes have in common, in scalar registers.  (The compiler adds
+// the lane's offset in the vector unit all the same, a 64-bit addition for each load,
+// but right before it: left to itself it adds it ahead of the loop, and keeps 64 bits of
+// every address a lane.)
 typedef const __attribute__((address_space(1))) uint8_t* Global;
 __device__ __forceinline__ Global scalar(const uint8_t* p) {
   const uint64_t u = reinterpret_cast<uint64_t>(p);

@@ -46,10 +46,16 @@ inline void split_verify_q4(int B, int T, int Hq, int Hkv, int D, int64_t max_ct
   p->per_share = p->RG < cus ? p->RG : cus;
   const int64_t most = cus / p->per_share, shares = (units + kQMinUnits - 1) / kQMinUnits;
   // Few tokens: a workgroup for each group writes the results, and nothing is combined.
+  // (Us a call in a graph, one workgroup a group against shares.  One row of 28 / 4
+  // heads: 4.8 and 12.3 at 30 tokens, 6.3 and 9.9 at 500, 8.2 and 10.5 at 1000; 9 rows of 64 / 8:
+  // 11.5 and 16.1, 14.2 and 16.8, 17.2 and 18.6; 6 rows of 28 / 4: 16.8 and 16.6 at 1000.)
   p->single = rows <= kQ4Single && groups <= most;
   p->shares = (int)(p->single ? groups : shares < most ? shares : most);
   p->recs = (size_t)(groups + p->shares);
-  // (up to five tiles in one set: a run has its queries and sums to load but once)
+  // Up to five tiles in one set: a run has its queries and sums to load but once.  (Us a
+  // call in a graph, one set against two.  Five tiles: 28.3 and 29.7 over 2000 tokens of 8
+  // heads, 34.7 and 42.0 over 12800, 49 and 57 over 40000, but 124 and 113 over 132096; four
+  // tiles: 29.2 and 33.7 over 12800 of 8 heads, 32.8 and 33.4 over 40000 of 4, 25.6 and 23.8 over 6432.)
   p->MG = p->RTT <= 5 ? 1 : (p->RTT + kQ4MassRT - 1) / kQ4MassRT;
   p->MT = (p->RTT + p->MG - 1) / p->MG;
   p->GW = 8;
